@@ -269,6 +269,83 @@ tng_status tng_step(tng_ctx* ctx, uint32_t iter, float* w, float* gref, float* g
  * by the caller and must outlive the calls that record them. */
 tng_status tng_set_profile_events(tng_ctx* ctx, void* const* events, uint32_t slots);
 
+/* ---- Layers of the simulated workers ---------------------------------------------------------------------------------
+ * The linear layers of a network whose gradients the coder above takes (TNG_PROB_EXTERNAL): products of 8-bit codes, their
+ * coders forward and backward, and dropout whose mask is drawn where it is used and never stored.  These calls need no context:
+ * they take the stream (a hipStream_t of the current device, NULL = the default stream), are asynchronous on it, and allocate nothing;
+ * scratch is the caller's, 256-byte aligned, and free again once the stream has passed the call.  Errors as above; sizes of 0 are
+ * allowed everywhere (what a product has to write is then its empty sum), and a call with nothing to write does nothing.
+ *
+ * A matrix is one row-major matrix for each worker.  Codes are int8 in -127 .. 127 with a binary32 scale s for each row:
+ *     R = max |v| of the row, taken as 0 below FLT_MIN;  s = R / 127;
+ *     x = min(max(v (1 / R), -1), 1) 127;  code = x rounded to the nearest integer, halves to even,
+ *     or, for gradients, floor(x) + [u < x - floor(x)] with u = h 2^-16 a 16-bit draw (unbiased to 2^-16 of a step)
+ * in binary32, one rounding per operation.  A row that holds an infinity or a NaN gets s = NaN and unspecified codes: what is
+ * computed from it is NaN.
+ * Draws: element e = row * cols + col of worker m's matrix uses output word e & 3 of the Philox4x32-10 block with counter
+ * (e >> 2, m, iter, stream + 256 site), stream 3 for dropout and 4 for the codes of gradients; at most 2^33 elements for each worker. */
+typedef enum {
+  TNG_TYPE_F32 = 0,
+  TNG_TYPE_BF16 = 1, /* the upper half of a binary32 */
+  TNG_TYPE_F16 = 2,  /* IEEE binary16 */
+  TNG_TYPE_I8 = 3
+} tng_type;
+
+typedef struct {
+  void* data;       /* device, aligned to the type; may be NULL if the matrix has no elements                        */
+  int32_t type;     /* tng_type                                                                                     */
+  uint32_t workers; /* M, 1 <= M <= 65535                                                                           */
+  uint64_t rows;    /* of each worker                                                                               */
+  uint64_t cols;    /* contiguous                                                                                   */
+  uint64_t ld;      /* elements from a row to the next: >= cols, or, for an input, 0 (one row that stands for all)   */
+  uint64_t pitch;   /* elements from a worker's matrix to the next: >= (rows - 1) ld + cols, or, for an input, 0      */
+} tng_matrix;
+
+/* What stands in front of a layer: h = keep f(x) / (1 - p), f(x) = x or max(x, 0) (NaN stays).  An element is kept if
+ * (word >> 8) 2^-24 >= p; 1 / (1 - p) is rounded once to binary32; a dropped element is 0 whatever x is. */
+typedef struct {
+  uint64_t seed;
+  uint32_t iter;
+  uint32_t site; /* which of a network's layers: < 2^24                                                             */
+  float p;       /* 0 <= p < 1; nothing is drawn at p = 0                                                           */
+  int32_t relu;  /* 0 or 1                                                                                         */
+} tng_drop;
+
+/* y = keep f(x) / (1 - p), plus residual (NULL: none), evaluated in binary32 and rounded once.  All matrices of one type (F32,
+ * BF16, F16) and size; y may be x or residual.  Worker m's draws are those of m whatever the strides. */
+tng_status tng_dropout(void* hip_stream, const tng_drop* drop, const tng_matrix* x, const tng_matrix* residual, const tng_matrix* y);
+/* dx = keep f'(x) dy / (1 - p), f'(x) = 0 where x <= 0 with relu.  x: what tng_dropout was given; not read, may be NULL, without relu. */
+tng_status tng_dropout_grad(void* hip_stream, const tng_drop* drop, const tng_matrix* x, const tng_matrix* dy, const tng_matrix* dx);
+
+/* Codes of the rows of h (drop NULL: of x).  x: F32, BF16 or F16, rows <= 2^22, workers * rows <= 2^23, cols <= 2^22; q: int8, of x's size;
+ * scale: device float[workers][rows]; qt: NULL, or int8 [cols][rows] for each worker, the same codes turned (what a product over
+ * the tokens reads). */
+tng_status tng_quantize_rows(void* hip_stream, const tng_drop* drop, const tng_matrix* x, const tng_matrix* q, float* scale,
+                             const tng_matrix* qt);
+
+/* Codes of a gradient dy (workers x rows x cols, limits as above) for the two products of a linear layer's backward pass, both by draws
+ * of the key's stream 4 (p and relu are not used):
+ *   q, q_scale[workers][rows]:   codes of the rows of dy[t][n] col_scale[n]        (h = upper 16 bits of the element's word)
+ *   qt, qt_scale[workers][cols]: codes of the columns of dy[t][n] row_scale[m][t], as rows of [cols][rows]      (lower 16 bits)
+ *   col_sum[workers][cols]:      sums over a worker's rows, binary32 in a fixed order; NULL: not wanted
+ * col_scale: device float[cols], row_scale: device float[workers][rows], NULL: 1. */
+size_t tng_quantize_grad_bytes(const tng_matrix* dy);
+tng_status tng_quantize_grad(void* hip_stream, const tng_drop* key, const tng_matrix* dy, const float* col_scale, const float* row_scale,
+                             const tng_matrix* q, float* q_scale, const tng_matrix* qt, float* qt_scale, float* col_sum, void* workspace,
+                             size_t workspace_bytes);
+
+/* y[m][t][n] = a_scale[m][t] b_scale[n] sum_k a[m][t][k] b[n][k] + bias[n]: the sum is exact, the rest binary32, and y (F32,
+ * BF16 or F16) is rounded once.  a: int8 [rows][depth] for each worker; b: int8 [channels][depth], one for all workers (workers = 1) or one
+ * for each; a_scale: device float[workers][rows], b_scale: device float[channels], or [workers][channels] with a b for each; bias: device float[channels];
+ * scales that are NULL are 1, bias NULL is 0.  rows, channels <= 2^22, workers * rows <= 2^23, depth <= 2^22.
+ * drop, x: NULL, or the gradient of what stood in front of the layer: y is then multiplied by keep f'(x) / (1 - p), with x of y's
+ * type and size as in tng_dropout_grad.
+ * Rows of a and b that begin 16-byte aligned (data, and ld and pitch multiples of 16) take the fast kernels. */
+size_t tng_matmul_i8_bytes(const tng_matrix* a, const tng_matrix* b, const tng_matrix* y);
+tng_status tng_matmul_i8(void* hip_stream, const tng_matrix* a, const float* a_scale, const tng_matrix* b, const float* b_scale,
+                         const float* bias, const tng_drop* drop, const tng_matrix* x, const tng_matrix* y, void* workspace,
+                         size_t workspace_bytes);
+
 #ifdef __cplusplus
 }
 #endif

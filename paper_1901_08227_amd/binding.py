@@ -29,6 +29,7 @@ NORM_NONE, NORM_SUB, NORM_QUOT, NORM_COMB, NORM_MEAN = 0, 1, 2, 3, 4
 SCALE_MAX, SCALE_L2 = 0, 1
 REF_ZERO, REF_LAST_AVG, REF_WINDOW_AVG = 0, 1, 2
 PROB_EXTERNAL, PROB_LOGREG_DENSE, PROB_LOGREG_CSR, PROB_ROSENBROCK = 0, 1, 2, 3
+TYPE_F32, TYPE_BF16, TYPE_F16, TYPE_I8 = 0, 1, 2, 3
 
 
 class TngConfig(ctypes.Structure):
@@ -40,6 +41,16 @@ class TngConfig(ctypes.Structure):
         ("batch", ctypes.c_uint32), ("problem", ctypes.c_int32), ("ref_window", ctypes.c_uint32),
         ("scale", ctypes.c_int32),
     ]
+
+
+class TngMatrix(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("type", ctypes.c_int32), ("workers", ctypes.c_uint32), ("rows", ctypes.c_uint64),
+                ("cols", ctypes.c_uint64), ("ld", ctypes.c_uint64), ("pitch", ctypes.c_uint64)]
+
+
+class TngDrop(ctypes.Structure):
+    _fields_ = [("seed", ctypes.c_uint64), ("iter", ctypes.c_uint32), ("site", ctypes.c_uint32), ("p", ctypes.c_float),
+                ("relu", ctypes.c_int32)]
 
 
 class TngError(RuntimeError):
@@ -109,6 +120,16 @@ def lib() -> ctypes.CDLL:
             "tng_update_reference": [vp, u32, vp, vp],
             "tng_step": [vp, u32, vp, vp, vp, vp, vp, vp],
         }
+        matp, dropp = ctypes.POINTER(TngMatrix), ctypes.POINTER(TngDrop)
+        sigs.update({  # the layer calls: a stream in the place of a context
+            "tng_dropout": [vp, dropp, matp, matp, matp],
+            "tng_dropout_grad": [vp, dropp, matp, matp, matp],
+            "tng_quantize_rows": [vp, dropp, matp, matp, vp, matp],
+            "tng_quantize_grad": [vp, dropp, matp, vp, vp, matp, vp, matp, vp, vp, vp, ctypes.c_size_t],
+            "tng_matmul_i8": [vp, matp, vp, matp, vp, vp, dropp, matp, matp, vp, ctypes.c_size_t],
+        })
+        L.tng_quantize_grad_bytes.restype, L.tng_quantize_grad_bytes.argtypes = ctypes.c_size_t, [matp]
+        L.tng_matmul_i8_bytes.restype, L.tng_matmul_i8_bytes.argtypes = ctypes.c_size_t, [matp, matp, matp]
         for name, argtypes in sigs.items():
             fn = getattr(L, name)
             fn.restype, fn.argtypes = ctypes.c_int, argtypes

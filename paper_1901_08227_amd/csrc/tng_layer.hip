@@ -1,0 +1,494 @@
+// Dropout from the counter-based generator, and the coders of 8-bit products (gfx950).
+#include "tng_layer_device.hpp"
+
+namespace tng {
+namespace {
+
+constexpr int kDropout = 0, kResidual = 1, kGrad = 2, kGradRelu = 3;
+
+template <int KIND>
+__device__ __forceinline__ float dropout_value(float x, float other, bool keep, const DropArgs& d) {
+  if (KIND == kDropout || KIND == kResidual) {
+    const float f = (d.relu ? relu(x) : x) * d.scale;
+    const float y = keep ? f : 0.f;
+    return KIND == kResidual ? other + y : y;
+  }
+  const bool pass = KIND == kGradRelu ? keep && !(other <= 0.f) : keep;  // (x: the gradient, other: what relu was taken of)
+  return pass ? x * d.scale : 0.f;
+}
+
+// Rows without gaps: a worker's elements are one run.  A lane takes 16 bytes of each operand; the two blocks of draws that 8
+// elements need (50 integer instructions a block) hide under the 48 bytes that they move.
+template <typename T, int KIND>
+__global__ void __launch_bounds__(kBlock) dropout_run_kernel(uint64_t n, DropArgs d, View x, View other, View y) {
+  constexpr int N = 16 / sizeof(T);
+  const uint32_t m = blockIdx.y;
+  const uint64_t e = ((uint64_t)blockIdx.x * kBlock + threadIdx.x) * N;
+  if (e >= n) return;
+  const uint64_t left = n - e;
+  float a[N], b[N];
+  load_n_within<T, N>(static_cast<const T*>(x.p) + m * x.pitch + e, left, 0.f, a);
+  if (KIND == kResidual || KIND == kGradRelu) load_n_within<T, N>(static_cast<const T*>(other.p) + m * other.pitch + e, left, 0.f, b);
+  uint32_t word[N];
+  if (d.threshold != 0u) {
+    draw_n<N>(e, true, m, d, word);
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) word[i] = 0u;
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) a[i] = dropout_value<KIND>(a[i], b[i], kept(word[i], d), d);
+  store_n_within<T, N>(static_cast<T*>(y.p) + m * y.pitch + e, left, a);
+}
+
+// Rows with gaps, or of differing pitches: a lane takes one block of four draws, wherever its elements lie.
+template <typename T, int KIND>
+__global__ void __launch_bounds__(kBlock) dropout_rows_kernel(uint64_t rows, uint64_t cols, DropArgs d, View x, View other, View y) {
+  const uint32_t m = blockIdx.y;
+  const uint64_t block = (uint64_t)blockIdx.x * kBlock + threadIdx.x, n = rows * cols;
+  uint64_t e = block * 4;
+  if (e >= n) return;
+  uint32_t word[4] = {0u, 0u, 0u, 0u};
+  if (d.threshold != 0u) draw_n<4>(e, true, m, d, word);
+  uint64_t r = e / cols, c = e - r * cols;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (e + i < n) {
+      const float a = (float)static_cast<const T*>(x.p)[m * x.pitch + r * x.ld + c];
+      float b = 0.f;
+      if (KIND == kResidual || KIND == kGradRelu) b = (float)static_cast<const T*>(other.p)[m * other.pitch + r * other.ld + c];
+      static_cast<T*>(y.p)[m * y.pitch + r * y.ld + c] = (T)dropout_value<KIND>(a, b, kept(word[i], d), d);
+    }
+    if (++c == cols) {
+      c = 0;
+      ++r;
+    }
+  }
+}
+
+template <typename T, int KIND>
+hipError_t dropout_typed(const Extent& n, const DropArgs& d, const View& x, const View& other, const View& y, hipStream_t s) {
+  const uint64_t elements = n.rows * n.cols;
+  const bool two = KIND == kResidual || KIND == kGradRelu;
+  const bool run = n.rows == 1 || (x.ld == n.cols && y.ld == n.cols && (!two || other.ld == n.cols));
+  const uint64_t per = run ? kBlock * (16 / sizeof(T)) : kBlock * 4;
+  const dim3 grid((uint32_t)((elements + per - 1) / per), n.workers);
+  if (run)
+    dropout_run_kernel<T, KIND><<<grid, kBlock, 0, s>>>(elements, d, x, other, y);
+  else
+    dropout_rows_kernel<T, KIND><<<grid, kBlock, 0, s>>>(n.rows, n.cols, d, x, other, y);
+  return hipGetLastError();
+}
+
+template <int KIND>
+hipError_t dropout_kind(tng_type type, const Extent& n, const DropArgs& d, const View& x, const View& other, const View& y,
+                        hipStream_t s) {
+  switch (type) {
+    case TNG_TYPE_F32: return dropout_typed<float, KIND>(n, d, x, other, y, s);
+    case TNG_TYPE_BF16: return dropout_typed<bf16_t, KIND>(n, d, x, other, y, s);
+    default: return dropout_typed<f16_t, KIND>(n, d, x, other, y, s);
+  }
+}
+
+// ---- codes of rows
+
+// The value that is coded, eight at a time: column c .. c + 7 of row r, 0 past the row's end.
+template <typename T, bool DROP>
+__device__ __forceinline__ void coded_values(const T* row, uint64_t c, uint64_t cols, uint64_t first, uint32_t m, const DropArgs& d,
+                                             float (&v)[8]) {
+  load_n_within<T, 8>(row + c, cols - c, 0.f, v);
+  if (DROP) {
+    uint32_t word[8];
+    if (d.threshold != 0u) {
+      draw_n<8>(first + c, (cols & 3u) == 0u, m, d, word);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) word[i] = 0u;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = c + i < cols ? dropped(v[i], word[i], d) : 0.f;
+  }
+}
+
+__device__ __forceinline__ void store_codes8(int8_t* p, uint64_t count, const int (&q)[8]) {
+  if (count >= 8) {
+    typedef uint32_t two __attribute__((ext_vector_type(2), aligned(1)));
+    two v;
+    v.x = (uint32_t)(q[0] & 255) | (uint32_t)(q[1] & 255) << 8 | (uint32_t)(q[2] & 255) << 16 | (uint32_t)q[3] << 24;
+    v.y = (uint32_t)(q[4] & 255) | (uint32_t)(q[5] & 255) << 8 | (uint32_t)(q[6] & 255) << 16 | (uint32_t)q[7] << 24;
+    *reinterpret_cast<two*>(p) = v;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if ((uint64_t)i < count) p[i] = (int8_t)q[i];
+  }
+}
+
+// A workgroup takes one row.  HELD: the row's values stay in registers, HELD times 2048 columns; 0: longer rows are read (and
+// drawn) again for the codes.
+template <typename T, bool DROP, int HELD>
+__global__ void __launch_bounds__(kBlock) quantize_rows_kernel(uint64_t rows, uint64_t cols, DropArgs d, View x, View q, float* scale) {
+  const uint64_t index = blockIdx.x;
+  const uint32_t m = (uint32_t)(index / rows);
+  const uint64_t r = index - m * rows;
+  const T* row = static_cast<const T*>(x.p) + m * x.pitch + r * x.ld;
+  int8_t* out = static_cast<int8_t*>(q.p) + m * q.pitch + r * q.ld;
+  float v[HELD ? HELD : 1][8];
+  uint32_t top = 0u;
+  if (HELD) {
+#pragma unroll
+    for (int k = 0; k < HELD; ++k) {
+      const uint64_t c = (uint64_t)(k * kBlock + threadIdx.x) * 8;
+      if (c < cols) {
+        coded_values<T, DROP>(row, c, cols, r * cols, m, d, v[k]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top = max(top, magnitude_bits(v[k][i]));
+      }
+    }
+  } else {
+    for (uint64_t c = threadIdx.x * 8; c < cols; c += kBlock * 8) {
+      coded_values<T, DROP>(row, c, cols, r * cols, m, d, v[0]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) top = max(top, magnitude_bits(v[0][i]));
+    }
+  }
+  __shared__ uint32_t tops[kBlock / kWave];
+  top = wave_max_bits(top);
+  if (threadIdx.x % kWave == 0) tops[threadIdx.x / kWave] = top;
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < kBlock / kWave; ++k) top = max(top, tops[k]);
+  const float inv = code_inverse(top);
+  if (threadIdx.x == 0) scale[index] = code_step(top);
+  int code[8];
+  if (HELD) {
+#pragma unroll
+    for (int k = 0; k < HELD; ++k) {
+      const uint64_t c = (uint64_t)(k * kBlock + threadIdx.x) * 8;
+      if (c < cols) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) code[i] = code_nearest(v[k][i], inv);
+        store_codes8(out + c, cols - c, code);
+      }
+    }
+  } else {
+    for (uint64_t c = threadIdx.x * 8; c < cols; c += kBlock * 8) {
+      coded_values<T, DROP>(row, c, cols, r * cols, m, d, v[0]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) code[i] = code_nearest(v[0][i], inv);
+      store_codes8(out + c, cols - c, code);
+    }
+  }
+}
+
+template <typename T, bool DROP>
+void quantize_rows_held(const Extent& n, const DropArgs& d, const View& x, const View& q, float* scale, hipStream_t s) {
+  const dim3 grid((uint32_t)(n.workers * n.rows));
+  if (n.cols <= 2048)
+    quantize_rows_kernel<T, DROP, 1><<<grid, kBlock, 0, s>>>(n.rows, n.cols, d, x, q, scale);
+  else if (n.cols <= 4096)
+    quantize_rows_kernel<T, DROP, 2><<<grid, kBlock, 0, s>>>(n.rows, n.cols, d, x, q, scale);
+  else if (n.cols <= 8192)
+    quantize_rows_kernel<T, DROP, 4><<<grid, kBlock, 0, s>>>(n.rows, n.cols, d, x, q, scale);
+  else
+    quantize_rows_kernel<T, DROP, 0><<<grid, kBlock, 0, s>>>(n.rows, n.cols, d, x, q, scale);
+}
+
+// ---- codes the other way round.  A tile is 128 x 128 codes; in LDS they lie as [column][row], 16-byte pieces of a column's 128
+// rows moved by the column's number / 16 so that the writes of a wavefront do not meet in one bank.
+constexpr int kTile = 128;
+
+__device__ __forceinline__ uint32_t turned_at(uint32_t col, uint32_t group) {  // 4-byte word of rows 4 group .. 4 group + 3
+  return col * (kTile / 4) + (group ^ ((col >> 4) << 2));
+}
+
+// words: [kTile][kTile / 4].  Columns c0 .. of a worker's matrix become rows of qt, r0 .. its columns.
+__device__ __forceinline__ void store_turned(const uint32_t* words, const View& qt, uint32_t m, uint64_t r0, uint64_t c0, uint64_t rows,
+                                             uint64_t cols) {
+  typedef uint32_t four __attribute__((ext_vector_type(4)));
+  typedef uint32_t four_any __attribute__((ext_vector_type(4), aligned(1)));
+#pragma unroll
+  for (int k = 0; k < kTile * kTile / 16 / kBlock; ++k) {
+    const uint32_t piece = k * kBlock + threadIdx.x, col = piece / 8, at = piece % 8;
+    const uint64_t r = r0 + at * 16;
+    if (c0 + col >= cols || r >= rows) continue;
+    const four v = *reinterpret_cast<const four*>(words + turned_at(col, at * 4));
+    int8_t* p = static_cast<int8_t*>(qt.p) + m * qt.pitch + (c0 + col) * qt.ld + r;
+    if (rows - r >= 16) {
+      *reinterpret_cast<four_any*>(p) = v;
+    } else {
+#pragma unroll
+      for (uint32_t i = 0; i < 16; ++i)
+        if (i < rows - r) p[i] = (int8_t)(v[i / 4] >> (i % 4 * 8));
+    }
+  }
+}
+
+// Four words of four codes each, turned: byte k of word i becomes byte i of word k.
+__device__ __forceinline__ void turn4(uint32_t (&w)[4]) {
+  const uint32_t a = __builtin_amdgcn_perm(w[1], w[0], 0x05010400u), b = __builtin_amdgcn_perm(w[1], w[0], 0x07030602u);
+  const uint32_t c = __builtin_amdgcn_perm(w[3], w[2], 0x05010400u), e = __builtin_amdgcn_perm(w[3], w[2], 0x07030602u);
+  w[0] = __builtin_amdgcn_perm(c, a, 0x05040100u);
+  w[1] = __builtin_amdgcn_perm(c, a, 0x07060302u);
+  w[2] = __builtin_amdgcn_perm(e, b, 0x05040100u);
+  w[3] = __builtin_amdgcn_perm(e, b, 0x07060302u);
+}
+
+__global__ void __launch_bounds__(kBlock) turn_codes_kernel(uint64_t rows, uint64_t cols, View q, View qt) {
+  __shared__ __align__(16) uint32_t words[kTile * kTile / 4];
+  const uint32_t m = blockIdx.z, chunk = threadIdx.x % 8, group = threadIdx.x / 8;
+  const uint64_t r0 = (uint64_t)blockIdx.y * kTile, c0 = (uint64_t)blockIdx.x * kTile;
+  const uint64_t c = c0 + chunk * 16;
+  typedef uint32_t four __attribute__((ext_vector_type(4), aligned(1)));
+  uint32_t w[4][4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint64_t r = r0 + group * 4 + i;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w[i][k] = 0u;
+    if (r < rows && c < cols) {
+      const int8_t* p = static_cast<const int8_t*>(q.p) + m * q.pitch + r * q.ld + c;
+      if (cols - c >= 16) {
+        const four v = *reinterpret_cast<const four*>(p);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[i][k] = v[k];
+      } else {
+#pragma unroll
+        for (uint32_t k = 0; k < 16; ++k)
+          if (k < cols - c) w[i][k / 4] |= (uint32_t)(uint8_t)p[k] << (k % 4 * 8);
+      }
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    uint32_t t[4] = {w[0][k], w[1][k], w[2][k], w[3][k]};
+    turn4(t);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) words[turned_at(chunk * 16 + k * 4 + j, group)] = t[j];
+  }
+  __syncthreads();
+  store_turned(words, qt, m, r0, c0, rows, cols);
+}
+
+// ---- codes of a gradient
+//
+// dy[t][n] is coded twice: dy[t][n] col_scale[n] along n (one scale a row, for the product with the weights' codes) and
+// dy[t][n] row_scale[t] along t (one scale a column of a worker, for the product with the tokens' codes).  The first kernel takes
+// both kinds of maxima and the columns' sums in one pass, the second puts the pieces together, the third codes.
+constexpr int kStatRows = 128, kStatCols = kWave * 8;
+
+struct GradScratch {
+  float *row_inv, *col_inv;         // [workers][rows], [workers][cols]
+  uint32_t *row_part, *col_part;    // [workers][column tiles][rows], [workers][row chunks][cols]
+  float* sum_part;                  // [workers][row chunks][cols]
+};
+
+template <typename T>
+__global__ void __launch_bounds__(kBlock) grad_stats_kernel(uint64_t rows, uint64_t cols, View dy, const float* col_scale,
+                                                            const float* row_scale, GradScratch out) {
+  constexpr int kWaves = kBlock / kWave;
+  const uint32_t m = blockIdx.z, lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const uint64_t c = (uint64_t)blockIdx.x * kStatCols + lane * 8, r0 = (uint64_t)blockIdx.y * kStatRows;
+  const uint64_t count = c < cols ? cols - c : 0;
+  float scale[8], sum[8];
+  uint32_t top[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    scale[i] = (uint64_t)i < count && col_scale != nullptr ? col_scale[c + i] : 1.f;
+    sum[i] = 0.f;
+    top[i] = 0u;
+  }
+  for (int k = wave; k < kStatRows; k += kWaves) {
+    const uint64_t r = r0 + k;
+    if (r >= rows) break;
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = 0.f;
+    if (count > 0) load_n_within<T, 8>(static_cast<const T*>(dy.p) + m * dy.pitch + r * dy.ld + c, count, 0.f, v);
+    const float s = row_scale != nullptr ? row_scale[m * rows + r] : 1.f;
+    uint32_t t = 0u;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      t = max(t, magnitude_bits(v[i] * scale[i]));
+      if ((uint64_t)i < count) top[i] = max(top[i], magnitude_bits(v[i] * s));
+      sum[i] += v[i];
+    }
+    t = wave_max_bits(t);
+    if (lane == 0) out.row_part[((uint64_t)m * gridDim.x + blockIdx.x) * rows + r] = t;
+  }
+  __shared__ uint32_t tops[kWaves][kStatCols];
+  __shared__ float sums[kWaves][kStatCols];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    tops[wave][lane * 8 + i] = top[i];
+    sums[wave][lane * 8 + i] = sum[i];
+  }
+  __syncthreads();
+  for (uint32_t j = threadIdx.x; j < kStatCols; j += kBlock) {
+    const uint64_t n = (uint64_t)blockIdx.x * kStatCols + j;
+    if (n >= cols) break;
+    uint32_t t = 0u;
+    float a = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      t = max(t, tops[w][j]);
+      a += sums[w][j];
+    }
+    const uint64_t at = ((uint64_t)m * gridDim.y + blockIdx.y) * cols + n;
+    out.col_part[at] = t;
+    out.sum_part[at] = a;
+  }
+}
+
+// One lane a row or a column: rows first (blockIdx.x < row_blocks), then columns.
+__global__ void __launch_bounds__(kBlock) grad_finish_kernel(uint64_t rows, uint64_t cols, uint32_t tiles, uint32_t chunks,
+                                                             uint32_t row_blocks, GradScratch in, float* q_scale, float* qt_scale,
+                                                             float* col_sum) {
+  const uint32_t m = blockIdx.y;
+  const bool by_rows = blockIdx.x < row_blocks;
+  const uint64_t j = (uint64_t)(by_rows ? blockIdx.x : blockIdx.x - row_blocks) * kBlock + threadIdx.x;
+  uint32_t top = 0u;
+  if (by_rows) {
+    if (j >= rows) return;
+    for (uint32_t k = 0; k < tiles; ++k) top = max(top, in.row_part[((uint64_t)m * tiles + k) * rows + j]);
+    in.row_inv[m * rows + j] = code_inverse(top);
+    q_scale[m * rows + j] = code_step(top);
+  } else {
+    if (j >= cols) return;
+    float sum = 0.f;
+    for (uint32_t k = 0; k < chunks; ++k) {
+      const uint64_t at = ((uint64_t)m * chunks + k) * cols + j;
+      top = max(top, in.col_part[at]);
+      sum += in.sum_part[at];
+    }
+    in.col_inv[m * cols + j] = code_inverse(top);
+    qt_scale[m * cols + j] = code_step(top);
+    if (col_sum != nullptr) col_sum[m * cols + j] = sum;
+  }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kBlock) grad_codes_kernel(uint64_t rows, uint64_t cols, DropArgs key, View dy, const float* col_scale,
+                                                            const float* row_scale, GradScratch in, View q, View qt) {
+  __shared__ __align__(16) uint32_t words[kTile * kTile / 4];
+  const uint32_t m = blockIdx.z, chunk = threadIdx.x % 16, group = threadIdx.x / 16;
+  const uint64_t r0 = (uint64_t)blockIdx.y * kTile, c0 = (uint64_t)blockIdx.x * kTile, c = c0 + chunk * 8;
+  const uint64_t count = c < cols ? cols - c : 0;
+  float scale[8], inv[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const bool in_row = (uint64_t)i < count;
+    scale[i] = in_row && col_scale != nullptr ? col_scale[c + i] : 1.f;
+    inv[i] = in_row ? in.col_inv[m * cols + c + i] : 0.f;
+  }
+#pragma unroll 1
+  for (uint32_t half = 0; half < 2; ++half) {
+    const uint32_t g = group + half * 16;
+    uint32_t turned[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const uint64_t r = r0 + g * 4 + k;
+      if (r >= rows || count == 0) continue;
+      float v[8];
+      load_n_within<T, 8>(static_cast<const T*>(dy.p) + m * dy.pitch + r * dy.ld + c, count, 0.f, v);
+      const float row_inv = in.row_inv[m * rows + r], s = row_scale != nullptr ? row_scale[m * rows + r] : 1.f;
+      uint32_t word[8];
+      draw_n<8>(r * cols + c, (cols & 3u) == 0u, m, key, word);
+      int code[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        code[i] = code_drawn(v[i] * scale[i], row_inv, word[i] >> 16);
+        turned[i] |= (uint32_t)(code_drawn(v[i] * s, inv[i], word[i] & 0xFFFFu) & 255) << (8 * k);
+      }
+      store_codes8(static_cast<int8_t*>(q.p) + m * q.pitch + r * q.ld + c, count, code);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) words[turned_at(chunk * 8 + i, g)] = turned[i];
+  }
+  __syncthreads();
+  store_turned(words, qt, m, r0, c0, rows, cols);
+}
+
+GradScratch grad_scratch(const Extent& n, float* p) {
+  const uint64_t tiles = (n.cols + kStatCols - 1) / kStatCols, chunks = (n.rows + kStatRows - 1) / kStatRows;
+  GradScratch g;
+  g.row_inv = p;
+  p += n.workers * n.rows;
+  g.col_inv = p;
+  p += n.workers * n.cols;
+  g.row_part = reinterpret_cast<uint32_t*>(p);
+  p += n.workers * tiles * n.rows;
+  g.col_part = reinterpret_cast<uint32_t*>(p);
+  p += n.workers * chunks * n.cols;
+  g.sum_part = p;
+  return g;
+}
+
+template <typename T>
+hipError_t quantize_grad_typed(const Extent& n, const DropArgs& key, const View& dy, const float* col_scale, const float* row_scale,
+                               const View& q, float* q_scale, const View& qt, float* qt_scale, float* col_sum, float* scratch,
+                               hipStream_t s) {
+  const GradScratch g = grad_scratch(n, scratch);
+  const uint32_t tiles = (uint32_t)((n.cols + kStatCols - 1) / kStatCols), chunks = (uint32_t)((n.rows + kStatRows - 1) / kStatRows);
+  const bool none = n.rows == 0 || n.cols == 0;  // (scales and sums are 0 then)
+  if (!none) grad_stats_kernel<T><<<dim3(tiles, chunks, n.workers), kBlock, 0, s>>>(n.rows, n.cols, dy, col_scale, row_scale, g);
+  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  const uint32_t row_blocks = (uint32_t)((n.rows + kBlock - 1) / kBlock), col_blocks = (uint32_t)((n.cols + kBlock - 1) / kBlock);
+  grad_finish_kernel<<<dim3(row_blocks + col_blocks, n.workers), kBlock, 0, s>>>(n.rows, n.cols, tiles, chunks, row_blocks, g, q_scale,
+                                                                                 qt_scale, col_sum);
+  if (hipError_t e = hipGetLastError(); e != hipSuccess || none) return e;
+  const dim3 grid((uint32_t)((n.cols + kTile - 1) / kTile), (uint32_t)((n.rows + kTile - 1) / kTile), n.workers);
+  grad_codes_kernel<T><<<grid, kBlock, 0, s>>>(n.rows, n.cols, key, dy, col_scale, row_scale, g, q, qt);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_dropout(tng_type type, const Extent& n, const DropArgs& d, const View& x, const View& residual, const View& y,
+                          hipStream_t s) {
+  return residual.p != nullptr ? dropout_kind<kResidual>(type, n, d, x, residual, y, s) : dropout_kind<kDropout>(type, n, d, x, residual, y, s);
+}
+
+hipError_t launch_dropout_grad(tng_type type, const Extent& n, const DropArgs& d, const View& x, const View& dy, const View& dx,
+                               hipStream_t s) {
+  return d.relu ? dropout_kind<kGradRelu>(type, n, d, dy, x, dx, s) : dropout_kind<kGrad>(type, n, d, dy, x, dx, s);
+}
+
+hipError_t launch_quantize_rows(tng_type type, const Extent& n, const DropArgs* drop, const View& x, const View& q, float* scale,
+                                const View& qt, hipStream_t s) {
+  const DropArgs d = drop != nullptr ? *drop : DropArgs{};
+  switch (type) {
+    case TNG_TYPE_F32:
+      drop ? quantize_rows_held<float, true>(n, d, x, q, scale, s) : quantize_rows_held<float, false>(n, d, x, q, scale, s);
+      break;
+    case TNG_TYPE_BF16:
+      drop ? quantize_rows_held<bf16_t, true>(n, d, x, q, scale, s) : quantize_rows_held<bf16_t, false>(n, d, x, q, scale, s);
+      break;
+    default:
+      drop ? quantize_rows_held<f16_t, true>(n, d, x, q, scale, s) : quantize_rows_held<f16_t, false>(n, d, x, q, scale, s);
+  }
+  if (hipError_t e = hipGetLastError(); e != hipSuccess || qt.p == nullptr) return e;
+  const dim3 grid((uint32_t)((n.cols + kTile - 1) / kTile), (uint32_t)((n.rows + kTile - 1) / kTile), n.workers);
+  turn_codes_kernel<<<grid, kBlock, 0, s>>>(n.rows, n.cols, q, qt);
+  return hipGetLastError();
+}
+
+size_t quantize_grad_floats(const Extent& n) {
+  const uint64_t tiles = (n.cols + kStatCols - 1) / kStatCols, chunks = (n.rows + kStatRows - 1) / kStatRows;
+  return n.workers * (n.rows + n.cols + tiles * n.rows + 2 * chunks * n.cols);
+}
+
+hipError_t launch_quantize_grad(tng_type type, const Extent& n, const DropArgs& key, const View& dy, const float* col_scale,
+                                const float* row_scale, const View& q, float* q_scale, const View& qt, float* qt_scale, float* col_sum,
+                                float* scratch, hipStream_t s) {
+  switch (type) {
+    case TNG_TYPE_F32:
+      return quantize_grad_typed<float>(n, key, dy, col_scale, row_scale, q, q_scale, qt, qt_scale, col_sum, scratch, s);
+    case TNG_TYPE_BF16:
+      return quantize_grad_typed<bf16_t>(n, key, dy, col_scale, row_scale, q, q_scale, qt, qt_scale, col_sum, scratch, s);
+    default:
+      return quantize_grad_typed<f16_t>(n, key, dy, col_scale, row_scale, q, q_scale, qt, qt_scale, col_sum, scratch, s);
+  }
+}
+
+}  // namespace tng
