@@ -59,6 +59,7 @@ struct Product {
   tng_type type;
   const DropArgs* drop;
   View x;  // of y's type, read only with relu
+  uint64_t rows_of_worker;  // set by launch_product
 };
 size_t product_scratch_bytes(const Product& p);
 hipError_t launch_product(const Product& p, void* scratch, hipStream_t s);
