@@ -61,16 +61,17 @@ class TngError(RuntimeError):
 
 _lib = None
 _call = None      # the extension's call() or _through_ctypes; set with the library
+_layer = None     # its layer() or _through_ctypes
 _address = None   # {entry point: its address} of those that go through it
 
 
 def _through_ctypes(*_):
-    """In the place of tng_call.call: no case is plain."""
+    """In the place of the extension's functions: no case is plain."""
     return None
 
 
-def _load_call():
-    """tng_call.call of the built extension; _through_ctypes where there is none that fits this torch and Python."""
+def _load_call(name="call"):
+    """A function of the built extension; _through_ctypes where there is none that fits this torch and Python."""
     if not os.path.exists(CALL_PATH):
         return _through_ctypes
     try:
@@ -79,12 +80,12 @@ def _load_call():
         loader.exec_module(module)
     except ImportError:
         return _through_ctypes
-    return module.call if getattr(module, "built_for", None) == build.call_target() else _through_ctypes
+    return getattr(module, name) if getattr(module, "built_for", None) == build.call_target() else _through_ctypes
 
 
 def lib() -> ctypes.CDLL:
     """The loaded library; raises if it has not been built (python -m paper_1901_08227_amd.build)."""
-    global _lib, _call, _address
+    global _lib, _call, _layer, _address
     if _lib is None:
         if not os.path.exists(LIB_PATH):
             raise RuntimeError(f"libtng is not built: {LIB_PATH} is missing; run __graft_entry__.build()")
@@ -133,10 +134,11 @@ def lib() -> ctypes.CDLL:
         for name, argtypes in sigs.items():
             fn = getattr(L, name)
             fn.restype, fn.argtypes = ctypes.c_int, argtypes
-        _call = _load_call()
+        _call, _layer = _load_call(), _load_call("layer")
         _address = {name: ctypes.cast(getattr(L, name), vp).value
                     for name in ("tng_local_grad", "tng_normalize_encode", "tng_decode_aggregate", "tng_update_reference",
-                                 "tng_step")}
+                                 "tng_step", "tng_dropout", "tng_dropout_grad", "tng_quantize_rows", "tng_quantize_grad",
+                                 "tng_quantize_grad_bytes", "tng_matmul_i8", "tng_matmul_i8_bytes")}
         _lib = L
     return _lib
 

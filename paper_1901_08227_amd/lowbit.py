@@ -48,8 +48,19 @@ class Saved(NamedTuple):
     qt: torch.Tensor           # the tokens' codes turned, [M, depth, rows]
 
 
+_I8 = {torch.int8: B.TYPE_I8}
+# The arguments of the layer calls behind the stream, a letter each (see csrc/tng_call.cpp), and what they are called here.
+_CALLS = {
+    "tng_dropout": ("dmmm", ("drop", "x", "residual", "out")),
+    "tng_dropout_grad": ("dmmm", ("drop", "x", "dy", "out")),
+    "tng_quantize_rows": ("dmiri", ("drop", "x", "q", "scale", "qt")),
+    "tng_quantize_grad": ("dmcririrrw", ("key", "dy", "col_scale", "row_scale", "q", "q_scale", "qt", "qt_scale", "col_sum")),
+    "tng_matmul_i8": ("irirndmmW", ("a", "a_scale", "b", "b_scale", "bias", "drop", "x", "out")),
+}
+
+
 def _matrix(t, dtypes, name):
-    """(tng_matrix, M, rows, cols) of a tensor."""
+    """The tng_matrix of a tensor."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name}: expected a CUDA tensor")
     kind = dtypes.get(t.dtype)
@@ -67,85 +78,104 @@ def _matrix(t, dtypes, name):
     return B.TngMatrix(t.data_ptr(), kind, workers, shape[-2], shape[-1], stride[-2], pitch)
 
 
-_I8 = {torch.int8: B.TYPE_I8}
-
-
-def _vector(t, shape, name, device):
-    """Address of a contiguous float32 tensor of that shape (None: no address)."""
-    if t is None:
-        return None
-    if not isinstance(t, torch.Tensor) or t.device != device or t.dtype != torch.float32 or not t.is_contiguous():
-        raise TypeError(f"{name}: expected contiguous float32 on {device}")
-    if t.numel() != shape:
-        raise ValueError(f"{name}: needs {shape} elements, has {t.numel()}")
+def _vector(t, n, name):
+    """Address of a contiguous float32 tensor of n elements."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != torch.float32 or not t.is_contiguous():
+        raise TypeError(f"{name}: expected contiguous float32 on the GPU")
+    if t.numel() != n:
+        raise ValueError(f"{name}: needs {n} elements, has {t.numel()}")
     return t.data_ptr()
 
 
-def _same_device(device, *tensors):
-    for t in tensors:
-        if t is not None and t.device != device:
-            raise ValueError(f"tensors on {device} and {t.device}")
-
-
 def _drop(d):
-    return B.TngDrop(int(d.seed) & 0xFFFFFFFFFFFFFFFF, int(d.iter) & 0xFFFFFFFF, int(d.site), float(d.p), int(bool(d.relu)))
+    return B.TngDrop(int(d[0]) & 0xFFFFFFFFFFFFFFFF, int(d[1]) & 0xFFFFFFFF, int(d[2]), float(d[3]), int(bool(d[4])))
 
 
-def _stream(device):
-    return ctypes.c_void_p(torch.cuda.current_stream(device).cuda_stream)
+def _through_ctypes(name, kinds, names, device, stream, args):
+    """The call with arguments that the native function does not take as plain: converts them, or says what is wrong."""
+    L, values, matrices = B.lib(), [], []
+    for kind, what, arg in zip(kinds, names, args):
+        if isinstance(arg, torch.Tensor) and arg.is_cuda and arg.device != device:
+            raise ValueError(f"{what}: on {arg.device}, the others on {device}")
+        if arg is None:
+            values.append(None)
+        elif kind == "d":
+            values.append(_drop(arg))
+        elif kind in "mi":
+            values.append(_matrix(arg, _TYPES if kind == "m" else _I8, what))
+            matrices.append(values[-1])
+        else:
+            m = matrices[-1]
+            values.append(_vector(arg, {"r": m.workers * m.rows, "n": m.rows, "c": m.cols}[kind], what))
+    if kinds[-1] in "wW":  # (the library sizes what it refuses as 0, and says so when it is called)
+        sized = matrices[:1] if kinds[-1] == "w" else [*matrices[:2], matrices[-1]]
+        scratch = torch.empty(getattr(L, name + "_bytes")(*sized), dtype=torch.uint8, device=device)
+        values += [scratch.data_ptr(), scratch.numel()]
+    return getattr(L, name)(ctypes.c_void_p(stream), *values)
 
 
-def _scratch(nbytes, device):
-    # (the library sizes what it refuses as 0, and says so when it is called)
-    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+def _run(name, device, *args):
+    """A layer call on the current stream of the device, by the native function where its arguments are plain."""
+    if device.type != "cuda":
+        raise TypeError(f"{name}: expected CUDA tensors")
+    if device.index != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            return _run(name, device, *args)
+    B.lib()
+    kinds, names = _CALLS[name]
+    stream = torch._C._cuda_getCurrentRawStream(device.index)
+    status = B._layer(B._address[name], B._address.get(name + "_bytes", 0), stream, kinds, *args)
+    if status is None:
+        status = _through_ctypes(name, kinds, names, device, stream, args)
+    B._check(status, name)
 
 
 def _codes(shape, device):
     """int8 codes whose rows begin 16 bytes apart, which the products' fast kernels ask for."""
     cols = shape[-1]
-    held = torch.empty((*shape[:-1], -(-cols // 16) * 16), dtype=torch.int8, device=device)
-    return held[..., :cols]
+    if cols % 16 == 0:
+        return torch.empty(shape, dtype=torch.int8, device=device)
+    return torch.empty((*shape[:-1], -(-cols // 16) * 16), dtype=torch.int8, device=device)[..., :cols]
 
 
-def _out(out, shape, dtype, device, name):
+def _floats(shape, device):
+    return torch.empty(shape, dtype=torch.float32, device=device)
+
+
+def _out(out, shape, dtype, device):
     if out is None:
         return torch.empty(shape, dtype=dtype, device=device)
     if tuple(out.shape) != tuple(shape) or out.dtype != dtype or out.device != device:
-        raise ValueError(f"{name}: expected {tuple(shape)} {dtype} on {device}")
+        raise ValueError(f"out: expected {tuple(shape)} {dtype} on {device}")
     return out
+
+
+def _dims(t, name):
+    if t.dim() not in (2, 3):
+        raise ValueError(f"{name}: expected [rows, cols] or [M, rows, cols], got {tuple(t.shape)}")
+    return t.shape
 
 
 def dropout(x, drop, residual=None, out=None):
     """keep f(x) / (1 - p), plus the residual if there is one."""
-    mx = _matrix(x, _TYPES, "x")
-    out = _out(out, x.shape, x.dtype, x.device, "out")
-    _same_device(x.device, residual)
-    mr = None if residual is None else _matrix(residual, _TYPES, "residual")
-    with torch.cuda.device(x.device):
-        B._check(B.lib().tng_dropout(_stream(x.device), _drop(drop), mx, mr, _matrix(out, _TYPES, "out")), "tng_dropout")
+    out = _out(out, x.shape, x.dtype, x.device)
+    _run("tng_dropout", x.device, drop, x, residual, out)
     return out
 
 
 def dropout_grad(dy, drop, x=None, out=None):
     """The gradient of dropout's x from that of its result; x is needed if there is a relu."""
-    md = _matrix(dy, _TYPES, "dy")
-    out = _out(out, dy.shape, dy.dtype, dy.device, "out")
-    _same_device(dy.device, x)
-    mx = None if x is None else _matrix(x, _TYPES, "x")
-    with torch.cuda.device(dy.device):
-        B._check(B.lib().tng_dropout_grad(_stream(dy.device), _drop(drop), mx, md, _matrix(out, _TYPES, "out")), "tng_dropout_grad")
+    out = _out(out, dy.shape, dy.dtype, dy.device)
+    _run("tng_dropout_grad", dy.device, drop, x, dy, out)
     return out
 
 
 def quantize_rows(x, drop=None, turned=False):
     """(codes, scales) of x's rows, or of what drop makes of them; turned: (codes, scales, turned codes)."""
-    mx = _matrix(x, _TYPES, "x")
-    q = _codes(x.shape, x.device)
-    scale = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
-    qt = _codes((*x.shape[:-2], x.shape[-1], x.shape[-2]), x.device) if turned else None
-    with torch.cuda.device(x.device):
-        B._check(B.lib().tng_quantize_rows(_stream(x.device), None if drop is None else _drop(drop), mx, _matrix(q, _I8, "q"),
-                                           scale.data_ptr(), None if qt is None else _matrix(qt, _I8, "qt")), "tng_quantize_rows")
+    shape, device = _dims(x, "x"), x.device
+    q, scale = _codes(shape, device), _floats(shape[:-1], device)
+    qt = _codes((*shape[:-2], shape[-1], shape[-2]), device) if turned else None
+    _run("tng_quantize_rows", device, drop, x, q, scale, qt)
     return (q, scale, qt) if turned else (q, scale)
 
 
@@ -156,38 +186,19 @@ def weight(w, turned=True):
 
 def quantize_grad(dy, col_scale=None, row_scale=None, *, seed, iter, site, sums=True):
     """(q, q_scale, qt, qt_scale, col_sum): the codes of dy col_scale by rows and of dy row_scale by columns, and dy's column sums."""
-    m = _matrix(dy, _TYPES, "dy")
-    dev, lead = dy.device, dy.shape[:-2]
-    rows, cols = dy.shape[-2:]
-    q, qt = _codes(dy.shape, dev), _codes((*lead, cols, rows), dev)
-    q_scale = torch.empty((*lead, rows), dtype=torch.float32, device=dev)
-    qt_scale = torch.empty((*lead, cols), dtype=torch.float32, device=dev)
-    col_sum = torch.empty((*lead, cols), dtype=torch.float32, device=dev) if sums else None
-    scratch = _scratch(B.lib().tng_quantize_grad_bytes(m), dev)
-    with torch.cuda.device(dev):
-        B._check(B.lib().tng_quantize_grad(
-            _stream(dev), _drop(Drop(seed, iter, site)), m, _vector(col_scale, cols, "col_scale", dev),
-            _vector(row_scale, m.workers * rows, "row_scale", dev), _matrix(q, _I8, "q"), q_scale.data_ptr(), _matrix(qt, _I8, "qt"),
-            qt_scale.data_ptr(), col_sum.data_ptr() if sums else None, scratch.data_ptr(), scratch.numel()), "tng_quantize_grad")
+    (*lead, rows, cols), device = _dims(dy, "dy"), dy.device
+    q, qt = _codes((*lead, rows, cols), device), _codes((*lead, cols, rows), device)
+    q_scale, qt_scale = _floats((*lead, rows), device), _floats((*lead, cols), device)
+    col_sum = _floats((*lead, cols), device) if sums else None
+    _run("tng_quantize_grad", device, Drop(seed, iter, site), dy, col_scale, row_scale, q, q_scale, qt, qt_scale, col_sum)
     return q, q_scale, qt, qt_scale, col_sum
 
 
 def matmul_i8(a, b, a_scale=None, b_scale=None, bias=None, dtype=torch.float32, out=None, drop=None, x=None):
     """a_scale b_scale (a b^T) + bias: codes a [rows, depth] or [M, rows, depth], b [channels, depth] or one for each worker.
     drop, x: the result is a gradient that goes on through that dropout (and its relu, of x)."""
-    ma, mb = _matrix(a, _I8, "a"), _matrix(b, _I8, "b")
-    dev = a.device
-    _same_device(dev, b, x)
-    out = _out(out, (*a.shape[:-1], b.shape[-2]), dtype, dev, "out")
-    my = _matrix(out, _TYPES, "out")
-    mx = None if x is None else _matrix(x, _TYPES, "x")
-    L = B.lib()
-    scratch = _scratch(L.tng_matmul_i8_bytes(ma, mb, my), dev)
-    with torch.cuda.device(dev):
-        B._check(L.tng_matmul_i8(
-            _stream(dev), ma, _vector(a_scale, ma.workers * ma.rows, "a_scale", dev), mb,
-            _vector(b_scale, mb.workers * mb.rows, "b_scale", dev), _vector(bias, mb.rows, "bias", dev),
-            None if drop is None else _drop(drop), mx, my, scratch.data_ptr(), scratch.numel()), "tng_matmul_i8")
+    out = _out(out, (*_dims(a, "a")[:-1], _dims(b, "b")[-2]), dtype, a.device)
+    _run("tng_matmul_i8", a.device, a, a_scale, b, b_scale, bias, drop, x, out)
     return out
 
 
