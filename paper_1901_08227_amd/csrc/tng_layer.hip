@@ -1,6 +1,8 @@
 // Dropout from the counter-based generator, and the coders of 8-bit products (gfx950).
 #include "tng_layer_device.hpp"
 
+#include <type_traits>
+
 namespace tng {
 namespace {
 
@@ -19,13 +21,11 @@ __device__ __forceinline__ float dropout_value(float x, float other, bool keep, 
 
 // Rows without gaps: a worker's elements are one run.  A lane takes 16 bytes of each operand; the two blocks of draws that 8
 // elements need (50 integer instructions a block) hide under the 48 bytes that they move.
-template <typename T, int KIND>
-__global__ void __launch_bounds__(kBlock) dropout_run_kernel(uint64_t n, DropArgs d, View x, View other, View y) {
+template <typename T, int KIND, bool WHOLE>
+__device__ __forceinline__ void dropout_piece(uint64_t e, uint64_t n, uint32_t m, const DropArgs& d, const View& x, const View& other,
+                                              const View& y) {
   constexpr int N = 16 / sizeof(T);
-  const uint32_t m = blockIdx.y;
-  const uint64_t e = ((uint64_t)blockIdx.x * kBlock + threadIdx.x) * N;
-  if (e >= n) return;
-  const uint64_t left = n - e;
+  const uint64_t left = WHOLE ? N : n - e;  // (WHOLE: known to the compiler, so no load is under a condition)
   float a[N], b[N];
   load_n_within<T, N>(static_cast<const T*>(x.p) + m * x.pitch + e, left, 0.f, a);
   if (KIND == kResidual || KIND == kGradRelu) load_n_within<T, N>(static_cast<const T*>(other.p) + m * other.pitch + e, left, 0.f, b);
@@ -39,6 +39,16 @@ __global__ void __launch_bounds__(kBlock) dropout_run_kernel(uint64_t n, DropArg
 #pragma unroll
   for (int i = 0; i < N; ++i) a[i] = dropout_value<KIND>(a[i], b[i], kept(word[i], d), d);
   store_n_within<T, N>(static_cast<T*>(y.p) + m * y.pitch + e, left, a);
+}
+
+template <typename T, int KIND>
+__global__ void __launch_bounds__(kBlock) dropout_run_kernel(uint64_t n, DropArgs d, View x, View other, View y) {
+  constexpr int N = 16 / sizeof(T);
+  const uint64_t first = (uint64_t)blockIdx.x * (kBlock * N), e = first + threadIdx.x * N;
+  if (first + kBlock * N <= n)
+    dropout_piece<T, KIND, true>(e, n, blockIdx.y, d, x, other, y);
+  else if (e < n)
+    dropout_piece<T, KIND, false>(e, n, blockIdx.y, d, x, other, y);
 }
 
 // Rows with gaps, or of differing pitches: a lane takes one block of four draws, wherever its elements lie.
@@ -92,65 +102,122 @@ hipError_t dropout_kind(tng_type type, const Extent& n, const DropArgs& d, const
 
 // ---- codes of rows
 
-// The value that is coded, eight at a time: column c .. c + 7 of row r, 0 past the row's end.
-template <typename T, bool DROP>
-__device__ __forceinline__ void coded_values(const T* row, uint64_t c, uint64_t cols, uint64_t first, uint32_t m, const DropArgs& d,
-                                             float (&v)[8]) {
-  load_n_within<T, 8>(row + c, cols - c, 0.f, v);
-  if (DROP) {
-    uint32_t word[8];
-    if (d.threshold != 0u) {
-      draw_n<8>(first + c, (cols & 3u) == 0u, m, d, word);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) word[i] = 0u;
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = c + i < cols ? dropped(v[i], word[i], d) : 0.f;
-  }
+// A lane takes eight columns.  Where a row ends inside them it takes the row's last eight instead: what two lanes have of one column is the
+// same, and so is what they write there.  No load is under a condition, so many are under way together (a load that only some lanes
+// make is waited for where the ways join again).  NARROW: rows of less than eight columns.
+template <bool NARROW>
+__device__ __forceinline__ uint64_t eight_at(uint64_t c, uint64_t cols) {
+  return NARROW ? c : min(c, cols - 8);
 }
 
-__device__ __forceinline__ void store_codes8(int8_t* p, uint64_t count, const int (&q)[8]) {
-  if (count >= 8) {
-    typedef uint32_t two __attribute__((ext_vector_type(2), aligned(1)));
-    two v;
-    v.x = (uint32_t)(q[0] & 255) | (uint32_t)(q[1] & 255) << 8 | (uint32_t)(q[2] & 255) << 16 | (uint32_t)q[3] << 24;
-    v.y = (uint32_t)(q[4] & 255) | (uint32_t)(q[5] & 255) << 8 | (uint32_t)(q[6] & 255) << 16 | (uint32_t)q[7] << 24;
+template <typename T, bool NARROW>
+__device__ __forceinline__ void load8(const T* row, uint64_t c, uint64_t cols, float (&v)[8]) {
+  if (NARROW)
+    load_n_within<T, 8>(row + c, c < cols ? cols - c : 0, 0.f, v);
+  else
+    load_n<T, 8>(row + c, v);
+}
+
+// The same as they lie, for loads that are under way while something else is worked on.
+template <typename T, bool NARROW>
+struct Raw8 {
+  typedef T vec __attribute__((ext_vector_type(8), aligned(alignof(T))));
+  vec v;
+  __device__ __forceinline__ void load(const T* row, uint64_t c, uint64_t cols) {
+    if (NARROW) {
+      for (int i = 0; i < 8; ++i) v[i] = c + i < cols ? row[c + i] : (T)0.f;
+    } else {
+      v = *reinterpret_cast<GlobalPtr<vec>>((GlobalPtr<T>)(row + c));
+    }
+  }
+};
+
+template <bool NARROW>
+__device__ __forceinline__ void store_codes8(int8_t* p, uint64_t count, const uint32_t (&q)[8]) {
+  typedef uint32_t two __attribute__((ext_vector_type(2), aligned(1)));
+  two v;
+  v.x = pack4(q[0], q[1], q[2], q[3]);
+  v.y = pack4(q[4], q[5], q[6], q[7]);
+  if (!NARROW) {
     *reinterpret_cast<two*>(p) = v;
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-      if ((uint64_t)i < count) p[i] = (int8_t)q[i];
+      if ((uint64_t)i < count) p[i] = (int8_t)(v[i / 4] >> (i % 4 * 8));
   }
 }
 
-// A workgroup takes one row.  HELD: the row's values stay in registers, HELD times 2048 columns; 0: longer rows are read (and
-// drawn) again for the codes.
-template <typename T, bool DROP, int HELD>
-__global__ void __launch_bounds__(kBlock) quantize_rows_kernel(uint64_t rows, uint64_t cols, DropArgs d, View x, View q, float* scale) {
-  const uint64_t index = blockIdx.x;
-  const uint32_t m = (uint32_t)(index / rows);
+// What drop makes of columns c .. c + 7 of a row whose first element is number `first`.
+__device__ __forceinline__ void drop_values(float (&v)[8], uint64_t c, uint64_t cols, uint64_t first, uint32_t m, const DropArgs& d) {
+  uint32_t word[8];
+  if (d.threshold != 0u) {
+    draw_n<8>(first + c, (cols & 3u) == 0u, m, d, word);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) word[i] = 0u;
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = dropped(v[i], word[i], d);
+}
+
+// LANES take one row, and hold it: HELD times 8 columns each.  A wavefront needs no barrier, a workgroup has a long row sooner.
+template <typename T, bool DROP, int LANES, int HELD, bool NARROW>
+__global__ void __launch_bounds__(kBlock) quantize_rows_kernel(uint64_t all, uint64_t rows, uint64_t cols, DropArgs d, View x, View q,
+                                                               float* scale) {
+  const uint32_t lane = threadIdx.x % LANES;
+  const uint64_t index = (uint64_t)blockIdx.x * (kBlock / LANES) + __builtin_amdgcn_readfirstlane(threadIdx.x / LANES);
+  if (LANES == kWave && index >= all) return;  // (one row for a workgroup: none is left over)
+  const uint32_t m = (uint32_t)index / (uint32_t)rows;
   const uint64_t r = index - m * rows;
   const T* row = static_cast<const T*>(x.p) + m * x.pitch + r * x.ld;
   int8_t* out = static_cast<int8_t*>(q.p) + m * q.pitch + r * q.ld;
-  float v[HELD ? HELD : 1][8];
+  float v[HELD][8];
   uint32_t top = 0u;
-  if (HELD) {
 #pragma unroll
-    for (int k = 0; k < HELD; ++k) {
-      const uint64_t c = (uint64_t)(k * kBlock + threadIdx.x) * 8;
-      if (c < cols) {
-        coded_values<T, DROP>(row, c, cols, r * cols, m, d, v[k]);
+  for (int k = 0; k < HELD; ++k) load8<T, NARROW>(row, eight_at<NARROW>((k * LANES + lane) * 8, cols), cols, v[k]);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) top = max(top, magnitude_bits(v[k][i]));
-      }
-    }
-  } else {
-    for (uint64_t c = threadIdx.x * 8; c < cols; c += kBlock * 8) {
-      coded_values<T, DROP>(row, c, cols, r * cols, m, d, v[0]);
+  for (int k = 0; k < HELD; ++k) {
+    if (DROP) drop_values(v[k], eight_at<NARROW>((k * LANES + lane) * 8, cols), cols, r * cols, m, d);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) top = max(top, magnitude_bits(v[0][i]));
-    }
+    for (int i = 0; i < 8; ++i) top = max(top, magnitude_bits(v[k][i]));
+  }
+  top = wave_max_bits(top);
+  if (LANES > kWave) {
+    __shared__ uint32_t tops[kBlock / kWave];
+    if (threadIdx.x % kWave == 0) tops[threadIdx.x / kWave] = top;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kBlock / kWave; ++k) top = max(top, tops[k]);
+  }
+  const float inv = code_inverse(top);
+  if (lane == 0) scale[index] = code_step(top);
+#pragma unroll
+  for (int k = 0; k < HELD; ++k) {
+    const uint64_t c = (k * LANES + lane) * 8;
+    uint32_t code[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) code[i] = code_nearest(v[k][i], inv);
+    if (c < cols) store_codes8<NARROW>(out + eight_at<NARROW>(c, cols), cols - c, code);
+  }
+}
+
+// Longer rows, a workgroup each: read (and drawn) again for the codes.
+template <typename T, bool DROP>
+__global__ void __launch_bounds__(kBlock) quantize_long_rows_kernel(uint64_t rows, uint64_t cols, DropArgs d, View x, View q, float* scale) {
+  const uint64_t index = blockIdx.x;
+  const uint32_t m = (uint32_t)index / (uint32_t)rows;
+  const uint64_t r = index - m * rows;
+  const T* row = static_cast<const T*>(x.p) + m * x.pitch + r * x.ld;
+  int8_t* out = static_cast<int8_t*>(q.p) + m * q.pitch + r * q.ld;
+  float v[8];
+  uint32_t top = 0u;
+#pragma unroll 4
+  for (uint64_t c = threadIdx.x * 8; c < cols; c += kBlock * 8) {
+    const uint64_t at = eight_at<false>(c, cols);
+    load8<T, false>(row, at, cols, v);
+    if (DROP) drop_values(v, at, cols, r * cols, m, d);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = max(top, magnitude_bits(v[i]));
   }
   __shared__ uint32_t tops[kBlock / kWave];
   top = wave_max_bits(top);
@@ -160,38 +227,52 @@ __global__ void __launch_bounds__(kBlock) quantize_rows_kernel(uint64_t rows, ui
   for (int k = 0; k < kBlock / kWave; ++k) top = max(top, tops[k]);
   const float inv = code_inverse(top);
   if (threadIdx.x == 0) scale[index] = code_step(top);
-  int code[8];
-  if (HELD) {
+#pragma unroll 2
+  for (uint64_t c = threadIdx.x * 8; c < cols; c += kBlock * 8) {
+    const uint64_t at = eight_at<false>(c, cols);
+    uint32_t code[8];
+    load8<T, false>(row, at, cols, v);
+    if (DROP) drop_values(v, at, cols, r * cols, m, d);
 #pragma unroll
-    for (int k = 0; k < HELD; ++k) {
-      const uint64_t c = (uint64_t)(k * kBlock + threadIdx.x) * 8;
-      if (c < cols) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) code[i] = code_nearest(v[k][i], inv);
-        store_codes8(out + c, cols - c, code);
-      }
-    }
-  } else {
-    for (uint64_t c = threadIdx.x * 8; c < cols; c += kBlock * 8) {
-      coded_values<T, DROP>(row, c, cols, r * cols, m, d, v[0]);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) code[i] = code_nearest(v[0][i], inv);
-      store_codes8(out + c, cols - c, code);
-    }
+    for (int i = 0; i < 8; ++i) code[i] = code_nearest(v[i], inv);
+    store_codes8<false>(out + at, 8, code);
   }
 }
 
+// Few rows get a workgroup each, for their latency, many a wavefront each.  (Both, us: 1 row of 4096 bfloat16 2.5 / 4; 8192 rows of 2048 with
+// dropout 27 / 19.)
 template <typename T, bool DROP>
-void quantize_rows_held(const Extent& n, const DropArgs& d, const View& x, const View& q, float* scale, hipStream_t s) {
-  const dim3 grid((uint32_t)(n.workers * n.rows));
-  if (n.cols <= 2048)
-    quantize_rows_kernel<T, DROP, 1><<<grid, kBlock, 0, s>>>(n.rows, n.cols, d, x, q, scale);
+void quantize_rows_typed(const Extent& n, const DropArgs& d, const View& x, const View& q, float* scale, hipStream_t s) {
+  const uint64_t all = n.workers * n.rows;
+  auto launch = [&](auto lanes, auto held, auto narrow) {
+    constexpr int each = kBlock / lanes;
+    quantize_rows_kernel<T, DROP, lanes, held, narrow>
+        <<<dim3((uint32_t)((all + each - 1) / each)), kBlock, 0, s>>>(all, n.rows, n.cols, d, x, q, scale);
+  };
+  constexpr std::integral_constant<int, 1> one;
+  constexpr std::integral_constant<int, 2> two;
+  constexpr std::integral_constant<int, 4> four;
+  constexpr std::integral_constant<int, 8> eight;
+  constexpr std::integral_constant<int, kWave> wave;
+  constexpr std::integral_constant<int, kBlock> block;
+  if (n.cols < 8)
+    launch(wave, one, std::true_type{});
+  else if (n.cols <= 512)
+    launch(wave, one, std::false_type{});
+  else if (all >= 1024 && n.cols <= 1024)
+    launch(wave, two, std::false_type{});
+  else if (all >= 1024 && n.cols <= 2048)
+    launch(wave, four, std::false_type{});
+  else if (all >= 1024 && n.cols <= 4096)
+    launch(wave, eight, std::false_type{});
+  else if (n.cols <= 2048)
+    launch(block, one, std::false_type{});
   else if (n.cols <= 4096)
-    quantize_rows_kernel<T, DROP, 2><<<grid, kBlock, 0, s>>>(n.rows, n.cols, d, x, q, scale);
+    launch(block, two, std::false_type{});
   else if (n.cols <= 8192)
-    quantize_rows_kernel<T, DROP, 4><<<grid, kBlock, 0, s>>>(n.rows, n.cols, d, x, q, scale);
+    launch(block, four, std::false_type{});
   else
-    quantize_rows_kernel<T, DROP, 0><<<grid, kBlock, 0, s>>>(n.rows, n.cols, d, x, q, scale);
+    quantize_long_rows_kernel<T, DROP><<<dim3((uint32_t)all), kBlock, 0, s>>>(n.rows, n.cols, d, x, q, scale);
 }
 
 // ---- codes the other way round.  A tile is 128 x 128 codes; in LDS they lie as [column][row], 16-byte pieces of a column's 128
@@ -275,7 +356,7 @@ __global__ void __launch_bounds__(kBlock) turn_codes_kernel(uint64_t rows, uint6
 // dy[t][n] is coded twice: dy[t][n] col_scale[n] along n (one scale a row, for the product with the weights' codes) and
 // dy[t][n] row_scale[t] along t (one scale a column of a worker, for the product with the tokens' codes).  The first kernel takes
 // both kinds of maxima and the columns' sums in one pass, the second puts the pieces together, the third codes.
-constexpr int kStatRows = 128, kStatCols = kWave * 8;
+constexpr int kStatRows = 64, kStatCols = kWave * 8;
 
 struct GradScratch {
   float *row_inv, *col_inv;         // [workers][rows], [workers][cols]
@@ -283,49 +364,75 @@ struct GradScratch {
   float* sum_part;                  // [workers][row chunks][cols]
 };
 
-template <typename T>
-__global__ void __launch_bounds__(kBlock) grad_stats_kernel(uint64_t rows, uint64_t cols, View dy, const float* col_scale,
-                                                            const float* row_scale, GradScratch out) {
-  constexpr int kWaves = kBlock / kWave;
-  const uint32_t m = blockIdx.z, lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  const uint64_t c = (uint64_t)blockIdx.x * kStatCols + lane * 8, r0 = (uint64_t)blockIdx.y * kStatRows;
-  const uint64_t count = c < cols ? cols - c : 0;
+template <typename T, bool NARROW>
+__global__ void __launch_bounds__(kBlock) grad_stats_kernel(uint64_t rows, uint64_t cols, uint32_t tiles, uint32_t chunks, View dy,
+                                                            const float* col_scale, const float* row_scale, GradScratch out) {
+  constexpr int kWaves = kBlock / kWave, kMany = 2;  // rows at a time, and as many under way
+  const uint32_t m = blockIdx.y, lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const uint32_t chunk = blockIdx.x / tiles, tile = blockIdx.x - chunk * tiles;
+  const uint64_t c0 = (uint64_t)tile * kStatCols, c = eight_at<NARROW>(c0 + lane * 8, cols);
+  const uint64_t r0 = (uint64_t)chunk * kStatRows + wave * (kStatRows / kWaves);
+  const uint64_t end = min(rows, r0 + kStatRows / kWaves);
   float scale[8], sum[8];
   uint32_t top[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    scale[i] = (uint64_t)i < count && col_scale != nullptr ? col_scale[c + i] : 1.f;
+    scale[i] = 1.f;
     sum[i] = 0.f;
     top[i] = 0u;
   }
-  for (int k = wave; k < kStatRows; k += kWaves) {
-    const uint64_t r = r0 + k;
-    if (r >= rows) break;
-    float v[8];
+  if (col_scale != nullptr) load8<float, NARROW>(col_scale, c, cols, scale);
+  Raw8<T, NARROW> raw[kMany], coming[kMany];
+  float s[kMany], coming_s[kMany];
+  auto ask = [&](uint64_t r, Raw8<T, NARROW>(&x)[kMany], float (&f)[kMany]) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = 0.f;
-    if (count > 0) load_n_within<T, 8>(static_cast<const T*>(dy.p) + m * dy.pitch + r * dy.ld + c, count, 0.f, v);
-    const float s = row_scale != nullptr ? row_scale[m * rows + r] : 1.f;
-    uint32_t t = 0u;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      t = max(t, magnitude_bits(v[i] * scale[i]));
-      if ((uint64_t)i < count) top[i] = max(top[i], magnitude_bits(v[i] * s));
-      sum[i] += v[i];
+    for (int k = 0; k < kMany; ++k) {  // (past the end: the last row again, which is not counted)
+      const uint64_t row = min(r + k, rows - 1);
+      x[k].load(static_cast<const T*>(dy.p) + m * dy.pitch + row * dy.ld, c, cols);
+      f[k] = row_scale != nullptr ? row_scale[m * rows + row] : 1.f;
     }
-    t = wave_max_bits(t);
-    if (lane == 0) out.row_part[((uint64_t)m * gridDim.x + blockIdx.x) * rows + r] = t;
+  };
+  ask(r0, raw, s);
+#pragma unroll 1
+  for (uint64_t r = r0; r < end; r += kMany) {
+    ask(r + kMany, coming, coming_s);
+    uint32_t t[kMany];
+#pragma unroll
+    for (int k = 0; k < kMany; ++k) {
+      const bool in = r + k < end;
+      t[k] = 0u;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float v = (float)raw[k].v[i];
+        t[k] = max(t[k], magnitude_bits(v * scale[i]));
+        top[i] = max(top[i], magnitude_bits(v * s[k]));
+        sum[i] += in ? v : 0.f;
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kMany; ++k) {
+      t[k] = wave_max_bits(t[k]);
+      if (lane == 0 && r + k < end) out.row_part[((uint64_t)m * tiles + tile) * rows + r + k] = t[k];
+    }
+#pragma unroll
+    for (int k = 0; k < kMany; ++k) {
+      raw[k] = coming[k];
+      s[k] = coming_s[k];
+    }
   }
   __shared__ uint32_t tops[kWaves][kStatCols];
   __shared__ float sums[kWaves][kStatCols];
+  const int at = NARROW ? (int)lane * 8 : (int)((int64_t)c - (int64_t)c0);  // (before the tile, in a last tile of less than eight columns)
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    tops[wave][lane * 8 + i] = top[i];
-    sums[wave][lane * 8 + i] = sum[i];
+    if (at + i >= 0) {
+      tops[wave][at + i] = top[i];
+      sums[wave][at + i] = sum[i];
+    }
   }
   __syncthreads();
   for (uint32_t j = threadIdx.x; j < kStatCols; j += kBlock) {
-    const uint64_t n = (uint64_t)blockIdx.x * kStatCols + j;
+    const uint64_t n = (uint64_t)tile * kStatCols + j;
     if (n >= cols) break;
     uint32_t t = 0u;
     float a = 0.f;
@@ -334,7 +441,7 @@ __global__ void __launch_bounds__(kBlock) grad_stats_kernel(uint64_t rows, uint6
       t = max(t, tops[w][j]);
       a += sums[w][j];
     }
-    const uint64_t at = ((uint64_t)m * gridDim.y + blockIdx.y) * cols + n;
+    const uint64_t at = ((uint64_t)m * chunks + chunk) * cols + n;
     out.col_part[at] = t;
     out.sum_part[at] = a;
   }
@@ -350,12 +457,14 @@ __global__ void __launch_bounds__(kBlock) grad_finish_kernel(uint64_t rows, uint
   uint32_t top = 0u;
   if (by_rows) {
     if (j >= rows) return;
+#pragma unroll 8
     for (uint32_t k = 0; k < tiles; ++k) top = max(top, in.row_part[((uint64_t)m * tiles + k) * rows + j]);
     in.row_inv[m * rows + j] = code_inverse(top);
     q_scale[m * rows + j] = code_step(top);
   } else {
     if (j >= cols) return;
     float sum = 0.f;
+#pragma unroll 8
     for (uint32_t k = 0; k < chunks; ++k) {
       const uint64_t at = ((uint64_t)m * chunks + k) * cols + j;
       top = max(top, in.col_part[at]);
@@ -367,43 +476,48 @@ __global__ void __launch_bounds__(kBlock) grad_finish_kernel(uint64_t rows, uint
   }
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kBlock) grad_codes_kernel(uint64_t rows, uint64_t cols, DropArgs key, View dy, const float* col_scale,
+template <typename T, bool NARROW>
+__global__ void __launch_bounds__(kBlock, 4) grad_codes_kernel(uint64_t rows, uint64_t cols, DropArgs key, View dy, const float* col_scale,
                                                             const float* row_scale, GradScratch in, View q, View qt) {
   __shared__ __align__(16) uint32_t words[kTile * kTile / 4];
   const uint32_t m = blockIdx.z, chunk = threadIdx.x % 16, group = threadIdx.x / 16;
-  const uint64_t r0 = (uint64_t)blockIdx.y * kTile, c0 = (uint64_t)blockIdx.x * kTile, c = c0 + chunk * 8;
-  const uint64_t count = c < cols ? cols - c : 0;
+  const uint64_t r0 = (uint64_t)blockIdx.y * kTile, c0 = (uint64_t)blockIdx.x * kTile, c = eight_at<NARROW>(c0 + chunk * 8, cols);
+  const bool some = c0 + chunk * 8 < cols;
+  const int at = NARROW ? (int)chunk * 8 : (int)((int64_t)c - (int64_t)c0);  // (before the tile, in a last tile of less than eight columns)
   float scale[8], inv[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const bool in_row = (uint64_t)i < count;
-    scale[i] = in_row && col_scale != nullptr ? col_scale[c + i] : 1.f;
-    inv[i] = in_row ? in.col_inv[m * cols + c + i] : 0.f;
-  }
+  for (int i = 0; i < 8; ++i) scale[i] = 1.f;
+  if (col_scale != nullptr) load8<float, NARROW>(col_scale, c, cols, scale);
+  load8<float, NARROW>(in.col_inv + m * cols, c, cols, inv);
 #pragma unroll 1
   for (uint32_t half = 0; half < 2; ++half) {
     const uint32_t g = group + half * 16;
-    uint32_t turned[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
+    const uint64_t r = r0 + g * 4;
+    Raw8<T, NARROW> raw[4];
+    float row_inv[4], s[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {  // (past the end: the last row again, whose codes go nowhere)
+      const uint64_t row = min(r + k, rows - 1);
+      raw[k].load(static_cast<const T*>(dy.p) + m * dy.pitch + row * dy.ld, c, cols);
+      row_inv[k] = in.row_inv[m * rows + row];
+      s[k] = row_scale != nullptr ? row_scale[m * rows + row] : 1.f;
+    }
+    uint32_t down[4][8];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      const uint64_t r = r0 + g * 4 + k;
-      if (r >= rows || count == 0) continue;
-      float v[8];
-      load_n_within<T, 8>(static_cast<const T*>(dy.p) + m * dy.pitch + r * dy.ld + c, count, 0.f, v);
-      const float row_inv = in.row_inv[m * rows + r], s = row_scale != nullptr ? row_scale[m * rows + r] : 1.f;
-      uint32_t word[8];
-      draw_n<8>(r * cols + c, (cols & 3u) == 0u, m, key, word);
-      int code[8];
+      uint32_t word[8], code[8];
+      draw_n<8>((r + k) * cols + c, (cols & 3u) == 0u, m, key, word);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        code[i] = code_drawn(v[i] * scale[i], row_inv, word[i] >> 16);
-        turned[i] |= (uint32_t)(code_drawn(v[i] * s, inv[i], word[i] & 0xFFFFu) & 255) << (8 * k);
+        const float v = (float)raw[k].v[i];
+        code[i] = code_drawn(v * scale[i], row_inv[k], word[i] >> 16);
+        down[k][i] = code_drawn(v * s[k], inv[i], word[i] & 0xFFFFu);
       }
-      store_codes8(static_cast<int8_t*>(q.p) + m * q.pitch + r * q.ld + c, count, code);
+      if (some && r + k < rows) store_codes8<NARROW>(static_cast<int8_t*>(q.p) + m * q.pitch + (r + k) * q.ld + c, cols - c, code);
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) words[turned_at(chunk * 8 + i, g)] = turned[i];
+    for (int i = 0; i < 8; ++i)
+      if (at + i >= 0 && some) words[turned_at(at + i, g)] = pack4(down[0][i], down[1][i], down[2][i], down[3][i]);
   }
   __syncthreads();
   store_turned(words, qt, m, r0, c0, rows, cols);
@@ -424,21 +538,21 @@ GradScratch grad_scratch(const Extent& n, float* p) {
   return g;
 }
 
-template <typename T>
+template <typename T, bool NARROW>
 hipError_t quantize_grad_typed(const Extent& n, const DropArgs& key, const View& dy, const float* col_scale, const float* row_scale,
                                const View& q, float* q_scale, const View& qt, float* qt_scale, float* col_sum, float* scratch,
                                hipStream_t s) {
   const GradScratch g = grad_scratch(n, scratch);
   const uint32_t tiles = (uint32_t)((n.cols + kStatCols - 1) / kStatCols), chunks = (uint32_t)((n.rows + kStatRows - 1) / kStatRows);
   const bool none = n.rows == 0 || n.cols == 0;  // (scales and sums are 0 then)
-  if (!none) grad_stats_kernel<T><<<dim3(tiles, chunks, n.workers), kBlock, 0, s>>>(n.rows, n.cols, dy, col_scale, row_scale, g);
+  if (!none) grad_stats_kernel<T, NARROW><<<dim3(tiles * chunks, n.workers), kBlock, 0, s>>>(n.rows, n.cols, tiles, chunks, dy, col_scale, row_scale, g);
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   const uint32_t row_blocks = (uint32_t)((n.rows + kBlock - 1) / kBlock), col_blocks = (uint32_t)((n.cols + kBlock - 1) / kBlock);
   grad_finish_kernel<<<dim3(row_blocks + col_blocks, n.workers), kBlock, 0, s>>>(n.rows, n.cols, tiles, chunks, row_blocks, g, q_scale,
                                                                                  qt_scale, col_sum);
   if (hipError_t e = hipGetLastError(); e != hipSuccess || none) return e;
   const dim3 grid((uint32_t)((n.cols + kTile - 1) / kTile), (uint32_t)((n.rows + kTile - 1) / kTile), n.workers);
-  grad_codes_kernel<T><<<grid, kBlock, 0, s>>>(n.rows, n.cols, key, dy, col_scale, row_scale, g, q, qt);
+  grad_codes_kernel<T, NARROW><<<grid, kBlock, 0, s>>>(n.rows, n.cols, key, dy, col_scale, row_scale, g, q, qt);
   return hipGetLastError();
 }
 
@@ -459,13 +573,13 @@ hipError_t launch_quantize_rows(tng_type type, const Extent& n, const DropArgs* 
   const DropArgs d = drop != nullptr ? *drop : DropArgs{};
   switch (type) {
     case TNG_TYPE_F32:
-      drop ? quantize_rows_held<float, true>(n, d, x, q, scale, s) : quantize_rows_held<float, false>(n, d, x, q, scale, s);
+      drop ? quantize_rows_typed<float, true>(n, d, x, q, scale, s) : quantize_rows_typed<float, false>(n, d, x, q, scale, s);
       break;
     case TNG_TYPE_BF16:
-      drop ? quantize_rows_held<bf16_t, true>(n, d, x, q, scale, s) : quantize_rows_held<bf16_t, false>(n, d, x, q, scale, s);
+      drop ? quantize_rows_typed<bf16_t, true>(n, d, x, q, scale, s) : quantize_rows_typed<bf16_t, false>(n, d, x, q, scale, s);
       break;
     default:
-      drop ? quantize_rows_held<f16_t, true>(n, d, x, q, scale, s) : quantize_rows_held<f16_t, false>(n, d, x, q, scale, s);
+      drop ? quantize_rows_typed<f16_t, true>(n, d, x, q, scale, s) : quantize_rows_typed<f16_t, false>(n, d, x, q, scale, s);
   }
   if (hipError_t e = hipGetLastError(); e != hipSuccess || qt.p == nullptr) return e;
   const dim3 grid((uint32_t)((n.cols + kTile - 1) / kTile), (uint32_t)((n.rows + kTile - 1) / kTile), n.workers);
@@ -481,14 +595,17 @@ size_t quantize_grad_floats(const Extent& n) {
 hipError_t launch_quantize_grad(tng_type type, const Extent& n, const DropArgs& key, const View& dy, const float* col_scale,
                                 const float* row_scale, const View& q, float* q_scale, const View& qt, float* qt_scale, float* col_sum,
                                 float* scratch, hipStream_t s) {
-  switch (type) {
-    case TNG_TYPE_F32:
-      return quantize_grad_typed<float>(n, key, dy, col_scale, row_scale, q, q_scale, qt, qt_scale, col_sum, scratch, s);
-    case TNG_TYPE_BF16:
-      return quantize_grad_typed<bf16_t>(n, key, dy, col_scale, row_scale, q, q_scale, qt, qt_scale, col_sum, scratch, s);
-    default:
-      return quantize_grad_typed<f16_t>(n, key, dy, col_scale, row_scale, q, q_scale, qt, qt_scale, col_sum, scratch, s);
-  }
+  auto launch = [&](auto narrow) {
+    switch (type) {
+      case TNG_TYPE_F32:
+        return quantize_grad_typed<float, narrow>(n, key, dy, col_scale, row_scale, q, q_scale, qt, qt_scale, col_sum, scratch, s);
+      case TNG_TYPE_BF16:
+        return quantize_grad_typed<bf16_t, narrow>(n, key, dy, col_scale, row_scale, q, q_scale, qt, qt_scale, col_sum, scratch, s);
+      default:
+        return quantize_grad_typed<f16_t, narrow>(n, key, dy, col_scale, row_scale, q, q_scale, qt, qt_scale, col_sum, scratch, s);
+    }
+  };
+  return n.cols < 8 ? launch(std::true_type{}) : launch(std::false_type{});
 }
 
 }  // namespace tng

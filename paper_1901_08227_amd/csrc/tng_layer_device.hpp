@@ -110,11 +110,18 @@ __device__ __forceinline__ float code_step(uint32_t r) {
 __device__ __forceinline__ float code_place(float v, float inv) {
   return __builtin_amdgcn_fmed3f(v * inv, -1.0f, 1.0f) * 127.0f;
 }
-__device__ __forceinline__ int code_nearest(float v, float inv) { return (int)rintf(code_place(v, inv)); }
-// Up with the probability of the fractional part, to 2^-16 of a step (of a code: the mean is within 2^-16 of a step of v).
-__device__ __forceinline__ int code_drawn(float v, float inv, uint32_t half) {
-  const float x = code_place(v, inv), low = floorf(x);
-  return (int)low + ((float)half * 0x1p-16f < x - low ? 1 : 0);
+// Its code is the lowest byte.  (1.5 2^23 leaves no place for a fraction: the sum is rounded to the nearest integer, halves to even.)
+__device__ __forceinline__ uint32_t code_nearest(float v, float inv) { return __float_as_uint(code_place(v, inv) + 0x1.8p23f); }
+// Up with the probability of the fractional part, to 2^-16 of a step (of a code: the mean is within 2^-16 of a step of v).  The code is the
+// lowest byte.  (v_fract gives x - floor(x), but no more than 1 - 2^-24; no draw lies between that and 1.)
+__device__ __forceinline__ uint32_t code_drawn(float v, float inv, uint32_t half) {
+  const float x = code_place(v, inv);
+  return (uint32_t)((int)floorf(x) + ((float)half * 0x1p-16f < __builtin_amdgcn_fractf(x) ? 1 : 0));
+}
+
+// The lowest bytes of four words as one.
+__device__ __forceinline__ uint32_t pack4(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0C0C0400u), __builtin_amdgcn_perm(b, a, 0x0C0C0400u), 0x05040100u);
 }
 
 }  // namespace tng

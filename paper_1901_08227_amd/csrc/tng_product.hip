@@ -32,13 +32,21 @@ struct Task {
 // y of one element from its sum, before the rounding to y's type.
 __device__ __forceinline__ float scaled(float sum, float a_scale, float b_scale, float bias) { return sum * a_scale * b_scale + bias; }
 
+// The worker that row t of the product belongs to, and its row there.
+__device__ __forceinline__ uint32_t worker_of(const Task& p, uint32_t m, uint32_t* t) {
+  if (p.rows == p.rows_of_worker) return m;
+  const uint32_t w = *t / p.rows_of_worker;  // (m is 0: the rows of all workers)
+  *t -= w * p.rows_of_worker;
+  return w;
+}
+
 // keep f'(x) / (1 - p) of element (t, n).
 template <typename T>
 __device__ __forceinline__ float tail(float y, const Task& p, uint32_t m, uint64_t t, uint64_t n) {
   if (!p.drops) return y;
-  const uint32_t w = p.rows == p.rows_of_worker ? m : (uint32_t)t / p.rows_of_worker;  // (its rows may lie among all workers')
-  t -= (uint64_t)(w - m) * p.rows_of_worker;
-  const uint64_t e = t * p.channels + n;
+  uint32_t row = (uint32_t)t;
+  const uint32_t w = worker_of(p, m, &row);
+  const uint64_t e = (uint64_t)row * p.channels + n;
   uint32_t word = 0u;
   if (p.drop.threshold != 0u) {
     const U32x4 v = philox4x32_10((uint32_t)(e >> 2), w, p.drop.iter, p.drop.word, p.drop.k0, p.drop.k1);
@@ -46,20 +54,14 @@ __device__ __forceinline__ float tail(float y, const Task& p, uint32_t m, uint64
     word = k == 0 ? v.x : k == 1 ? v.y : k == 2 ? v.z : v.w;
   }
   bool pass = kept(word, p.drop);
-  if (p.drop.relu) pass = pass && !((float)static_cast<const T*>(p.x.p)[w * p.x.pitch + t * p.x.ld + n] <= 0.f);
+  if (p.drop.relu) pass = pass && !((float)static_cast<const T*>(p.x.p)[w * p.x.pitch + (uint64_t)row * p.x.ld + n] <= 0.f);
   return pass ? y * p.drop.scale : 0.f;
 }
 
-// The same of N consecutive channels, `left` of which exist.
-template <typename T, int N>
-__device__ __forceinline__ void tail_n(float (&y)[N], const Task& p, uint32_t m, uint64_t t, uint64_t n, uint64_t left) {
-  const uint32_t w = p.rows == p.rows_of_worker ? m : (uint32_t)t / p.rows_of_worker;
-  t -= (uint64_t)(w - m) * p.rows_of_worker;
+// The same of N consecutive channels from n on; x: what relu was taken of, t: the row among worker w's.
+template <int N>
+__device__ __forceinline__ void tail_n(float (&y)[N], const float (&x)[N], const Task& p, uint32_t w, uint64_t t, uint64_t n) {
   const uint64_t e = t * p.channels + n;
-  float x[N];
-#pragma unroll
-  for (int i = 0; i < N; ++i) x[i] = 1.f;
-  if (p.drop.relu) load_n_within<T, N>(static_cast<const T*>(p.x.p) + w * p.x.pitch + t * p.x.ld + n, left, 1.f, x);
 #pragma unroll
   for (int b = 0; b < N; b += 4) {  // (a block at a time: the sums leave few registers)
     uint32_t word[4] = {0u, 0u, 0u, 0u};
@@ -68,6 +70,13 @@ __device__ __forceinline__ void tail_n(float (&y)[N], const Task& p, uint32_t m,
     for (int i = 0; i < 4; ++i) y[b + i] = kept(word[i], p.drop) && !(x[b + i] <= 0.f) ? y[b + i] * p.drop.scale : 0.f;
     __builtin_amdgcn_sched_barrier(0);
   }
+}
+
+template <typename T, int N>
+__device__ __forceinline__ void load_gate(float (&x)[N], const Task& p, uint32_t w, uint64_t t, uint64_t n, uint64_t left) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] = 1.f;
+  if (p.drop.relu) load_n_within<T, N>(static_cast<const T*>(p.x.p) + w * p.x.pitch + t * p.x.ld + n, left, 1.f, x);
 }
 
 template <typename T>
@@ -291,6 +300,21 @@ __device__ __forceinline__ void write_tile(const Task& p, const Spot& s, const v
   constexpr int kRun = K::kRun;
   const uint32_t n_in = cw * CN * 16 + K::channel_row(0, lane / 16 * 4), t_in = tw * TN * 16 + lane % 16;
   const bool full = s.channels == K::kChannels && s.tokens == K::kTokens;
+  // With a tail: each row's worker and its number there, and what relu was taken of, a run of channels ahead of its use.
+  typedef T run_t __attribute__((ext_vector_type(kRun), aligned(alignof(T))));
+  uint32_t w[TN], row[TN];
+  run_t ahead[TN];
+  auto fetch = [&](int b, uint32_t n) {
+    ahead[b] = *reinterpret_cast<const run_t*>(static_cast<const T*>(p.x.p) + w[b] * p.x.pitch + row[b] * p.x.ld + s.n0 + n);
+  };
+  if (END == kTail) {
+#pragma unroll
+    for (int b = 0; b < TN; ++b) {
+      row[b] = (uint32_t)s.t0 + t_in + b * 16;
+      w[b] = worker_of(p, s.m, &row[b]);
+      if (full && p.drop.relu) fetch(b, n_in);
+    }
+  }
   float sa[TN];
 #pragma unroll
   for (int b = 0; b < TN; ++b) sa[b] = p.a_scale != nullptr ? factors[2 * K::kChannels + t_in + b * 16] : 1.f;
@@ -315,18 +339,26 @@ __device__ __forceinline__ void write_tile(const Task& p, const Spot& s, const v
         sb[r] = p.b_scale != nullptr ? factors[n + r] : 1.f;
         bias[r] = factors[K::kChannels + n + r];
       }
-#pragma unroll
-      for (int b = 0; b < TN; ++b) {
-        uint32_t t = t_in + b * 16;
-        // (what follows from t is not worth registers from one run of channels to the next: there are none left)
-        if (END == kTail) asm("" : "+v"(t));
-        if (!full && t >= s.tokens) continue;
+      each_of<TN, 1>([&](auto of) {
+        constexpr int b = of;
+        const uint32_t t = t_in + b * 16;
+        if (!full && t >= s.tokens) return;
         float y[kRun];
 #pragma unroll
         for (int r = 0; r < kRun; ++r) y[r] = scaled((float)sum[a + r / 4][b][r % 4], sa[b], sb[r], bias[r]);
-        if (END == kTail) tail_n<T, kRun>(y, p, s.m, s.t0 + t, s.n0 + n, left);
+        if (END == kTail) {
+          float x[kRun];
+          if (full) {
+#pragma unroll
+            for (int r = 0; r < kRun; ++r) x[r] = p.drop.relu ? (float)ahead[b][r] : 1.f;
+            if (p.drop.relu && a + K::kTilesOfRun < CN) fetch(b, n_in + K::channel_row(a + K::kTilesOfRun, 0));
+          } else {
+            load_gate<T, kRun>(x, p, w[b], row[b], s.n0 + n, left);
+          }
+          tail_n<kRun>(y, x, p, w[b], row[b], s.n0 + n);
+        }
         store_n_within<T, kRun>(static_cast<T*>(p.y.p) + s.m * p.y.pitch + (s.t0 + t) * p.y.ld + s.n0 + n, left, y);
-      }
+      });
     }
   });
 }
@@ -593,7 +625,13 @@ __global__ void __launch_bounds__(kBlock) product_join_kernel(Task p) {
   if (p.bias != nullptr) load_n_within<float, 4>(p.bias + n, left, 0.f, bias);
 #pragma unroll
   for (int r = 0; r < 4; ++r) y[r] = scaled((float)sum[r], sa, sb[r], bias[r]);
-  if (p.drops) tail_n<T, 4>(y, p, m, t, n, left);
+  if (p.drops) {
+    float x[4];
+    uint32_t row = (uint32_t)t;
+    const uint32_t w = worker_of(p, m, &row);
+    load_gate<T, 4>(x, p, w, row, n, left);
+    tail_n<4>(y, x, p, w, row, n);
+  }
   store_n_within<T, 4>(static_cast<T*>(p.y.p) + m * p.y.pitch + t * p.y.ld + n, left, y);
 }
 
