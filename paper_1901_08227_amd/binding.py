@@ -61,7 +61,7 @@ class TngError(RuntimeError):
 
 _lib = None
 _call = None      # the extension's call() or _through_ctypes; set with the library
-_layer = None     # its layer() or _through_ctypes
+_layer = _linear = _linear_grad = None  # its layer(), linear() and linear_grad() or _through_ctypes
 _address = None   # {entry point: its address} of those that go through it
 
 
@@ -85,7 +85,7 @@ def _load_call(name="call"):
 
 def lib() -> ctypes.CDLL:
     """The loaded library; raises if it has not been built (python -m paper_1901_08227_amd.build)."""
-    global _lib, _call, _layer, _address
+    global _lib, _call, _layer, _linear, _linear_grad, _address
     if _lib is None:
         if not os.path.exists(LIB_PATH):
             raise RuntimeError(f"libtng is not built: {LIB_PATH} is missing; run __graft_entry__.build()")
@@ -134,7 +134,7 @@ def lib() -> ctypes.CDLL:
         for name, argtypes in sigs.items():
             fn = getattr(L, name)
             fn.restype, fn.argtypes = ctypes.c_int, argtypes
-        _call, _layer = _load_call(), _load_call("layer")
+        _call, _layer, _linear, _linear_grad = (_load_call(name) for name in ("call", "layer", "linear", "linear_grad"))
         _address = {name: ctypes.cast(getattr(L, name), vp).value
                     for name in ("tng_local_grad", "tng_normalize_encode", "tng_decode_aggregate", "tng_update_reference",
                                  "tng_step", "tng_dropout", "tng_dropout_grad", "tng_quantize_rows", "tng_quantize_grad",

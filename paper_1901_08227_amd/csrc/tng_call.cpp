@@ -14,10 +14,19 @@
 // the same for the calls on layers: kinds has a letter per argument, m a matrix of numbers ([rows, cols] or [M, rows, cols]), i one of codes,
 // d the five fields of tng_drop in a tuple, and float32 vectors by the last matrix before them: r workers * rows, n rows, c cols long.  A w
 // (W) at the end takes no argument: scratch, as large as is said of the first matrix (of the first two and the last), from torch.
+//
+//   linear(addresses, stream, x, drop, codes, scales, bias, keep) -> y, or (y, scales, turned codes) with keep
+//   linear_grad(addresses, stream, dy, scales, turned codes, weights' scales, weights' turned codes, drop, x, (seed, iter, site), out)
+//     -> (dx, dw, db)
+//
+// whole layers, what they put in between from torch: None as above, or the status of a call that refused.  addresses: a tuple.
 #include <Python.h>
+
+#include <algorithm>
 
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
+#include <c10/util/SmallVector.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "../../include/tng.h"
@@ -227,9 +236,174 @@ PyObject* layer(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   return PyLong_FromLong(status);
 }
 
+// ---- whole layers
+
+using QuantizeRows = int (*)(uintptr_t, const tng_drop*, const tng_matrix*, const tng_matrix*, float*, const tng_matrix*);
+using QuantizeGrad = int (*)(uintptr_t, const tng_drop*, const tng_matrix*, const float*, const float*, const tng_matrix*, float*,
+                             const tng_matrix*, float*, float*, void*, size_t);
+using GradBytes = size_t (*)(const tng_matrix*);
+using Product = int (*)(uintptr_t, const tng_matrix*, const float*, const tng_matrix*, const float*, const float*, const tng_drop*,
+                        const tng_matrix*, const tng_matrix*, void*, size_t);
+using ProductBytes = size_t (*)(const tng_matrix*, const tng_matrix*, const tng_matrix*);
+
+struct Entries {
+  QuantizeRows quantize_rows;
+  QuantizeGrad quantize_grad;
+  GradBytes grad_bytes;
+  Product product;
+  ProductBytes product_bytes;
+};
+
+bool entries_of(PyObject* obj, Entries* e) {
+  if (!PyTuple_Check(obj) || PyTuple_GET_SIZE(obj) != 5) return false;
+  uintptr_t a[5];
+  for (int i = 0; i < 5; ++i) a[i] = (uintptr_t)PyLong_AsUnsignedLongLong(PyTuple_GET_ITEM(obj, i));
+  e->quantize_rows = reinterpret_cast<QuantizeRows>(a[0]);
+  e->quantize_grad = reinterpret_cast<QuantizeGrad>(a[1]);
+  e->grad_bytes = reinterpret_cast<GradBytes>(a[2]);
+  e->product = reinterpret_cast<Product>(a[3]);
+  e->product_bytes = reinterpret_cast<ProductBytes>(a[4]);
+  return !PyErr_Occurred();
+}
+
+using Shape = c10::SmallVector<int64_t, 4>;
+
+// [M, rows, cols], without the M where x had none.
+Shape shape_like(const at::Tensor& x, int64_t rows, int64_t cols) {
+  Shape s;
+  if (x.dim() == 3) s.push_back(x.size(0));
+  s.push_back(rows);
+  s.push_back(cols);
+  return s;
+}
+
+// Codes whose rows begin 16 bytes apart, and their matrix.
+at::Tensor codes(const at::Tensor& x, int64_t rows, int64_t cols, tng_matrix* m) {
+  const int64_t ld = (cols + 15) / 16 * 16;
+  const at::Tensor t = at::empty(shape_like(x, rows, ld), x.options().dtype(at::kChar));
+  *m = tng_matrix{t.data_ptr(), TNG_TYPE_I8, x.dim() == 3 ? (uint32_t)x.size(0) : 1u, (uint64_t)rows, (uint64_t)cols, (uint64_t)ld,
+                  (uint64_t)(rows * ld)};
+  return ld == cols ? t : t.narrow(-1, 0, cols);
+}
+
+// A matrix of numbers of x's type (or float32), and its tng_matrix.
+at::Tensor numbers(const at::Tensor& x, int64_t rows, int64_t cols, at::ScalarType type, tng_matrix* m) {
+  const at::Tensor t = at::empty(shape_like(x, rows, cols), x.options().dtype(type));
+  *m = tng_matrix{t.data_ptr(), type == at::kFloat ? TNG_TYPE_F32 : type == at::kHalf ? TNG_TYPE_F16 : TNG_TYPE_BF16,
+                  x.dim() == 3 ? (uint32_t)x.size(0) : 1u, (uint64_t)rows, (uint64_t)cols, (uint64_t)cols, (uint64_t)(rows * cols)};
+  return t;
+}
+
+// A float32 vector: a row of each worker's.
+at::Tensor floats(const at::Tensor& x, int64_t n) {
+  Shape s;
+  if (x.dim() == 3) s.push_back(x.size(0));
+  s.push_back(n);
+  return at::empty(s, x.options().dtype(at::kFloat));
+}
+
+at::Tensor bytes_of(const at::Tensor& x, size_t n) { return at::empty({(int64_t)n}, x.options().dtype(at::kByte)); }
+
+PyObject* linear(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  Entries e;
+  if (nargs != 8 || !entries_of(args[0], &e)) {
+    if (!PyErr_Occurred()) PyErr_SetString(PyExc_TypeError, "linear: addresses, stream, x, drop, codes, scales, bias, keep");
+    return nullptr;
+  }
+  const uintptr_t stream = (uintptr_t)PyLong_AsUnsignedLongLong(args[1]);
+  const bool keep = args[7] == Py_True;
+  if (PyErr_Occurred()) return nullptr;
+  try {
+    LayerCall c;
+    uintptr_t mx, mw, drop = 0, scales, bias = 0;
+    if (!c.as_matrix(args[2], false, &mx) || (args[3] != Py_None && !c.as_drop(args[3], &drop)) || !c.as_matrix(args[4], true, &mw) ||
+        !c.as_vector(args[5], 'r', &scales) || (args[6] != Py_None && !c.as_vector(args[6], 'n', &bias)))
+      Py_RETURN_NONE;
+    const tng_matrix x = c.matrix[0], w = c.matrix[1];
+    if (w.cols != x.cols || w.workers != 1) Py_RETURN_NONE;
+    const at::Tensor& tx = THPVariable_Unpack(args[2]);
+    tng_matrix q, qt{}, y;
+    const at::Tensor tq = codes(tx, x.rows, x.cols, &q), ts = floats(tx, x.rows), ty = numbers(tx, x.rows, w.rows, tx.scalar_type(), &y);
+    at::Tensor tqt;
+    if (keep) tqt = codes(tx, x.cols, x.rows, &qt);
+    const size_t bytes = e.product_bytes(&q, &w, &y);
+    if (bytes == 0) Py_RETURN_NONE;
+    const at::Tensor scratch = bytes_of(tx, bytes);
+    int status;
+    Py_BEGIN_ALLOW_THREADS
+    status = e.quantize_rows(stream, reinterpret_cast<const tng_drop*>(drop), &x, &q, ts.data_ptr<float>(), keep ? &qt : nullptr);
+    if (status == 0)
+      status = e.product(stream, &q, ts.data_ptr<float>(), &w, reinterpret_cast<const float*>(scales), reinterpret_cast<const float*>(bias),
+                         nullptr, nullptr, &y, scratch.data_ptr(), bytes);
+    Py_END_ALLOW_THREADS
+    if (status != 0) return PyLong_FromLong(status);
+    if (!keep) return THPVariable_Wrap(ty);
+    return Py_BuildValue("(NNN)", THPVariable_Wrap(ty), THPVariable_Wrap(ts), THPVariable_Wrap(tqt));
+  } catch (const std::exception&) {
+    Py_RETURN_NONE;
+  }
+}
+
+PyObject* linear_grad(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  Entries e;
+  if (nargs != 11 || !entries_of(args[0], &e)) {
+    if (!PyErr_Occurred()) PyErr_SetString(PyExc_TypeError, "linear_grad: addresses, stream, dy, scales, turned codes, those of the weights, drop, x, key, out");
+    return nullptr;
+  }
+  const uintptr_t stream = (uintptr_t)PyLong_AsUnsignedLongLong(args[1]);
+  if (PyErr_Occurred()) return nullptr;
+  try {
+    LayerCall c, k;
+    uintptr_t at, row_scale, col_scale, drop = 0, gate = 0, key;
+    // in the order in which a vector's length goes by the matrix before it
+    if (!c.as_matrix(args[2], false, &at) || !c.as_vector(args[3], 'r', &row_scale) || !c.as_vector(args[5], 'c', &col_scale) ||
+        !c.as_matrix(args[4], true, &at) || !c.as_matrix(args[6], true, &at) || (args[7] != Py_None && !c.as_drop(args[7], &drop)) ||
+        (args[8] != Py_None && !c.as_matrix(args[8], false, &gate)) || !k.as_drop(args[9], &key))
+      Py_RETURN_NONE;
+    const tng_matrix dy = c.matrix[0], xt = c.matrix[1], wt = c.matrix[2];
+    if (xt.cols != dy.rows || xt.workers != dy.workers || wt.cols != dy.cols || wt.rows != xt.rows || wt.workers != 1) Py_RETURN_NONE;
+    const at::Tensor& ty = THPVariable_Unpack(args[2]);
+    tng_matrix q, qt, dx, dw;
+    at::Tensor tdw;
+    if (args[10] == Py_None) {
+      tdw = numbers(ty, dy.cols, xt.rows, at::kFloat, &dw);
+    } else {
+      if (!c.as_matrix(args[10], false, &at)) Py_RETURN_NONE;
+      dw = *reinterpret_cast<const tng_matrix*>(at);
+      tdw = THPVariable_Unpack(args[10]);
+      if (dw.type != TNG_TYPE_F32 || dw.rows != dy.cols || dw.cols != xt.rows || tdw.dim() != ty.dim()) Py_RETURN_NONE;
+    }
+    const at::Tensor tq = codes(ty, dy.rows, dy.cols, &q), tqt = codes(ty, dy.cols, dy.rows, &qt);
+    const at::Tensor tqs = floats(ty, dy.rows), tqts = floats(ty, dy.cols), tdb = floats(ty, dy.cols);
+    const at::Tensor tdx = numbers(ty, dy.rows, xt.rows, ty.scalar_type(), &dx);
+    // one scratch for the three calls, which follow each other on the stream
+    const size_t first = e.grad_bytes(&dy), second = e.product_bytes(&q, &wt, &dx), third = e.product_bytes(&qt, &xt, &dw);
+    if (first == 0 || second == 0 || third == 0) Py_RETURN_NONE;
+    const size_t bytes = std::max(first, std::max(second, third));
+    const at::Tensor scratch = bytes_of(ty, bytes);
+    int status;
+    Py_BEGIN_ALLOW_THREADS
+    status = e.quantize_grad(stream, reinterpret_cast<const tng_drop*>(key), &dy, reinterpret_cast<const float*>(col_scale),
+                             reinterpret_cast<const float*>(row_scale), &q, tqs.data_ptr<float>(), &qt, tqts.data_ptr<float>(),
+                             tdb.data_ptr<float>(), scratch.data_ptr(), bytes);
+    if (status == 0)
+      status = e.product(stream, &q, tqs.data_ptr<float>(), &wt, nullptr, nullptr, reinterpret_cast<const tng_drop*>(drop),
+                         reinterpret_cast<const tng_matrix*>(gate), &dx, scratch.data_ptr(), bytes);
+    if (status == 0)
+      status = e.product(stream, &qt, tqts.data_ptr<float>(), &xt, nullptr, nullptr, nullptr, nullptr, &dw, scratch.data_ptr(), bytes);
+    Py_END_ALLOW_THREADS
+    if (status != 0) return PyLong_FromLong(status);
+    return Py_BuildValue("(NNN)", THPVariable_Wrap(tdx), THPVariable_Wrap(tdw), THPVariable_Wrap(tdb));
+  } catch (const std::exception&) {
+    Py_RETURN_NONE;
+  }
+}
+
 PyMethodDef methods[] = {
     {"call", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(call)), METH_FASTCALL, nullptr},
     {"layer", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(layer)), METH_FASTCALL, nullptr},
+    {"linear", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(linear)), METH_FASTCALL, nullptr},
+    {"linear_grad", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(linear_grad)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "tng_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

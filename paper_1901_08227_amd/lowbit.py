@@ -114,6 +114,27 @@ def _through_ctypes(name, kinds, names, device, stream, args):
     return getattr(L, name)(ctypes.c_void_p(stream), *values)
 
 
+def _stream(device):
+    return torch._C._cuda_getCurrentRawStream(device.index)
+
+
+def _plain(device):
+    """Whether the whole layer may be tried by the native function: on the current GPU."""
+    B.lib()
+    return device.type == "cuda" and device.index == torch.cuda.current_device()
+
+
+_entries = None
+
+
+def _layer_entries():
+    global _entries
+    if _entries is None:
+        _entries = tuple(B._address[n] for n in ("tng_quantize_rows", "tng_quantize_grad", "tng_quantize_grad_bytes", "tng_matmul_i8",
+                                                 "tng_matmul_i8_bytes"))
+    return _entries
+
+
 def _run(name, device, *args):
     """A layer call on the current stream of the device, by the native function where its arguments are plain."""
     if device.type != "cuda":
@@ -123,7 +144,7 @@ def _run(name, device, *args):
             return _run(name, device, *args)
     B.lib()
     kinds, names = _CALLS[name]
-    stream = torch._C._cuda_getCurrentRawStream(device.index)
+    stream = _stream(device)
     status = B._layer(B._address[name], B._address.get(name + "_bytes", 0), stream, kinds, *args)
     if status is None:
         status = _through_ctypes(name, kinds, names, device, stream, args)
@@ -205,6 +226,14 @@ def matmul_i8(a, b, a_scale=None, b_scale=None, bias=None, dtype=torch.float32, 
 def linear(x, weight, bias=None, drop=None, keep=False):
     """The layer's result of x's type: the rows of x (of what drop makes of them) are coded and multiplied by the weights' codes.
     keep: also what linear_grad needs of this pass."""
+    kept_x = x if drop is not None and drop.relu else None
+    if _plain(x.device):
+        got = B._linear(_layer_entries(), _stream(x.device), x, drop, weight.q, weight.scale, bias, bool(keep))
+        if isinstance(got, int):
+            B._check(got, "linear")
+        if got is not None:
+            return (got[0], Saved(kept_x, drop, got[1], got[2])) if keep else got
+    # (what is not plain: the calls one by one, which take it or say what is wrong)
     if keep:
         q, scale, qt = quantize_rows(x, drop, turned=True)
     else:
@@ -212,7 +241,7 @@ def linear(x, weight, bias=None, drop=None, keep=False):
     y = matmul_i8(q, weight.q, scale, weight.scale, bias, dtype=x.dtype)
     if not keep:
         return y
-    return y, Saved(x if drop is not None and drop.relu else None, drop, scale, qt)
+    return y, Saved(kept_x, drop, scale, qt)
 
 
 def linear_grad(dy, saved, weight, *, seed, iter, site, out=None):
@@ -221,6 +250,13 @@ def linear_grad(dy, saved, weight, *, seed, iter, site, out=None):
     is that of the product of the codes, which stand for x and the weights.  out: where dw is written, any pitch."""
     if weight.qt is None:
         raise ValueError("linear_grad needs the weights' turned codes")
+    if _plain(dy.device):
+        got = B._linear_grad(_layer_entries(), _stream(dy.device), dy, saved.scale, saved.qt, weight.scale, weight.qt, saved.drop, saved.x,
+                             (seed, iter, site, 0.0, False), out)
+        if isinstance(got, int):
+            B._check(got, "linear_grad")
+        if got is not None:
+            return got
     q, q_scale, qt, qt_scale, db = quantize_grad(dy, weight.scale, saved.scale, seed=seed, iter=iter, site=site)
     dx = matmul_i8(q, weight.qt, q_scale, dtype=dy.dtype, drop=saved.drop, x=saved.x)
     dw = matmul_i8(qt, saved.qt, qt_scale, out=out)
