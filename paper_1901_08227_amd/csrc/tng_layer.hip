@@ -275,25 +275,27 @@ void quantize_rows_typed(const Extent& n, const DropArgs& d, const View& x, cons
     quantize_long_rows_kernel<T, DROP><<<dim3((uint32_t)all), kBlock, 0, s>>>(n.rows, n.cols, d, x, q, scale);
 }
 
-// ---- codes the other way round.  A tile is 128 x 128 codes; in LDS they lie as [column][row], 16-byte pieces of a column's 128
-// rows moved by the column's number / 16 so that the writes of a wavefront do not meet in one bank.
+// ---- codes the other way round.  A tile is ROWS x 128 codes; in LDS they lie as [column][row], 16-byte pieces of a column's rows moved
+// by the column's number / 16 so that the writes of a wavefront do not meet in one bank.
 constexpr int kTile = 128;
 
+template <int ROWS>
 __device__ __forceinline__ uint32_t turned_at(uint32_t col, uint32_t group) {  // 4-byte word of rows 4 group .. 4 group + 3
-  return col * (kTile / 4) + (group ^ ((col >> 4) << 2));
+  return col * (ROWS / 4) + (group ^ ((col >> 4 << 2) & (ROWS / 4 - 1)));
 }
 
-// words: [kTile][kTile / 4].  Columns c0 .. of a worker's matrix become rows of qt, r0 .. its columns.
+// words: [kTile][ROWS / 4].  Columns c0 .. of a worker's matrix become rows of qt, r0 .. its columns.
+template <int ROWS>
 __device__ __forceinline__ void store_turned(const uint32_t* words, const View& qt, uint32_t m, uint64_t r0, uint64_t c0, uint64_t rows,
                                              uint64_t cols) {
   typedef uint32_t four __attribute__((ext_vector_type(4)));
   typedef uint32_t four_any __attribute__((ext_vector_type(4), aligned(1)));
 #pragma unroll
-  for (int k = 0; k < kTile * kTile / 16 / kBlock; ++k) {
-    const uint32_t piece = k * kBlock + threadIdx.x, col = piece / 8, at = piece % 8;
+  for (int k = 0; k < kTile * ROWS / 16 / kBlock; ++k) {
+    const uint32_t piece = k * kBlock + threadIdx.x, col = piece / (ROWS / 16), at = piece % (ROWS / 16);
     const uint64_t r = r0 + at * 16;
     if (c0 + col >= cols || r >= rows) continue;
-    const four v = *reinterpret_cast<const four*>(words + turned_at(col, at * 4));
+    const four v = *reinterpret_cast<const four*>(words + turned_at<ROWS>(col, at * 4));
     int8_t* p = static_cast<int8_t*>(qt.p) + m * qt.pitch + (c0 + col) * qt.ld + r;
     if (rows - r >= 16) {
       *reinterpret_cast<four_any*>(p) = v;
@@ -319,25 +321,25 @@ __global__ void __launch_bounds__(kBlock) turn_codes_kernel(uint64_t rows, uint6
   __shared__ __align__(16) uint32_t words[kTile * kTile / 4];
   const uint32_t m = blockIdx.z, chunk = threadIdx.x % 8, group = threadIdx.x / 8;
   const uint64_t r0 = (uint64_t)blockIdx.y * kTile, c0 = (uint64_t)blockIdx.x * kTile;
-  const uint64_t c = c0 + chunk * 16;
+  // 16 columns a lane; the last 16 where a row ends inside them (as eight_at)
+  const bool narrow = cols < 16, some = c0 + chunk * 16 < cols;
+  const uint64_t c = narrow ? c0 + chunk * 16 : min(c0 + chunk * 16, cols - 16);
+  const int at = narrow ? (int)chunk * 16 : (int)((int64_t)c - (int64_t)c0);
   typedef uint32_t four __attribute__((ext_vector_type(4), aligned(1)));
-  uint32_t w[4][4];
+  four w[4];
+  if (!narrow) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint64_t r = r0 + group * 4 + i;
+    for (int i = 0; i < 4; ++i)
+      w[i] = *reinterpret_cast<const four*>(static_cast<const int8_t*>(q.p) + m * q.pitch + min(r0 + group * 4 + i, rows - 1) * q.ld + c);
+  } else {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) w[i][k] = 0u;
-    if (r < rows && c < cols) {
-      const int8_t* p = static_cast<const int8_t*>(q.p) + m * q.pitch + r * q.ld + c;
-      if (cols - c >= 16) {
-        const four v = *reinterpret_cast<const four*>(p);
+    for (int i = 0; i < 4; ++i) {
+      const int8_t* p = static_cast<const int8_t*>(q.p) + m * q.pitch + min(r0 + group * 4 + i, rows - 1) * q.ld + c;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) w[i][k] = v[k];
-      } else {
+      for (uint32_t k = 0; k < 4; ++k) w[i][k] = 0u;
 #pragma unroll
-        for (uint32_t k = 0; k < 16; ++k)
-          if (k < cols - c) w[i][k / 4] |= (uint32_t)(uint8_t)p[k] << (k % 4 * 8);
-      }
+      for (uint32_t k = 0; k < 16; ++k)
+        if (c + k < cols) w[i][k / 4] |= (uint32_t)(uint8_t)p[k] << (k % 4 * 8);
     }
   }
 #pragma unroll
@@ -345,10 +347,11 @@ __global__ void __launch_bounds__(kBlock) turn_codes_kernel(uint64_t rows, uint6
     uint32_t t[4] = {w[0][k], w[1][k], w[2][k], w[3][k]};
     turn4(t);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) words[turned_at(chunk * 16 + k * 4 + j, group)] = t[j];
+    for (int j = 0; j < 4; ++j)
+      if (some && at + k * 4 + j >= 0) words[turned_at<kTile>(at + k * 4 + j, group)] = t[j];
   }
   __syncthreads();
-  store_turned(words, qt, m, r0, c0, rows, cols);
+  store_turned<kTile>(words, qt, m, r0, c0, rows, cols);
 }
 
 // ---- codes of a gradient
@@ -356,7 +359,15 @@ __global__ void __launch_bounds__(kBlock) turn_codes_kernel(uint64_t rows, uint6
 // dy[t][n] is coded twice: dy[t][n] col_scale[n] along n (one scale a row, for the product with the weights' codes) and
 // dy[t][n] row_scale[t] along t (one scale a column of a worker, for the product with the tokens' codes).  The first kernel takes
 // both kinds of maxima and the columns' sums in one pass, the second puts the pieces together, the third codes.
-constexpr int kStatRows = 64, kStatCols = kWave * 8;
+constexpr int kStatCols = kWave * 8;
+
+// Rows of a chunk: a wavefront takes a quarter of them, one pair after another, so few where that still leaves every CU a workgroup.
+uint32_t chunk_rows(const Extent& n) {
+  const uint64_t tiles = (n.cols + kStatCols - 1) / kStatCols;
+  for (const uint32_t rows : {64u, 32u, 16u})
+    if (n.workers * tiles * ((n.rows + rows - 1) / rows) >= 512) return rows;
+  return 8u;
+}
 
 struct GradScratch {
   float *row_inv, *col_inv;         // [workers][rows], [workers][cols]
@@ -365,14 +376,14 @@ struct GradScratch {
 };
 
 template <typename T, bool NARROW>
-__global__ void __launch_bounds__(kBlock) grad_stats_kernel(uint64_t rows, uint64_t cols, uint32_t tiles, uint32_t chunks, View dy,
+__global__ void __launch_bounds__(kBlock) grad_stats_kernel(uint64_t rows, uint64_t cols, uint32_t tiles, uint32_t chunks, uint32_t each, View dy,
                                                             const float* col_scale, const float* row_scale, GradScratch out) {
   constexpr int kWaves = kBlock / kWave, kMany = 2;  // rows at a time, and as many under way
   const uint32_t m = blockIdx.y, lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   const uint32_t chunk = blockIdx.x / tiles, tile = blockIdx.x - chunk * tiles;
   const uint64_t c0 = (uint64_t)tile * kStatCols, c = eight_at<NARROW>(c0 + lane * 8, cols);
-  const uint64_t r0 = (uint64_t)chunk * kStatRows + wave * (kStatRows / kWaves);
-  const uint64_t end = min(rows, r0 + kStatRows / kWaves);
+  const uint64_t r0 = (uint64_t)chunk * each + wave * (each / kWaves);
+  const uint64_t end = min(rows, r0 + each / kWaves);
   float scale[8], sum[8];
   uint32_t top[8];
 #pragma unroll
@@ -476,12 +487,14 @@ __global__ void __launch_bounds__(kBlock) grad_finish_kernel(uint64_t rows, uint
   }
 }
 
-template <typename T, bool NARROW>
+// HALVES times 64 rows for a workgroup: one where there are few tiles, for its time.
+template <typename T, bool NARROW, int HALVES>
 __global__ void __launch_bounds__(kBlock, 4) grad_codes_kernel(uint64_t rows, uint64_t cols, DropArgs key, View dy, const float* col_scale,
                                                             const float* row_scale, GradScratch in, View q, View qt) {
-  __shared__ __align__(16) uint32_t words[kTile * kTile / 4];
+  constexpr int kRows = HALVES * 64;
+  __shared__ __align__(16) uint32_t words[kTile * kRows / 4];
   const uint32_t m = blockIdx.z, chunk = threadIdx.x % 16, group = threadIdx.x / 16;
-  const uint64_t r0 = (uint64_t)blockIdx.y * kTile, c0 = (uint64_t)blockIdx.x * kTile, c = eight_at<NARROW>(c0 + chunk * 8, cols);
+  const uint64_t r0 = (uint64_t)blockIdx.y * kRows, c0 = (uint64_t)blockIdx.x * kTile, c = eight_at<NARROW>(c0 + chunk * 8, cols);
   const bool some = c0 + chunk * 8 < cols;
   const int at = NARROW ? (int)chunk * 8 : (int)((int64_t)c - (int64_t)c0);  // (before the tile, in a last tile of less than eight columns)
   float scale[8], inv[8];
@@ -490,7 +503,7 @@ __global__ void __launch_bounds__(kBlock, 4) grad_codes_kernel(uint64_t rows, ui
   if (col_scale != nullptr) load8<float, NARROW>(col_scale, c, cols, scale);
   load8<float, NARROW>(in.col_inv + m * cols, c, cols, inv);
 #pragma unroll 1
-  for (uint32_t half = 0; half < 2; ++half) {
+  for (uint32_t half = 0; half < HALVES; ++half) {
     const uint32_t g = group + half * 16;
     const uint64_t r = r0 + g * 4;
     Raw8<T, NARROW> raw[4];
@@ -517,14 +530,14 @@ __global__ void __launch_bounds__(kBlock, 4) grad_codes_kernel(uint64_t rows, ui
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-      if (at + i >= 0 && some) words[turned_at(at + i, g)] = pack4(down[0][i], down[1][i], down[2][i], down[3][i]);
+      if (at + i >= 0 && some) words[turned_at<kRows>(at + i, g)] = pack4(down[0][i], down[1][i], down[2][i], down[3][i]);
   }
   __syncthreads();
-  store_turned(words, qt, m, r0, c0, rows, cols);
+  store_turned<kRows>(words, qt, m, r0, c0, rows, cols);
 }
 
 GradScratch grad_scratch(const Extent& n, float* p) {
-  const uint64_t tiles = (n.cols + kStatCols - 1) / kStatCols, chunks = (n.rows + kStatRows - 1) / kStatRows;
+  const uint64_t tiles = (n.cols + kStatCols - 1) / kStatCols, chunks = (n.rows + chunk_rows(n) - 1) / chunk_rows(n);
   GradScratch g;
   g.row_inv = p;
   p += n.workers * n.rows;
@@ -543,16 +556,22 @@ hipError_t quantize_grad_typed(const Extent& n, const DropArgs& key, const View&
                                const View& q, float* q_scale, const View& qt, float* qt_scale, float* col_sum, float* scratch,
                                hipStream_t s) {
   const GradScratch g = grad_scratch(n, scratch);
-  const uint32_t tiles = (uint32_t)((n.cols + kStatCols - 1) / kStatCols), chunks = (uint32_t)((n.rows + kStatRows - 1) / kStatRows);
+  const uint32_t each = chunk_rows(n);
+  const uint32_t tiles = (uint32_t)((n.cols + kStatCols - 1) / kStatCols), chunks = (uint32_t)((n.rows + each - 1) / each);
   const bool none = n.rows == 0 || n.cols == 0;  // (scales and sums are 0 then)
-  if (!none) grad_stats_kernel<T, NARROW><<<dim3(tiles * chunks, n.workers), kBlock, 0, s>>>(n.rows, n.cols, tiles, chunks, dy, col_scale, row_scale, g);
+  if (!none) grad_stats_kernel<T, NARROW><<<dim3(tiles * chunks, n.workers), kBlock, 0, s>>>(n.rows, n.cols, tiles, chunks, each, dy, col_scale, row_scale, g);
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   const uint32_t row_blocks = (uint32_t)((n.rows + kBlock - 1) / kBlock), col_blocks = (uint32_t)((n.cols + kBlock - 1) / kBlock);
   grad_finish_kernel<<<dim3(row_blocks + col_blocks, n.workers), kBlock, 0, s>>>(n.rows, n.cols, tiles, chunks, row_blocks, g, q_scale,
                                                                                  qt_scale, col_sum);
   if (hipError_t e = hipGetLastError(); e != hipSuccess || none) return e;
-  const dim3 grid((uint32_t)((n.cols + kTile - 1) / kTile), (uint32_t)((n.rows + kTile - 1) / kTile), n.workers);
-  grad_codes_kernel<T, NARROW><<<grid, kBlock, 0, s>>>(n.rows, n.cols, key, dy, col_scale, row_scale, g, q, qt);
+  const uint32_t across = (uint32_t)((n.cols + kTile - 1) / kTile);
+  if (n.workers * across * ((n.rows + 127) / 128) >= 256)
+    grad_codes_kernel<T, NARROW, 2><<<dim3(across, (uint32_t)((n.rows + 127) / 128), n.workers), kBlock, 0, s>>>(
+        n.rows, n.cols, key, dy, col_scale, row_scale, g, q, qt);
+  else
+    grad_codes_kernel<T, NARROW, 1><<<dim3(across, (uint32_t)((n.rows + 63) / 64), n.workers), kBlock, 0, s>>>(n.rows, n.cols, key, dy, col_scale,
+                                                                                                          row_scale, g, q, qt);
   return hipGetLastError();
 }
 
@@ -588,7 +607,7 @@ hipError_t launch_quantize_rows(tng_type type, const Extent& n, const DropArgs* 
 }
 
 size_t quantize_grad_floats(const Extent& n) {
-  const uint64_t tiles = (n.cols + kStatCols - 1) / kStatCols, chunks = (n.rows + kStatRows - 1) / kStatRows;
+  const uint64_t tiles = (n.cols + kStatCols - 1) / kStatCols, chunks = (n.rows + chunk_rows(n) - 1) / chunk_rows(n);
   return n.workers * (n.rows + n.cols + tiles * n.rows + 2 * chunks * n.cols);
 }
 

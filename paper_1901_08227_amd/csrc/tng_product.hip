@@ -304,15 +304,22 @@ __device__ __forceinline__ void write_tile(const Task& p, const Spot& s, const v
   typedef T run_t __attribute__((ext_vector_type(kRun), aligned(alignof(T))));
   uint32_t w[TN], row[TN];
   run_t ahead[TN];
+  constexpr bool kClamped = CN <= 4;  // (large tiles have no registers for it, and few of them are not whole)
   auto fetch = [&](int b, uint32_t n) {
-    ahead[b] = *reinterpret_cast<const run_t*>(static_cast<const T*>(p.x.p) + w[b] * p.x.pitch + row[b] * p.x.ld + s.n0 + n);
+    const T* from = static_cast<const T*>(p.x.p) + w[b] * p.x.pitch + row[b] * p.x.ld + s.n0;
+    if (full) {
+      ahead[b] = *reinterpret_cast<const run_t*>(from + n);
+    } else if (kClamped) {  // (past the end: the last channel, for a result that goes nowhere)
+#pragma unroll
+      for (int r = 0; r < kRun; ++r) ahead[b][r] = from[min(n + r, s.channels - 1)];
+    }
   };
   if (END == kTail) {
 #pragma unroll
     for (int b = 0; b < TN; ++b) {
-      row[b] = (uint32_t)s.t0 + t_in + b * 16;
+      row[b] = (uint32_t)s.t0 + min(t_in + b * 16, s.tokens - 1);
       w[b] = worker_of(p, s.m, &row[b]);
-      if (full && p.drop.relu) fetch(b, n_in);
+      if (p.drop.relu) fetch(b, n_in);
     }
   }
   float sa[TN];
@@ -348,7 +355,7 @@ __device__ __forceinline__ void write_tile(const Task& p, const Spot& s, const v
         for (int r = 0; r < kRun; ++r) y[r] = scaled((float)sum[a + r / 4][b][r % 4], sa[b], sb[r], bias[r]);
         if (END == kTail) {
           float x[kRun];
-          if (full) {
+          if (full || kClamped) {
 #pragma unroll
             for (int r = 0; r < kRun; ++r) x[r] = p.drop.relu ? (float)ahead[b][r] : 1.f;
             if (p.drop.relu && a + K::kTilesOfRun < CN) fetch(b, n_in + K::channel_row(a + K::kTilesOfRun, 0));
@@ -643,7 +650,7 @@ bool pieces_aligned(const Product& p) {
   return fits(p.a) && fits(p.b);
 }
 
-enum class Way { kAny, kFew, kSmallTiles, kLargeTiles };
+enum class Way { kAny, kFew, kNarrowTiles, kSmallTiles, kLargeTiles };
 
 struct Plan {
   Way way;
@@ -655,26 +662,33 @@ uint64_t over(uint64_t n, uint64_t by) { return (n + by - 1) / by; }
 
 uint64_t part_pitch(const Product& p) { return over(p.channels, 8) * 8; }  // (rows of partial sums hold whole runs)
 
-// Which tiles, and how many splits of the depth.  Estimated, in us, from what was measured: a stage of 256 x 256 results takes 1.2 to 1.6, of
-// 128 x 128 0.43 where few CUs work (the loads' latency) to 0.62 where all do; each tile of a workgroup 8 or 3 beside its stages (first
-// loads, scaling, writing); joining splits 5 and their bytes at 4 TB/s.  Both sides, us, large / small tiles: 8192 x 8192 x 8192 426 / 585;
-// 8192 x 8192 x 1024 105 / 137; 2048 x 2048 x 2048 26.7 / 14.3; 1537 x 2053 x 1999 31 / 18; 200 x 8192 x 5000 58 / 26; one / two
-// splits of the small: 1024 x 1024 x 8192 31 / 25; 4096 x 512 x 4096 19.8 / 24.6.
+// Which tiles, and how many splits of the depth.  Estimated, in us, from what was measured: a stage takes a fixed time where few CUs work (the
+// loads' latency) and more where all do (what the dies' caches hand out, some 13 TB/s in all); each tile of a workgroup has its time
+// beside its stages (first loads, scaling, writing); joining splits takes 5 and their bytes at 4 TB/s.  All sides, us, tokens x channels x depth,
+// narrow (64 channels x 128 tokens) / small (128 x 128) / large tiles (256 x 256): 333 x 1003 x 1000 6.9 / 8.7 / 12; 200 x 8192 x 5000 22.7 / 26 / 58;
+// 1024 x 1024 x 8192 24.4 / 31.7 / 75; 2048 x 2048 x 2048 18.6 / 14.7 / 26.7; 8192 x 8192 x 1024 166 / 134 / 94; 8192 x 8192 x 8192 - / 585 /
+// 407; one / two splits of the small: 1024 x 1024 x 8192 31 / 25; 4096 x 512 x 4096 19.8 / 24.6.
 void by_tiles(const Product& p, Plan* plan) {
+  struct Kind {
+    Way way;
+    uint64_t tokens, channels;
+    double stage, busy_stage, tile;
+  };
+  constexpr Kind kinds[] = {{Way::kNarrowTiles, 128, 64, 0.30, 0.17, 3.0}, {Way::kSmallTiles, 128, 128, 0.43, 0.19, 3.0}, {Way::kLargeTiles, 256, 256, 1.2, 0.4, 8.0}};
   constexpr double kCus = 256.0;
   const uint32_t least = plan->splits;  // that keep the sums inside 32 bits
   double best = 0.0;
-  for (const bool large : {false, true}) {
-    const uint64_t side = large ? 256 : 128, tiles = over(p.rows, side) * over(p.channels, side) * p.workers;
+  for (const Kind& kind : kinds) {
+    const uint64_t tiles = over(p.rows, kind.tokens) * over(p.channels, kind.channels) * p.workers;
     for (uint32_t splits = least; splits <= std::max(least, 8u); ++splits) {
       const uint64_t stages = over(over(p.depth, kDepth), splits), all = tiles * splits;
       if (splits > least && (all > (uint64_t)kCus || stages < 8)) break;
-      const double busy = std::min(1.0, (double)all / kCus), stage = large ? 1.2 + 0.4 * busy : 0.43 + 0.19 * busy;
-      double us = std::ceil((double)all / kCus) * ((double)stages * stage + (large ? 8.0 : 3.0));
+      const double stage = kind.stage + kind.busy_stage * std::min(1.0, (double)all / kCus);
+      double us = std::ceil((double)all / kCus) * ((double)stages * stage + kind.tile);
       if (splits > 1) us += 5.0 + (double)(splits * p.workers * p.rows) * (double)part_pitch(p) * 8e-6 / 4.0;
       if (best == 0.0 || us < best) {
         best = us;
-        plan->way = large ? Way::kLargeTiles : Way::kSmallTiles;
+        plan->way = kind.way;
         plan->splits = splits;
       }
     }
@@ -768,6 +782,7 @@ hipError_t product_typed(const Product& p, void* scratch, hipStream_t s) {
       else
         launch_few<T, 4>(t, s);
       break;
+    case Way::kNarrowTiles: launch_tiles<T, 2, 2, 2, 4, 4>(t, s); break;
     case Way::kSmallTiles: launch_tiles<T, 4, 2, 2, 4, 4>(t, s); break;
     case Way::kLargeTiles:
       launch_tiles<T, 8, 4, 2, 4, 2>(t, s);
