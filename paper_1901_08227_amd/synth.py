@@ -113,3 +113,14 @@ def codec_inputs(M: int, d: int, seed: int, rel_variance: float = 0.1, device="c
         grads[m].normal_(generator=g)
         grads[m].mul_(sd).mul_(gref.abs()).add_(gref)
     return grads, gref
+
+
+def class_mixture(M: int, rows: int, width: int, classes: int, seed: int, it: int, spread: float = 1.0, device="cpu"):
+    """Minibatches of a Gaussian mixture, one centre ~ N(0, spread^2 I) for each class: iteration `it` of worker m.
+
+    Returns (x[M][rows][width] = centre of the label + N(0, 1), labels[M][rows] uniform).
+    """
+    centres = spread * torch.randn((classes, width), generator=_gen(seed, device), device=device)
+    g = _gen(seed * 1000003 + it + 1, device)
+    labels = torch.randint(0, classes, (M, rows), generator=g, device=device)
+    return centres[labels] + torch.randn((M, rows, width), generator=g, device=device), labels
