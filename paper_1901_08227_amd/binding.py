@@ -128,9 +128,11 @@ def lib() -> ctypes.CDLL:
             "tng_quantize_rows": [vp, dropp, matp, matp, vp, matp],
             "tng_quantize_grad": [vp, dropp, matp, vp, vp, matp, vp, matp, vp, vp, vp, ctypes.c_size_t],
             "tng_matmul_i8": [vp, matp, vp, matp, vp, vp, dropp, matp, matp, vp, ctypes.c_size_t],
+            "tng_linear_i8": [vp, dropp, matp, matp, vp, vp, matp, vp, ctypes.c_size_t],
         })
         L.tng_quantize_grad_bytes.restype, L.tng_quantize_grad_bytes.argtypes = ctypes.c_size_t, [matp]
-        L.tng_matmul_i8_bytes.restype, L.tng_matmul_i8_bytes.argtypes = ctypes.c_size_t, [matp, matp, matp]
+        for name in ("tng_matmul_i8_bytes", "tng_linear_i8_bytes"):
+            getattr(L, name).restype, getattr(L, name).argtypes = ctypes.c_size_t, [matp, matp, matp]
         for name, argtypes in sigs.items():
             fn = getattr(L, name)
             fn.restype, fn.argtypes = ctypes.c_int, argtypes
@@ -138,7 +140,8 @@ def lib() -> ctypes.CDLL:
         _address = {name: ctypes.cast(getattr(L, name), vp).value
                     for name in ("tng_local_grad", "tng_normalize_encode", "tng_decode_aggregate", "tng_update_reference",
                                  "tng_step", "tng_dropout", "tng_dropout_grad", "tng_quantize_rows", "tng_quantize_grad",
-                                 "tng_quantize_grad_bytes", "tng_matmul_i8", "tng_matmul_i8_bytes")}
+                                 "tng_quantize_grad_bytes", "tng_matmul_i8", "tng_matmul_i8_bytes", "tng_linear_i8",
+                                 "tng_linear_i8_bytes")}
         _lib = L
     return _lib
 

@@ -15,11 +15,11 @@
 // d the five fields of tng_drop in a tuple, and float32 vectors by the last matrix before them: r workers * rows, n rows, c cols long.  A w
 // (W) at the end takes no argument: scratch, as large as is said of the first matrix (of the first two and the last), from torch.
 //
-//   linear(addresses, stream, x, drop, codes, scales, bias, keep) -> y, or (y, scales, turned codes) with keep
+//   linear(addresses, stream, x, drop, codes, scales, bias) -> (y, scales, turned codes)
 //   linear_grad(addresses, stream, dy, scales, turned codes, weights' scales, weights' turned codes, drop, x, (seed, iter, site), out)
 //     -> (dx, dw, db)
 //
-// whole layers, what they put in between from torch: None as above, or the status of a call that refused.  addresses: a tuple.
+// whole layers in training, what they put in between from torch: None as above, or the status of a call that refused.  addresses: a tuple.
 #include <Python.h>
 
 #include <algorithm>
@@ -224,6 +224,7 @@ PyObject* layer(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     switch (n) {
       case 5: status = enter_layer(f, a, std::make_index_sequence<5>{}); break;
       case 6: status = enter_layer(f, a, std::make_index_sequence<6>{}); break;
+      case 9: status = enter_layer(f, a, std::make_index_sequence<9>{}); break;
       case 11: status = enter_layer(f, a, std::make_index_sequence<11>{}); break;
       case 12: status = enter_layer(f, a, std::make_index_sequence<12>{}); break;
       default: break;
@@ -306,12 +307,11 @@ at::Tensor bytes_of(const at::Tensor& x, size_t n) { return at::empty({(int64_t)
 
 PyObject* linear(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   Entries e;
-  if (nargs != 8 || !entries_of(args[0], &e)) {
-    if (!PyErr_Occurred()) PyErr_SetString(PyExc_TypeError, "linear: addresses, stream, x, drop, codes, scales, bias, keep");
+  if (nargs != 7 || !entries_of(args[0], &e)) {
+    if (!PyErr_Occurred()) PyErr_SetString(PyExc_TypeError, "linear: addresses, stream, x, drop, codes, scales, bias");
     return nullptr;
   }
   const uintptr_t stream = (uintptr_t)PyLong_AsUnsignedLongLong(args[1]);
-  const bool keep = args[7] == Py_True;
   if (PyErr_Occurred()) return nullptr;
   try {
     LayerCall c;
@@ -322,22 +322,20 @@ PyObject* linear(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     const tng_matrix x = c.matrix[0], w = c.matrix[1];
     if (w.cols != x.cols || w.workers != 1) Py_RETURN_NONE;
     const at::Tensor& tx = THPVariable_Unpack(args[2]);
-    tng_matrix q, qt{}, y;
-    const at::Tensor tq = codes(tx, x.rows, x.cols, &q), ts = floats(tx, x.rows), ty = numbers(tx, x.rows, w.rows, tx.scalar_type(), &y);
-    at::Tensor tqt;
-    if (keep) tqt = codes(tx, x.cols, x.rows, &qt);
+    tng_matrix q, qt, y;
+    const at::Tensor tq = codes(tx, x.rows, x.cols, &q), tqt = codes(tx, x.cols, x.rows, &qt), ts = floats(tx, x.rows);
+    const at::Tensor ty = numbers(tx, x.rows, w.rows, tx.scalar_type(), &y);
     const size_t bytes = e.product_bytes(&q, &w, &y);
     if (bytes == 0) Py_RETURN_NONE;
     const at::Tensor scratch = bytes_of(tx, bytes);
     int status;
     Py_BEGIN_ALLOW_THREADS
-    status = e.quantize_rows(stream, reinterpret_cast<const tng_drop*>(drop), &x, &q, ts.data_ptr<float>(), keep ? &qt : nullptr);
+    status = e.quantize_rows(stream, reinterpret_cast<const tng_drop*>(drop), &x, &q, ts.data_ptr<float>(), &qt);
     if (status == 0)
       status = e.product(stream, &q, ts.data_ptr<float>(), &w, reinterpret_cast<const float*>(scales), reinterpret_cast<const float*>(bias),
                          nullptr, nullptr, &y, scratch.data_ptr(), bytes);
     Py_END_ALLOW_THREADS
     if (status != 0) return PyLong_FromLong(status);
-    if (!keep) return THPVariable_Wrap(ty);
     return Py_BuildValue("(NNN)", THPVariable_Wrap(ty), THPVariable_Wrap(ts), THPVariable_Wrap(tqt));
   } catch (const std::exception&) {
     Py_RETURN_NONE;

@@ -10,6 +10,7 @@ namespace {
 constexpr uint64_t kMaxDrawn = 1ull << 33, kMaxSide = 1ull << 22, kMaxRows = 1ull << 23;
 constexpr uint64_t kMaxStride = 1ull << 40;  // (products of strides and indexes stay far inside 64 bits)
 
+inline size_t round_up(size_t v) { return (v + 255) / 256 * 256; }
 inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 inline size_t size_of(int32_t type) { return type == TNG_TYPE_I8 ? 1 : type == TNG_TYPE_F32 ? 4 : 2; }
 inline bool is_float(int32_t type) { return type == TNG_TYPE_F32 || type == TNG_TYPE_BF16 || type == TNG_TYPE_F16; }
@@ -79,6 +80,24 @@ bool product_of(const tng_matrix* a, const tng_matrix* b, const tng_matrix* y, t
   p->b_scale_pitch = b->workers == 1 ? 0 : b->rows;
   p->y = view(y);
   p->type = (tng_type)y->type;
+  return true;
+}
+
+// Where tng_linear_i8 keeps the codes of x: rows 16 bytes apart, their scales, and what the product needs.
+struct LinearScratch {
+  tng_matrix q;  // (data: set where the workspace is known)
+  tng::Product product;
+  size_t scale_at, rest_at, bytes;
+};
+
+bool linear_scratch(const tng_matrix* x, const tng_matrix* b, const tng_matrix* y, LinearScratch* l) {
+  if (!sound(x, false) || !is_float(x->type) || !sides_ok(x) || y == nullptr || y->type != x->type) return false;
+  const uint64_t ld = (x->cols + 15) / 16 * 16;
+  l->q = tng_matrix{reinterpret_cast<void*>((uintptr_t)256), TNG_TYPE_I8, x->workers, x->rows, x->cols, ld, x->rows * ld};
+  if (!product_of(&l->q, b, y, &l->product)) return false;
+  l->scale_at = round_up(x->workers * x->rows * ld);
+  l->rest_at = l->scale_at + round_up(x->workers * x->rows * sizeof(float));
+  l->bytes = l->rest_at + 256 + tng::product_scratch_bytes(l->product);
   return true;
 }
 
@@ -170,6 +189,31 @@ tng_status tng_matmul_i8(void* hip_stream, const tng_matrix* a, const float* a_s
     if (drop->relu) p.x = view(x);
   }
   return hip_status(tng::launch_product(p, workspace, static_cast<hipStream_t>(hip_stream)));
+}
+
+size_t tng_linear_i8_bytes(const tng_matrix* x, const tng_matrix* b, const tng_matrix* y) {
+  LinearScratch l;
+  return linear_scratch(x, b, y, &l) ? l.bytes : 0;
+}
+
+tng_status tng_linear_i8(void* hip_stream, const tng_drop* drop, const tng_matrix* x, const tng_matrix* b, const float* b_scale,
+                         const float* bias, const tng_matrix* y, void* workspace, size_t workspace_bytes) {
+  LinearScratch l;
+  if ((drop != nullptr && !drop_ok(drop)) || !linear_scratch(x, b, y, &l)) return TNG_ERR_INVALID_ARG;
+  if (!aligned(b_scale, 4) || !aligned(bias, 4)) return TNG_ERR_INVALID_ARG;
+  if (empty(*y)) return TNG_OK;
+  if (workspace == nullptr || !aligned(workspace, 256) || workspace_bytes < l.bytes) return TNG_ERR_WORKSPACE;
+  if (drop == nullptr && tng::coded_product_applies(l.product)) {
+    l.product.b_scale = b_scale;
+    l.product.bias = bias;
+    return hip_status(tng::launch_coded_product(l.product, view(x), static_cast<hipStream_t>(hip_stream)));
+  }
+  char* at = static_cast<char*>(workspace);
+  l.q.data = at;
+  float* scale = reinterpret_cast<float*>(at + l.scale_at);
+  const tng_status s = tng_quantize_rows(hip_stream, drop, x, &l.q, scale, nullptr);
+  if (s != TNG_OK) return s;
+  return tng_matmul_i8(hip_stream, &l.q, scale, b, b_scale, bias, nullptr, nullptr, y, at + l.rest_at, workspace_bytes - l.rest_at);
 }
 
 }  // extern "C"

@@ -56,6 +56,7 @@ _CALLS = {
     "tng_quantize_rows": ("dmiri", ("drop", "x", "q", "scale", "qt")),
     "tng_quantize_grad": ("dmcririrrw", ("key", "dy", "col_scale", "row_scale", "q", "q_scale", "qt", "qt_scale", "col_sum")),
     "tng_matmul_i8": ("irirndmmW", ("a", "a_scale", "b", "b_scale", "bias", "drop", "x", "out")),
+    "tng_linear_i8": ("dmirnmW", ("drop", "x", "codes", "scale", "bias", "out")),
 }
 
 
@@ -226,22 +227,20 @@ def matmul_i8(a, b, a_scale=None, b_scale=None, bias=None, dtype=torch.float32, 
 def linear(x, weight, bias=None, drop=None, keep=False):
     """The layer's result of x's type: the rows of x (of what drop makes of them) are coded and multiplied by the weights' codes.
     keep: also what linear_grad needs of this pass."""
+    if not keep:
+        out = torch.empty((*_dims(x, "x")[:-1], _dims(weight.q, "codes")[-2]), dtype=x.dtype, device=x.device)
+        _run("tng_linear_i8", x.device, drop, x, weight.q, weight.scale, bias, out)
+        return out
     kept_x = x if drop is not None and drop.relu else None
     if _plain(x.device):
-        got = B._linear(_layer_entries(), _stream(x.device), x, drop, weight.q, weight.scale, bias, bool(keep))
+        got = B._linear(_layer_entries(), _stream(x.device), x, drop, weight.q, weight.scale, bias)
         if isinstance(got, int):
             B._check(got, "linear")
         if got is not None:
-            return (got[0], Saved(kept_x, drop, got[1], got[2])) if keep else got
+            return got[0], Saved(kept_x, drop, got[1], got[2])
     # (what is not plain: the calls one by one, which take it or say what is wrong)
-    if keep:
-        q, scale, qt = quantize_rows(x, drop, turned=True)
-    else:
-        q, scale = quantize_rows(x, drop)
-    y = matmul_i8(q, weight.q, scale, weight.scale, bias, dtype=x.dtype)
-    if not keep:
-        return y
-    return y, Saved(kept_x, drop, scale, qt)
+    q, scale, qt = quantize_rows(x, drop, turned=True)
+    return matmul_i8(q, weight.q, scale, weight.scale, bias, dtype=x.dtype), Saved(kept_x, drop, scale, qt)
 
 
 def linear_grad(dy, saved, weight, *, seed, iter, site, out=None):

@@ -336,6 +336,26 @@ def test_linear_and_its_gradient(M, T, K, N, dtype):
         assert np.all(np.abs(host(db) - host(dy).astype(np.float64).sum(1)) <= (40 + T / 128) * 2.0 ** -24 * np.abs(host(dy)).astype(np.float64).sum(1))
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("M,T", [(1, 1), (1, 2), (1, 3), (1, 5), (1, 8), (1, 9), (3, 1), (2, 7)])
+@pytest.mark.parametrize("K,N", [(1, 5), (7, 16), (8, 33), (100, 50), (128, 1000), (1000, 513), (1025, 40), (4096, 2050), (5000, 130), (20000, 60), (45000, 20)])
+def test_few_rows_in_one_call_are_the_two_calls(M, T, K, N, dtype):
+    x = normal((M, T, K), dtype, 78)
+    w = lowbit.weight(normal((N, K), torch.float32, 79), turned=False)
+    bias = normal((N,), torch.float32, 80)
+    if T > 2:
+        x[0, 1] = 0.0
+        x[0, 2, K // 2] = float("inf")
+    q, s = lowbit.quantize_rows(x)
+    for a in (x, spread(x, 0)):
+        for b in (bias, None):
+            want = lowbit.matmul_i8(q, w.q, s, w.scale, b, dtype=dtype)
+            got = lowbit.linear(a, w, b)
+            assert same(got, want.cpu())
+            if M == 1:
+                assert same(lowbit.linear(a[0], w, b), want[0].cpu())
+
+
 def test_one_worker_without_a_leading_dimension_is_the_same():
     x, dy = normal((1, 37, 130), torch.bfloat16, 75), normal((1, 37, 65), torch.bfloat16, 76)
     w = lowbit.weight(normal((65, 130), torch.float32, 77))

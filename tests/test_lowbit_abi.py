@@ -108,6 +108,25 @@ def test_product_refusals():
     assert call(a=mat(0, 8, B.TYPE_I8, data=None), y=mat(0, 6, data=None), ws=None, size=0) == B.TNG_OK
 
 
+def test_linear_refusals():
+    L = B.lib()
+    x, b, y = mat(4, 8, B.TYPE_F16), mat(6, 8, B.TYPE_I8), mat(4, 6, B.TYPE_F16)
+    need = L.tng_linear_i8_bytes(x, b, y)
+    assert need >= 4 * 16 + 4 * 4
+
+    def call(d=None, x=x, b=b, sb=None, bias=None, y=y, ws=P, size=need):
+        return L.tng_linear_i8(None, d, x, b, sb, bias, y, ws, size)
+
+    for kw in (dict(x=None), dict(b=None), dict(y=None), dict(x=mat(4, 8)), dict(x=mat(4, 8, B.TYPE_I8)), dict(x=mat(4, 7, B.TYPE_F16)), dict(b=x),
+               dict(y=mat(4, 5, B.TYPE_F16)), dict(y=mat(4, 6)), dict(d=drop(p=1.0)), dict(sb=P + 1), dict(bias=P + 2)):
+        assert call(**kw) == B.TNG_ERR_INVALID_ARG, kw
+        if set(kw) <= {"x", "b", "y"}:
+            assert L.tng_linear_i8_bytes(kw.get("x", x), kw.get("b", b), kw.get("y", y)) == 0
+    for kw in (dict(ws=None), dict(ws=P + 8), dict(size=need - 1)):
+        assert call(**kw) == B.TNG_ERR_WORKSPACE, kw
+    assert call(x=mat(0, 8, B.TYPE_F16, data=None), y=mat(0, 6, B.TYPE_F16, data=None), ws=None, size=0) == B.TNG_OK
+
+
 def test_a_product_of_many_pieces_sizes_their_sums():
     L = B.lib()
     a, b, y = mat(100, 1 << 18, B.TYPE_I8), mat(6, 1 << 18, B.TYPE_I8), mat(100, 6)
