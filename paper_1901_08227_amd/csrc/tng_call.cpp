@@ -13,7 +13,9 @@
 //
 // the same for the calls on layers: kinds has a letter per argument, m a matrix of numbers ([rows, cols] or [M, rows, cols]), i one of codes,
 // d the five fields of tng_drop in a tuple, and float32 vectors by the last matrix before them: r workers * rows, n rows, c cols long.  A w
-// (W) at the end takes no argument: scratch, as large as is said of the first matrix (of the first two and the last), from torch.
+// (W) at the end takes no argument: scratch, as large as is said of the first matrix (of the first two and the last), from torch.  Nor
+// does an o (p): a matrix like the first (with a column for each row of the last before it), from torch; that tensor is what is returned
+// where the call succeeds.
 //
 //   linear(addresses, stream, x, drop, codes, scales, bias) -> (y, scales, turned codes)
 //   linear_grad(addresses, stream, dy, scales, turned codes, weights' scales, weights' turned codes, drop, x, (seed, iter, site), out)
@@ -23,6 +25,7 @@
 #include <Python.h>
 
 #include <algorithm>
+#include <cstring>
 
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
@@ -94,6 +97,25 @@ PyObject* call(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   return PyLong_FromLong(status);
 }
 
+using Shape = c10::SmallVector<int64_t, 4>;
+
+// [M, rows, cols], without the M where x had none.
+Shape shape_like(const at::Tensor& x, int64_t rows, int64_t cols) {
+  Shape s;
+  if (x.dim() == 3) s.push_back(x.size(0));
+  s.push_back(rows);
+  s.push_back(cols);
+  return s;
+}
+
+// A matrix of numbers of x's type (or float32), and its tng_matrix.
+at::Tensor numbers(const at::Tensor& x, int64_t rows, int64_t cols, at::ScalarType type, tng_matrix* m) {
+  const at::Tensor t = at::empty(shape_like(x, rows, cols), x.options().dtype(type));
+  *m = tng_matrix{t.data_ptr(), type == at::kFloat ? TNG_TYPE_F32 : type == at::kHalf ? TNG_TYPE_F16 : TNG_TYPE_BF16,
+                  x.dim() == 3 ? (uint32_t)x.size(0) : 1u, (uint64_t)rows, (uint64_t)cols, (uint64_t)cols, (uint64_t)(rows * cols)};
+  return t;
+}
+
 constexpr int kLayerFixed = 4, kLayerMost = 16;
 
 // One argument of a layer call as the 64 bits that the entry point takes.
@@ -103,6 +125,7 @@ struct LayerCall {
   tng_drop drop;
   c10::Device device{c10::kCPU};
   bool have_device = false;
+  PyObject* first = nullptr;  // the first matrix
 
   bool same_device(const at::Tensor& t) {
     if (!have_device) {
@@ -142,7 +165,7 @@ struct LayerCall {
     m.cols = (uint64_t)sizes[dim - 1];
     m.ld = (uint64_t)strides[dim - 2];
     m.pitch = dim == 3 ? (uint64_t)strides[0] : 0u;
-    ++matrices;
+    if (matrices++ == 0) first = obj;
     *out = reinterpret_cast<uintptr_t>(&m);
     return true;
   }
@@ -188,7 +211,9 @@ PyObject* layer(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   }
   const Py_ssize_t letters = PyUnicode_GET_LENGTH(args[3]);
   const bool scratch = letters > 0 && (kinds[letters - 1] == 'w' || kinds[letters - 1] == 'W');
-  if (nargs != kLayerFixed + letters - scratch || letters > kLayerMost - 3) {
+  Py_ssize_t made = 0;  // without an argument
+  for (Py_ssize_t i = 0; i < letters; ++i) made += strchr("wWop", kinds[i]) != nullptr;
+  if (nargs != kLayerFixed + letters - made || letters > kLayerMost - 3) {
     PyErr_SetString(PyExc_TypeError, "layer: an argument per letter");
     return nullptr;
   }
@@ -198,8 +223,19 @@ PyObject* layer(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   LayerCall c;
   int n = 1, status = -1;
   try {
+    at::Tensor out;
+    PyObject* const* next = args + kLayerFixed;
     for (Py_ssize_t i = 0; i < letters - scratch; ++i, ++n) {
-      PyObject* obj = args[kLayerFixed + i];
+      if (kinds[i] == 'o' || kinds[i] == 'p') {
+        if (c.matrices == 0 || c.matrices == 8 || c.first == nullptr) Py_RETURN_NONE;
+        const tng_matrix& m = c.matrix[0];
+        const at::Tensor& like = THPVariable_Unpack(c.first);
+        out = numbers(like, (int64_t)m.rows, (int64_t)(kinds[i] == 'o' ? m.cols : c.matrix[c.matrices - 1].rows), like.scalar_type(),
+                      &c.matrix[c.matrices]);
+        a[n] = reinterpret_cast<uintptr_t>(&c.matrix[c.matrices++]);
+        continue;
+      }
+      PyObject* obj = *next++;
       if (obj == Py_None) {
         a[n] = 0;
         continue;
@@ -230,6 +266,7 @@ PyObject* layer(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
       default: break;
     }
     Py_END_ALLOW_THREADS
+    if (status == 0 && out.defined()) return THPVariable_Wrap(out);
   } catch (const std::exception&) {
     Py_RETURN_NONE;
   }
@@ -267,17 +304,6 @@ bool entries_of(PyObject* obj, Entries* e) {
   return !PyErr_Occurred();
 }
 
-using Shape = c10::SmallVector<int64_t, 4>;
-
-// [M, rows, cols], without the M where x had none.
-Shape shape_like(const at::Tensor& x, int64_t rows, int64_t cols) {
-  Shape s;
-  if (x.dim() == 3) s.push_back(x.size(0));
-  s.push_back(rows);
-  s.push_back(cols);
-  return s;
-}
-
 // Codes whose rows begin 16 bytes apart, and their matrix.
 at::Tensor codes(const at::Tensor& x, int64_t rows, int64_t cols, tng_matrix* m) {
   const int64_t ld = (cols + 15) / 16 * 16;
@@ -285,14 +311,6 @@ at::Tensor codes(const at::Tensor& x, int64_t rows, int64_t cols, tng_matrix* m)
   *m = tng_matrix{t.data_ptr(), TNG_TYPE_I8, x.dim() == 3 ? (uint32_t)x.size(0) : 1u, (uint64_t)rows, (uint64_t)cols, (uint64_t)ld,
                   (uint64_t)(rows * ld)};
   return ld == cols ? t : t.narrow(-1, 0, cols);
-}
-
-// A matrix of numbers of x's type (or float32), and its tng_matrix.
-at::Tensor numbers(const at::Tensor& x, int64_t rows, int64_t cols, at::ScalarType type, tng_matrix* m) {
-  const at::Tensor t = at::empty(shape_like(x, rows, cols), x.options().dtype(type));
-  *m = tng_matrix{t.data_ptr(), type == at::kFloat ? TNG_TYPE_F32 : type == at::kHalf ? TNG_TYPE_F16 : TNG_TYPE_BF16,
-                  x.dim() == 3 ? (uint32_t)x.size(0) : 1u, (uint64_t)rows, (uint64_t)cols, (uint64_t)cols, (uint64_t)(rows * cols)};
-  return t;
 }
 
 // A float32 vector: a row of each worker's.

@@ -49,14 +49,15 @@ class Saved(NamedTuple):
 
 
 _I8 = {torch.int8: B.TYPE_I8}
-# The arguments of the layer calls behind the stream, a letter each (see csrc/tng_call.cpp), and what they are called here.
+# The arguments of the layer calls behind the stream, a letter each (see csrc/tng_call.cpp), what they are called here, and the letters of a
+# call that makes its result.
 _CALLS = {
-    "tng_dropout": ("dmmm", ("drop", "x", "residual", "out")),
-    "tng_dropout_grad": ("dmmm", ("drop", "x", "dy", "out")),
-    "tng_quantize_rows": ("dmiri", ("drop", "x", "q", "scale", "qt")),
-    "tng_quantize_grad": ("dmcririrrw", ("key", "dy", "col_scale", "row_scale", "q", "q_scale", "qt", "qt_scale", "col_sum")),
-    "tng_matmul_i8": ("irirndmmW", ("a", "a_scale", "b", "b_scale", "bias", "drop", "x", "out")),
-    "tng_linear_i8": ("dmirnmW", ("drop", "x", "codes", "scale", "bias", "out")),
+    "tng_dropout": ("dmmm", ("drop", "x", "residual", "out"), "dmmo"),
+    "tng_dropout_grad": ("dmmm", ("drop", "x", "dy", "out"), None),
+    "tng_quantize_rows": ("dmiri", ("drop", "x", "q", "scale", "qt"), None),
+    "tng_quantize_grad": ("dmcririrrw", ("key", "dy", "col_scale", "row_scale", "q", "q_scale", "qt", "qt_scale", "col_sum"), None),
+    "tng_matmul_i8": ("irirndmmW", ("a", "a_scale", "b", "b_scale", "bias", "drop", "x", "out"), None),
+    "tng_linear_i8": ("dmirnmW", ("drop", "x", "codes", "scale", "bias", "out"), "dmirnpW"),
 }
 
 
@@ -136,20 +137,26 @@ def _layer_entries():
     return _entries
 
 
-def _run(name, device, *args):
-    """A layer call on the current stream of the device, by the native function where its arguments are plain."""
+def _run(name, device, *args, made=None):
+    """A layer call on the current stream of the device, by the native function where its arguments are plain.  made: the shape of the
+    result, which is like the first matrix but for its columns, if there is none among the arguments; the native function makes it."""
     if device.type != "cuda":
         raise TypeError(f"{name}: expected CUDA tensors")
     if device.index != torch.cuda.current_device():
         with torch.cuda.device(device):
-            return _run(name, device, *args)
+            return _run(name, device, *args, made=made)
     B.lib()
-    kinds, names = _CALLS[name]
+    kinds, names, makes = _CALLS[name]
     stream = _stream(device)
-    status = B._layer(B._address[name], B._address.get(name + "_bytes", 0), stream, kinds, *args)
+    status = B._layer(B._address[name], B._address.get(name + "_bytes", 0), stream, makes if made else kinds, *args)
     if status is None:
+        if made:
+            args = (*args, torch.empty(made, dtype=args[1].dtype, device=device))
         status = _through_ctypes(name, kinds, names, device, stream, args)
+    elif not isinstance(status, int):
+        return status
     B._check(status, name)
+    return args[-1]
 
 
 def _codes(shape, device):
@@ -180,16 +187,14 @@ def _dims(t, name):
 
 def dropout(x, drop, residual=None, out=None):
     """keep f(x) / (1 - p), plus the residual if there is one."""
-    out = _out(out, x.shape, x.dtype, x.device)
-    _run("tng_dropout", x.device, drop, x, residual, out)
-    return out
+    if out is None:
+        return _run("tng_dropout", x.device, drop, x, residual, made=x.shape)
+    return _run("tng_dropout", x.device, drop, x, residual, _out(out, x.shape, x.dtype, x.device))
 
 
 def dropout_grad(dy, drop, x=None, out=None):
     """The gradient of dropout's x from that of its result; x is needed if there is a relu."""
-    out = _out(out, dy.shape, dy.dtype, dy.device)
-    _run("tng_dropout_grad", dy.device, drop, x, dy, out)
-    return out
+    return _run("tng_dropout_grad", dy.device, drop, x, dy, _out(out, dy.shape, dy.dtype, dy.device))
 
 
 def quantize_rows(x, drop=None, turned=False):
@@ -220,17 +225,15 @@ def matmul_i8(a, b, a_scale=None, b_scale=None, bias=None, dtype=torch.float32, 
     """a_scale b_scale (a b^T) + bias: codes a [rows, depth] or [M, rows, depth], b [channels, depth] or one for each worker.
     drop, x: the result is a gradient that goes on through that dropout (and its relu, of x)."""
     out = _out(out, (*_dims(a, "a")[:-1], _dims(b, "b")[-2]), dtype, a.device)
-    _run("tng_matmul_i8", a.device, a, a_scale, b, b_scale, bias, drop, x, out)
-    return out
+    return _run("tng_matmul_i8", a.device, a, a_scale, b, b_scale, bias, drop, x, out)
 
 
 def linear(x, weight, bias=None, drop=None, keep=False):
     """The layer's result of x's type: the rows of x (of what drop makes of them) are coded and multiplied by the weights' codes.
     keep: also what linear_grad needs of this pass."""
     if not keep:
-        out = torch.empty((*_dims(x, "x")[:-1], _dims(weight.q, "codes")[-2]), dtype=x.dtype, device=x.device)
-        _run("tng_linear_i8", x.device, drop, x, weight.q, weight.scale, bias, out)
-        return out
+        made = (*_dims(x, "x")[:-1], _dims(weight.q, "codes")[-2])
+        return _run("tng_linear_i8", x.device, drop, x, weight.q, weight.scale, bias, made=made)
     kept_x = x if drop is not None and drop.relu else None
     if _plain(x.device):
         got = B._linear(_layer_entries(), _stream(x.device), x, drop, weight.q, weight.scale, bias)
