@@ -458,39 +458,72 @@ __global__ void __launch_bounds__(kBlock) grad_stats_kernel(uint64_t rows, uint6
   }
 }
 
+// The maximum (and the sum) of n partial results that are `stride` apart, eight under way at a time.
+__device__ __forceinline__ uint32_t max_of(const uint32_t* p, uint32_t n, uint64_t stride) {
+  uint32_t top = 0u;
+  for (uint32_t k = 0; k < n; k += 8) {
+    uint32_t t[8];
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i) t[i] = p[min(k + i, n - 1) * stride];
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i) top = max(top, t[i]);
+  }
+  return top;
+}
+__device__ __forceinline__ float sum_of(const float* p, uint32_t n, uint64_t stride) {
+  float sum = 0.f;
+  for (uint32_t k = 0; k < n; k += 8) {
+    float t[8];
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i) t[i] = p[min(k + i, n - 1) * stride];
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i) sum += k + i < n ? t[i] : 0.f;
+  }
+  return sum;
+}
+
+// What the statistics' pieces go to: where a product reads the scales, and the columns' sums (may be null).
+struct GradResults {
+  float *q_scale, *qt_scale, *col_sum;
+};
+
+// Row r and column c of worker m: its scale (and sum) out, the inverse of its largest magnitude back.
+__device__ __forceinline__ float finish_row(const GradScratch& in, const GradResults& out, uint32_t m, uint64_t r, uint64_t rows, uint32_t tiles,
+                                            bool write) {
+  const uint32_t top = max_of(in.row_part + (uint64_t)m * tiles * rows + r, tiles, rows);
+  if (write) out.q_scale[m * rows + r] = code_step(top);
+  return code_inverse(top);
+}
+__device__ __forceinline__ float finish_col(const GradScratch& in, const GradResults& out, uint32_t m, uint64_t c, uint64_t cols,
+                                            uint32_t chunks, bool write) {
+  const uint64_t at = (uint64_t)m * chunks * cols + c;
+  const uint32_t top = max_of(in.col_part + at, chunks, cols);
+  if (write) {
+    out.qt_scale[m * cols + c] = code_step(top);
+    if (out.col_sum != nullptr) out.col_sum[m * cols + c] = sum_of(in.sum_part + at, chunks, cols);
+  }
+  return code_inverse(top);
+}
+
 // One lane a row or a column: rows first (blockIdx.x < row_blocks), then columns.
 __global__ void __launch_bounds__(kBlock) grad_finish_kernel(uint64_t rows, uint64_t cols, uint32_t tiles, uint32_t chunks,
-                                                             uint32_t row_blocks, GradScratch in, float* q_scale, float* qt_scale,
-                                                             float* col_sum) {
+                                                             uint32_t row_blocks, GradScratch in, GradResults out) {
   const uint32_t m = blockIdx.y;
   const bool by_rows = blockIdx.x < row_blocks;
   const uint64_t j = (uint64_t)(by_rows ? blockIdx.x : blockIdx.x - row_blocks) * kBlock + threadIdx.x;
-  uint32_t top = 0u;
   if (by_rows) {
-    if (j >= rows) return;
-#pragma unroll 8
-    for (uint32_t k = 0; k < tiles; ++k) top = max(top, in.row_part[((uint64_t)m * tiles + k) * rows + j]);
-    in.row_inv[m * rows + j] = code_inverse(top);
-    q_scale[m * rows + j] = code_step(top);
+    if (j < rows) in.row_inv[m * rows + j] = finish_row(in, out, m, j, rows, tiles, true);
   } else {
-    if (j >= cols) return;
-    float sum = 0.f;
-#pragma unroll 8
-    for (uint32_t k = 0; k < chunks; ++k) {
-      const uint64_t at = ((uint64_t)m * chunks + k) * cols + j;
-      top = max(top, in.col_part[at]);
-      sum += in.sum_part[at];
-    }
-    in.col_inv[m * cols + j] = code_inverse(top);
-    qt_scale[m * cols + j] = code_step(top);
-    if (col_sum != nullptr) col_sum[m * cols + j] = sum;
+    if (j < cols) in.col_inv[m * cols + j] = finish_col(in, out, m, j, cols, chunks, true);
   }
 }
 
-// HALVES times 64 rows for a workgroup: one where there are few tiles, for its time.
-template <typename T, bool NARROW, int HALVES>
+// HALVES times 64 rows for a workgroup: one where there are few tiles, for its time.  JOINS: it puts the statistics of its rows and columns
+// together itself, where that is less than a launch.
+template <typename T, bool NARROW, int HALVES, bool JOINS>
 __global__ void __launch_bounds__(kBlock, 4) grad_codes_kernel(uint64_t rows, uint64_t cols, DropArgs key, View dy, const float* col_scale,
-                                                            const float* row_scale, GradScratch in, View q, View qt) {
+                                                            const float* row_scale, GradScratch in, GradResults out, uint32_t tiles,
+                                                            uint32_t chunks, View q, View qt) {
   constexpr int kRows = HALVES * 64;
   __shared__ __align__(16) uint32_t words[kTile * kRows / 4];
   const uint32_t m = blockIdx.z, chunk = threadIdx.x % 16, group = threadIdx.x / 16;
@@ -501,7 +534,20 @@ __global__ void __launch_bounds__(kBlock, 4) grad_codes_kernel(uint64_t rows, ui
 #pragma unroll
   for (int i = 0; i < 8; ++i) scale[i] = 1.f;
   if (col_scale != nullptr) load8<float, NARROW>(col_scale, c, cols, scale);
-  load8<float, NARROW>(in.col_inv + m * cols, c, cols, inv);
+  __shared__ float row_invs[JOINS ? kRows : 1], col_invs[JOINS ? kTile : 1];
+  if (JOINS) {
+    const uint32_t j = threadIdx.x % kTile;
+    if (threadIdx.x < kTile) {
+      if (j < kRows && r0 + j < rows) row_invs[j] = finish_row(in, out, m, r0 + j, rows, tiles, blockIdx.x == 0);
+    } else if (c0 + j < cols) {
+      col_invs[j] = finish_col(in, out, m, c0 + j, cols, chunks, blockIdx.y == 0);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) inv[i] = col_invs[min(max(at + i, 0), kTile - 1)];
+  } else {
+    load8<float, NARROW>(in.col_inv + m * cols, c, cols, inv);
+  }
 #pragma unroll 1
   for (uint32_t half = 0; half < HALVES; ++half) {
     const uint32_t g = group + half * 16;
@@ -512,7 +558,7 @@ __global__ void __launch_bounds__(kBlock, 4) grad_codes_kernel(uint64_t rows, ui
     for (int k = 0; k < 4; ++k) {  // (past the end: the last row again, whose codes go nowhere)
       const uint64_t row = min(r + k, rows - 1);
       raw[k].load(static_cast<const T*>(dy.p) + m * dy.pitch + row * dy.ld, c, cols);
-      row_inv[k] = in.row_inv[m * rows + row];
+      row_inv[k] = JOINS ? row_invs[row - r0] : in.row_inv[m * rows + row];
       s[k] = row_scale != nullptr ? row_scale[m * rows + row] : 1.f;
     }
     uint32_t down[4][8];
@@ -561,17 +607,26 @@ hipError_t quantize_grad_typed(const Extent& n, const DropArgs& key, const View&
   const bool none = n.rows == 0 || n.cols == 0;  // (scales and sums are 0 then)
   if (!none) grad_stats_kernel<T, NARROW><<<dim3(tiles * chunks, n.workers), kBlock, 0, s>>>(n.rows, n.cols, tiles, chunks, each, dy, col_scale, row_scale, g);
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-  const uint32_t row_blocks = (uint32_t)((n.rows + kBlock - 1) / kBlock), col_blocks = (uint32_t)((n.cols + kBlock - 1) / kBlock);
-  grad_finish_kernel<<<dim3(row_blocks + col_blocks, n.workers), kBlock, 0, s>>>(n.rows, n.cols, tiles, chunks, row_blocks, g, q_scale,
-                                                                                 qt_scale, col_sum);
-  if (hipError_t e = hipGetLastError(); e != hipSuccess || none) return e;
+  const GradResults out{q_scale, qt_scale, col_sum};
   const uint32_t across = (uint32_t)((n.cols + kTile - 1) / kTile);
-  if (n.workers * across * ((n.rows + 127) / 128) >= 256)
-    grad_codes_kernel<T, NARROW, 2><<<dim3(across, (uint32_t)((n.rows + 127) / 128), n.workers), kBlock, 0, s>>>(
-        n.rows, n.cols, key, dy, col_scale, row_scale, g, q, qt);
+  const uint64_t halves = (n.rows + 127) / 128 * across * n.workers >= 1024 ? 2 : 1, down = (n.rows + halves * 64 - 1) / (halves * 64);
+  // (a step of 3 x 111 tokens, 1003 channels 48 -> 45 us; of 4 x 2048, 8192 the pieces would be read 4096 times)
+  const bool joins = !none && down * across * n.workers <= 1024 && tiles <= 32 && chunks <= 64;
+  if (!joins) {
+    const uint32_t row_blocks = (uint32_t)((n.rows + kBlock - 1) / kBlock), col_blocks = (uint32_t)((n.cols + kBlock - 1) / kBlock);
+    grad_finish_kernel<<<dim3(row_blocks + col_blocks, n.workers), kBlock, 0, s>>>(n.rows, n.cols, tiles, chunks, row_blocks, g, out);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess || none) return e;
+  }
+  auto launch = [&](auto half_count, auto joining) {
+    grad_codes_kernel<T, NARROW, half_count, joining><<<dim3(across, (uint32_t)down, n.workers), kBlock, 0, s>>>(
+        n.rows, n.cols, key, dy, col_scale, row_scale, g, out, tiles, chunks, q, qt);
+  };
+  if (halves == 2)
+    launch(std::integral_constant<int, 2>{}, std::false_type{});
+  else if (joins)
+    launch(std::integral_constant<int, 1>{}, std::true_type{});
   else
-    grad_codes_kernel<T, NARROW, 1><<<dim3(across, (uint32_t)((n.rows + 63) / 64), n.workers), kBlock, 0, s>>>(n.rows, n.cols, key, dy, col_scale,
-                                                                                                          row_scale, g, q, qt);
+    launch(std::integral_constant<int, 1>{}, std::false_type{});
   return hipGetLastError();
 }
 
