@@ -273,6 +273,27 @@ def test_products_of_several_workers(M, T, N, K):
         assert (out[:, :11] == 7).all() and (out[:, 11 + T * N:] == 7).all()
 
 
+@pytest.mark.parametrize("M,T,N,K", [(1, 4100, 4000, 130), (1, 8200, 4200, 257), (3, 2900, 2000, 128), (1, 2100, 3000, 700), (1, 700, 3000, 1111),
+                                     (1, 1000, 1000, 513), (4, 300, 700, 64), (1, 2048, 2048, 140000)])
+def test_products_of_many_tiles(M, T, N, K):
+    """Every kind of tile, whole and not, several for a workgroup, with and without what goes back through dropout."""
+    say(f"layer calls: product of {M} x {T} x {N} x {K} codes")
+    a, b = random_codes((M, T, K), 46), random_codes((N, K) if M == 1 else (M, N, K), 47)
+    sa, sb = torch.rand((M, T), generator=gen(48), device=DEV) * 1e-3, torch.rand(b.shape[:-1], generator=gen(49), device=DEV) * 1e-3
+    bias = normal((N,), torch.float32, 50)
+    want = torch.stack([a[m].double() @ (b if M == 1 else b[m]).double().t() for m in range(M)])  # (whole numbers below 2^53)
+    want = (want * sa[..., None].double() * (sb if M == 1 else sb[:, None, :]).double()).cpu().numpy()
+    for dtype in TYPES:
+        got = lowbit.matmul_i8(held(a), held(b), sa, sb, bias, dtype=dtype)
+        assert product_close(got, want + host(bias).astype(np.float64), sa, sb, bias, dtype), dtype
+        x = normal((M, T, N), dtype, 51)
+        d = lowbit.Drop(2, 3, 4, 0.25, True)
+        keep = torch.from_numpy(L.kept(2, 3, 4, 0.25, (M, T, N))).to(DEV) & ~(x <= 0)
+        got = lowbit.matmul_i8(held(a), held(b), sa, sb, dtype=dtype, drop=d, x=x)
+        assert not got[~keep].any()
+        assert product_close(got, np.where(keep.cpu().numpy(), want * float(L.over_keep(0.25)), 0.0), sa, sb, None, dtype, extra=1), dtype
+
+
 @pytest.mark.parametrize("T,N,K", [(2, 3, 140000), (1, 40, 300001), (130, 70, 131072), (20, 257, 65537), (300, 300, 20000)])
 def test_deep_products(T, N, K):
     """All codes at the end of the range: the sum leaves 32 bits."""
