@@ -45,7 +45,7 @@ tng::DropArgs drop_args(const tng_drop& d, uint32_t stream) {
   a.k1 = (uint32_t)(d.seed >> 32);
   a.iter = d.iter;
   a.word = stream | d.site << 8;
-  a.threshold = (uint32_t)std::ceil((double)d.p * 0x1p24);
+  a.threshold = (uint32_t)std::ceil((double)d.p * 0x1p24) << 8;  // (below 2^24: p is below 1)
   a.scale = (float)(1.0 / (1.0 - (double)d.p));
   a.relu = d.relu;
   return a;

@@ -71,7 +71,7 @@ __device__ __forceinline__ void draw_n(uint64_t e, bool aligned, uint32_t worker
   }
 }
 
-__device__ __forceinline__ bool kept(uint32_t word, const DropArgs& d) { return (word >> 8) >= d.threshold; }
+__device__ __forceinline__ bool kept(uint32_t word, const DropArgs& d) { return word >= d.threshold; }
 
 // relu that lets NaN through.
 __device__ __forceinline__ float relu(float x) { return x < 0.f ? 0.f : x; }

@@ -21,7 +21,7 @@ struct View {
 
 struct DropArgs {
   uint32_t k0, k1, iter, word;  // key; counter words 2 and 3
-  uint32_t threshold;           // ceil(p 2^24): an element is kept if its 24-bit draw is no less; 0: nothing is drawn
+  uint32_t threshold;           // ceil(p 2^24) 2^8: an element is kept if its word is no less, which says the same of its 24-bit draw; 0: nothing is drawn
   float scale;                  // 1 / (1 - p)
   int relu;
 };

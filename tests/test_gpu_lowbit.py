@@ -81,6 +81,17 @@ def test_dropout(shape, dtype):
                 assert same(lowbit.dropout_grad(g, d), want)
 
 
+def test_dropout_of_more_than_the_caches_hold():
+    shape = (2, 2100, 4099)
+    say("layer calls: dropout of 2 x 2100 x 4099")
+    x, res = normal(shape, torch.bfloat16, 8), normal(shape, torch.bfloat16, 9)
+    d = lowbit.Drop(3, 1, 4, 0.3, True)
+    keep = L.kept(3, 1, 4, 0.3, shape)
+    assert same(lowbit.dropout(x, d, res), rounded(L.dropout(host(x), keep, 0.3, True, host(res)), torch.bfloat16))
+    assert same(lowbit.dropout(x, d), rounded(L.dropout(host(x), keep, 0.3, True), torch.bfloat16))
+    assert same(lowbit.dropout_grad(res, d, x), rounded(L.dropout_grad(host(res), keep, 0.3, True, host(x)), torch.bfloat16))
+
+
 def test_dropout_of_one_worker_in_place_and_broadcast():
     x = normal((40, 66), torch.bfloat16, 4)
     d = lowbit.Drop(1, 2, 3, 0.3)
