@@ -340,7 +340,8 @@ tng_status tng_quantize_grad(void* hip_stream, const tng_drop* key, const tng_ma
  * scales that are NULL are 1, bias NULL is 0.  rows, channels <= 2^22, workers * rows <= 2^23, depth <= 2^22.
  * drop, x: NULL, or the gradient of what stood in front of the layer: y is then multiplied by keep f'(x) / (1 - p), with x of y's
  * type and size as in tng_dropout_grad.
- * Rows of a and b that begin 16-byte aligned (data, and ld and pitch multiples of 16) take the fast kernels. */
+ * Rows of a and b that begin 16-byte aligned (data, and ld and pitch multiples of 16, ld < 2^23) take the fast kernels.  Those read a row to the
+ * end of its last 16-byte piece; what lies there does not matter. */
 size_t tng_matmul_i8_bytes(const tng_matrix* a, const tng_matrix* b, const tng_matrix* y);
 tng_status tng_matmul_i8(void* hip_stream, const tng_matrix* a, const float* a_scale, const tng_matrix* b, const float* b_scale,
                          const float* bias, const tng_drop* drop, const tng_matrix* x, const tng_matrix* y, void* workspace,

@@ -3,7 +3,8 @@ iteration runs in the HIP kernels of the library; torch tensors are used as devi
 a training loop are marshalled by a native function (csrc/tng_call.cpp) where their arguments are plain.
 
 The module-level functions carry the names of the C entry points and take a context handle
-plus torch CUDA tensors; `Context` owns the workspace and keeps problem data alive.
+plus torch CUDA tensors; `Context` owns the workspace and keeps problem data alive.  The calls on layers, which need no
+context, are in lowbit.py.
 There is no fallback for the library: if it has not been built, loading raises.  Without the native function, or with one that
 was built for another torch or Python, the calls all go through ctypes.
 """
@@ -70,17 +71,22 @@ def _through_ctypes(*_):
     return None
 
 
-def _load_call(name="call"):
-    """A function of the built extension; _through_ctypes where there is none that fits this torch and Python."""
+def _load_extension():
+    """The built extension; None where there is none that fits this torch and Python."""
     if not os.path.exists(CALL_PATH):
-        return _through_ctypes
+        return None
     try:
         loader = importlib.machinery.ExtensionFileLoader("tng_call", CALL_PATH)
         module = importlib.util.module_from_spec(importlib.util.spec_from_loader("tng_call", loader))
         loader.exec_module(module)
     except ImportError:
-        return _through_ctypes
-    return getattr(module, name) if getattr(module, "built_for", None) == build.call_target() else _through_ctypes
+        return None
+    return module if getattr(module, "built_for", None) == build.call_target() else None
+
+
+def _load_call():
+    """tng_call.call of the extension, or _through_ctypes."""
+    return getattr(_load_extension(), "call", _through_ctypes)
 
 
 def lib() -> ctypes.CDLL:
@@ -136,7 +142,9 @@ def lib() -> ctypes.CDLL:
         for name, argtypes in sigs.items():
             fn = getattr(L, name)
             fn.restype, fn.argtypes = ctypes.c_int, argtypes
-        _call, _layer, _linear, _linear_grad = (_load_call(name) for name in ("call", "layer", "linear", "linear_grad"))
+        extension = _load_extension()
+        _call, _layer, _linear, _linear_grad = (getattr(extension, name, _through_ctypes)
+                                                for name in ("call", "layer", "linear", "linear_grad"))
         _address = {name: ctypes.cast(getattr(L, name), vp).value
                     for name in ("tng_local_grad", "tng_normalize_encode", "tng_decode_aggregate", "tng_update_reference",
                                  "tng_step", "tng_dropout", "tng_dropout_grad", "tng_quantize_rows", "tng_quantize_grad",

@@ -454,6 +454,29 @@ def test_calls_are_ordered_on_the_current_stream_and_replay_from_a_graph():
             assert all(torch.equal(u, v) for u, v in zip(held_out, want if k != 1 else other)), f"replay {k}"
 
 
+def test_calls_through_ctypes_are_the_same(monkeypatch):
+    x, dy = normal((2, 37, 90), torch.bfloat16, 98), normal((2, 37, 50), torch.bfloat16, 99)
+    w = lowbit.weight(normal((50, 90), torch.float32, 100))
+    bias = normal((50,), torch.float32, 101)
+    drop = lowbit.Drop(1, 2, 3, 0.1, True)
+
+    def everything():
+        y, saved = lowbit.linear(x, w, bias, drop, keep=True)
+        out = torch.zeros((2, 50, 90), device=DEV)
+        return (y, *lowbit.linear_grad(dy, saved, w, seed=1, iter=2, site=3, out=out), out, lowbit.linear(x, w, bias), lowbit.linear(x[0, :3], w),
+                lowbit.dropout(x, drop, x), lowbit.dropout_grad(x, drop, x), *lowbit.quantize_rows(x, drop, True),
+                *lowbit.quantize_grad(dy, w.scale, seed=4, iter=5, site=6))
+
+    want = everything()
+    plain = lowbit.Drop(1, 2, 3, 0.0)
+    zero = lowbit.dropout(x, plain), lowbit.dropout(x, plain._replace(p=0, relu=0)), lowbit.dropout(x, (1, 2, 3, 0.0, False))
+    assert torch.equal(zero[0], x) and torch.equal(zero[1], x) and torch.equal(zero[2], x)
+    for name in ("_layer", "_linear", "_linear_grad"):
+        assert getattr(B, name) is not B._through_ctypes  # (built here)
+        monkeypatch.setattr(B, name, B._through_ctypes)
+    assert all(torch.equal(u, v) for u, v in zip(everything(), want))
+
+
 def test_strides_that_pass_32_bits():
     rows, cols, ld = 5, 300, 1 << 30
     say("layer calls: rows 2^30 elements apart")
