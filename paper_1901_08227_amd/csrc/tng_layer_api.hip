@@ -203,7 +203,7 @@ tng_status tng_linear_i8(void* hip_stream, const tng_drop* drop, const tng_matri
   if (!aligned(b_scale, 4) || !aligned(bias, 4)) return TNG_ERR_INVALID_ARG;
   if (empty(*y)) return TNG_OK;
   if (workspace == nullptr || !aligned(workspace, 256) || workspace_bytes < l.bytes) return TNG_ERR_WORKSPACE;
-  if (drop == nullptr && tng::coded_product_applies(l.product)) {
+  if (drop == nullptr && tng::coded_product_applies(l.product, view(x))) {
     l.product.b_scale = b_scale;
     l.product.bias = bias;
     return hip_status(tng::launch_coded_product(l.product, view(x), static_cast<hipStream_t>(hip_stream)));

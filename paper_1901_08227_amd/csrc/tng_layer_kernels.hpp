@@ -64,7 +64,7 @@ struct Product {
 size_t product_scratch_bytes(const Product& p);
 hipError_t launch_product(const Product& p, void* scratch, hipStream_t s);
 // The same with rows of a that are the codes of x (of y's type), which the kernel makes itself; a and a_scale are not looked at.
-bool coded_product_applies(const Product& p);
+bool coded_product_applies(const Product& p, const View& x);
 hipError_t launch_coded_product(const Product& p, const View& x, hipStream_t s);
 
 }  // namespace tng

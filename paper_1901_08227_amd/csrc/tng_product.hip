@@ -611,9 +611,8 @@ __global__ void __launch_bounds__(kFewWaves* kWave) product_few_kernel(Task p) {
 }
 
 // ---- Few rows that are not coded yet: every workgroup codes them itself, into LDS, while its first codes of b are on their way, and the
-// second launch with its rows of codes in between is saved (one token, 4096 -> 4096 bfloat16: 7.8 us become 5.9).  The eight wavefronts
-// share the rows: 8 / `spread` of them each.
-constexpr int kCodedRows = 8;
+// second launch with its rows of codes in between is saved.  The eight wavefronts share the rows: 8 / `spread` of them each.
+constexpr int kCodedRows = 4;
 constexpr uint32_t kCodedBytes = 40 * 1024;  // of the codes in LDS
 
 inline uint32_t coded_pitch(uint64_t depth) { return (uint32_t)((depth + kFewStep - 1) / kFewStep * kFewStep + 16); }  // 16 rows, 64 banks
@@ -936,6 +935,13 @@ Product joined(Product p) {
   return p;
 }
 
+// x in the place of a, all workers' rows together where they share b.
+Product coded_rows(const Product& p, const View& x) {
+  Product c = p;
+  c.a = x;
+  return joined(c);
+}
+
 }  // namespace
 
 size_t product_scratch_bytes(const Product& given) {
@@ -953,19 +959,26 @@ hipError_t launch_product(const Product& given, void* scratch, hipStream_t s) {
   }
 }
 
-bool coded_product_applies(const Product& p) {
-  const bool aligned = reinterpret_cast<uintptr_t>(p.b.p) % 16 == 0 && p.b.ld % 16 == 0 && p.b.pitch % 16 == 0 && p.b.ld < (1u << 23);
-  return aligned && p.rows <= kCodedRows && p.depth >= 8 && p.depth <= kMaxDepth && p.rows * coded_pitch(p.depth) <= kCodedBytes;
+// Every workgroup reads and codes the rows again, so few of both.  Measured, us, with / without (a launch to code, a launch of
+// product_few_kernel), bfloat16: 1 row 4096 -> 4096 5.1 / 6.8, 4096 -> 16384 14.0 / 14.4, 8192 -> 8192 14.7 / 15.7; 4 rows 7.0 / 7.7,
+// 16.4 / 14.9, 18.6 / 16.6; 8 rows of 4096 -> 4096 9.3 / 8.0.
+bool coded_product_applies(const Product& p, const View& x) {
+  const Product c = coded_rows(p, x);
+  const bool aligned = reinterpret_cast<uintptr_t>(c.b.p) % 16 == 0 && c.b.ld % 16 == 0 && c.b.pitch % 16 == 0 && c.b.ld < (1u << 23);
+  const bool shared = c.workers > 1 && c.b.pitch == 0;  // (by rows that do not lie together)
+  const bool few = c.rows == 1 || (c.rows <= kCodedRows && c.rows * c.depth <= 16384 && over(c.channels, 16) * c.workers <= 512);
+  return aligned && !shared && few && c.depth >= 8 && c.depth <= kMaxDepth && c.rows * coded_pitch(c.depth) <= kCodedBytes;
 }
 
-hipError_t launch_coded_product(const Product& p, const View& x, hipStream_t s) {
+hipError_t launch_coded_product(const Product& given, const View& x, hipStream_t s) {
+  const Product p = coded_rows(given, x);
   const Task t = task_of(p);
   uint32_t spread = kFewWaves;
   while (spread * p.rows > kFewWaves) spread /= 2;
   const uint32_t pitch = coded_pitch(p.depth);
   auto launch = [&](auto type, auto tiles) {
     product_coded_kernel<decltype(type), tiles><<<dim3((uint32_t)over(p.channels, tiles * 16), p.workers), kFewWaves * kWave, p.rows * pitch, s>>>(
-        t, x, spread, pitch);
+        t, p.a, spread, pitch);
   };
   auto typed = [&](auto tiles) {
     switch (p.type) {

@@ -388,6 +388,24 @@ def test_few_rows_in_one_call_are_the_two_calls(M, T, K, N, dtype):
                 assert same(lowbit.linear(a[0], w, b), want[0].cpu())
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("M,T", [(2, 1), (4, 1), (2, 2), (1, 4), (8, 1), (3, 4)])
+@pytest.mark.parametrize("K,N", [(8, 16), (100, 50), (1000, 9000), (4100, 130)])
+def test_few_rows_of_several_workers(M, T, K, N, dtype):
+    x = normal((M, T, K), dtype, 81)
+    x[-1, 0] = 0.0
+    one = lowbit.weight(normal((N, K), torch.float32, 82), turned=False)
+    own = lowbit.weight(normal((M, N, K), torch.float32, 83), turned=False)
+    bias = normal((N,), torch.float32, 84)
+    for a in (x, spread(x, 0), x[:1].expand(M, T, K)):
+        q, s = lowbit.quantize_rows(a)
+        for w in (one, own):
+            want = lowbit.matmul_i8(q, w.q, s, w.scale, bias, dtype=dtype)
+            assert same(lowbit.linear(a, w, bias), want.cpu())
+            each = [lowbit.linear(a[m], lowbit.Weight(w.q[m], w.scale[m], None) if w is own else w, bias) for m in range(M)]
+            assert same(torch.stack(each), want.cpu())
+
+
 def test_one_worker_without_a_leading_dimension_is_the_same():
     x, dy = normal((1, 37, 130), torch.bfloat16, 75), normal((1, 37, 65), torch.bfloat16, 76)
     w = lowbit.weight(normal((65, 130), torch.float32, 77))
