@@ -532,7 +532,7 @@ __global__ void __launch_bounds__(CW* TW* kWave) product_tile_kernel(Task p) {
 // they read whole runs of a row) straight into registers, and their sums meet in LDS.  A lane takes 32 bytes of a row, the operands
 // of two matrix instructions: which codes meet in one of them does not matter as long as it is the same ones of both sides.
 constexpr int kFewWaves = 8, kFewRows = 64, kFewStep = 128;
-constexpr uint64_t kFewDepth = kFewWaves * kMaxDepth;
+constexpr uint64_t kFewDepth = 16384, kFewCodes = 3 << 16;
 
 template <typename T, int CN, int TN>
 __global__ void __launch_bounds__(kFewWaves* kWave) product_few_kernel(Task p) {
@@ -765,7 +765,7 @@ bool pieces_aligned(const Product& p) {
   return fits(p.a) && fits(p.b);
 }
 
-enum class Way { kAny, kFew, kNarrowTiles, kSmallTiles, kLargeTiles };
+enum class Way { kAny, kFew, kFlatTiles, kNarrowTiles, kSmallTiles, kLargeTiles };
 
 struct Plan {
   Way way;
@@ -782,14 +782,16 @@ uint64_t part_pitch(const Product& p) { return over(p.channels, 8) * 8; }  // (r
 // beside its stages (first loads, scaling, writing); joining splits takes 5 and their bytes at 4 TB/s.  All sides, us, tokens x channels x depth,
 // narrow (64 channels x 128 tokens) / small (128 x 128) / large tiles (256 x 256): 333 x 1003 x 1000 6.9 / 8.7 / 12; 200 x 8192 x 5000 22.7 / 26 / 58;
 // 1024 x 1024 x 8192 24.4 / 31.7 / 75; 2048 x 2048 x 2048 18.6 / 14.7 / 26.7; 8192 x 8192 x 1024 166 / 134 / 94; 8192 x 8192 x 8192 - / 585 /
-// 407; one / two splits of the small: 1024 x 1024 x 8192 31 / 25; 4096 x 512 x 4096 19.8 / 24.6.
+// 407; one / two splits of the small: 1024 x 1024 x 8192 31 / 25; 4096 x 512 x 4096 19.8 / 24.6.  Flat tiles (128 x 64) against narrow: 64 x 16384 x
+// 4096 14.3 / 16.5; 64 x 32768 x 512 5.7 / 6.6; 129 x 8192 x 8192 23.5 / 27.1.
 void by_tiles(const Product& p, Plan* plan) {
   struct Kind {
     Way way;
     uint64_t tokens, channels;
     double stage, busy_stage, tile;
   };
-  constexpr Kind kinds[] = {{Way::kNarrowTiles, 128, 64, 0.30, 0.17, 3.0}, {Way::kSmallTiles, 128, 128, 0.43, 0.19, 3.0}, {Way::kLargeTiles, 256, 256, 1.2, 0.4, 8.0}};
+  constexpr Kind kinds[] = {{Way::kNarrowTiles, 128, 64, 0.30, 0.17, 3.0}, {Way::kFlatTiles, 64, 128, 0.30, 0.17, 3.0},
+                            {Way::kSmallTiles, 128, 128, 0.43, 0.19, 3.0}, {Way::kLargeTiles, 256, 256, 1.2, 0.4, 8.0}};
   constexpr double kCus = 256.0;
   const uint32_t least = plan->splits;  // that keep the sums inside 32 bits
   double best = 0.0;
@@ -810,12 +812,21 @@ void by_tiles(const Product& p, Plan* plan) {
   }
 }
 
+// The kernel for few rows takes time with its rows and the depth, tiles hardly with the rows.  Measured, us, few / tiles, rows x channels x depth:
+// 1 x 4096 x 16384 15.4 / 18.9; 16 x 512 x 8192 8.9 / 10.2; 16 x 512 x 16384 15.9 / 12.3; 48 x 8192 x 4096 12.3 / 12.9; 64 x 4096 x 1024
+// 4.9 / 6.0; 64 x 512 x 4096 11.1 / 9.2; 32 x 8192 x 8192 17.9 / 18.3; 48 x 8192 x 8192 21.3 / 19.1; 32 x 16384 x 4096 17.5 / 13.5; 16 x
+// 16384 x 4096 13.6 / 13.1.
+bool few_is_sooner(const Product& p) {
+  const uint64_t groups = over(p.channels, 16) * p.workers;
+  return p.rows <= kFewRows && p.depth <= kFewDepth && p.rows * p.depth <= kFewCodes && (p.rows <= 16 || groups <= (p.rows <= 48 ? 512 : 256));
+}
+
 Plan plan_of(const Product& p) {
   Plan plan{};
   plan.splits = (uint32_t)std::max<uint64_t>(over(p.depth, kMaxDepth), 1);
   if (!pieces_aligned(p) || p.depth == 0) {
     plan.way = Way::kAny;
-  } else if (p.rows <= kFewRows && p.depth <= kFewDepth) {
+  } else if (few_is_sooner(p)) {
     plan.way = Way::kFew;
     plan.splits = 1;
   } else {
@@ -844,21 +855,17 @@ void launch_tiles(const Task& t, hipStream_t s) {
   }
 }
 
-// Codes of a are read again by every workgroup: two or four tiles of channels each, where that leaves a workgroup for every CU.
-// Measured, us, one / two / four tiles (depth 8192 but for the last): 1 token, 8192 channels 13.2 / 15.3 / 19.0; 1, 16384 13.4 / 12.3 /
-// 13.0; 16, 8192 17.7 / 14.2 / 21.5; 64, 8192 39.4 / 27.6 / 36.1; 64 tokens, 16384 channels, depth 2048 23.6 / 18.7 / 14.6.
+// Codes of a are read again by every workgroup: two tiles of channels each, where that leaves a workgroup for every CU.
+// Measured, us, one / two tiles (depth 8192): 1 token, 8192 channels 13.2 / 15.3; 1, 16384 13.4 / 12.3; 16, 8192 17.7 / 14.2; 64, 8192 39.4 / 27.6.
 template <typename T, int TN>
 void launch_few(const Task& t, hipStream_t s) {
-  auto groups = [&](int tiles) { return over(t.channels, tiles * 16) * t.workers; };
   auto launch = [&](auto tiles) {
     product_few_kernel<T, tiles, TN><<<dim3((uint32_t)over(t.channels, tiles * 16), t.workers), kFewWaves * kWave, 0, s>>>(t);
   };
-  if (TN > 2 && groups(4) >= 256)
-    launch(std::integral_constant<int, 4>{});
-  else if (groups(2) >= (t.rows > 4 ? 256 : 512))
-    launch(std::integral_constant<int, 2>{});
-  else
-    launch(std::integral_constant<int, 1>{});
+  if constexpr (TN <= 3) {  // (more rows: few_is_sooner has less channels)
+    if (over(t.channels, 32) * t.workers >= (t.rows > 4 ? 256 : 512)) return launch(std::integral_constant<int, 2>{});
+  }
+  launch(std::integral_constant<int, 1>{});
 }
 
 Task task_of(const Product& p) {
@@ -902,6 +909,7 @@ hipError_t product_typed(const Product& p, void* scratch, hipStream_t s) {
       else
         launch_few<T, 4>(t, s);
       break;
+    case Way::kFlatTiles: launch_tiles<T, 2, 2, 4, 2, 4>(t, s); break;
     case Way::kNarrowTiles: launch_tiles<T, 2, 2, 2, 4, 4>(t, s); break;
     case Way::kSmallTiles:
       // More tiles than CUs: two stages each and two workgroups a CU, one writes while the other multiplies (8 x 1024 x 1024 x 512 16.8 -> 14.0 us);

@@ -305,6 +305,13 @@ def test_products_of_many_tiles(M, T, N, K):
         assert product_close(got, np.where(keep.cpu().numpy(), want * float(L.over_keep(0.25)), 0.0), sa, sb, None, dtype, extra=1), dtype
 
 
+@pytest.mark.parametrize("M,T,N,K", [(1, 17, 8300, 200), (1, 33, 300, 9000), (1, 64, 16400, 130), (1, 60, 33000, 70), (1, 129, 8200, 1000), (1, 16, 100, 16500),
+                                     (2, 40, 5000, 1003), (1, 49, 4100, 333), (1, 5, 8200, 300), (3, 30, 2730, 520)])
+def test_products_of_few_rows(M, T, N, K):
+    """The kernel for few rows, one tile of channels and two, and the tiles that take over from it."""
+    test_products_of_many_tiles(M, T, N, K)
+
+
 @pytest.mark.parametrize("T,N,K", [(2, 3, 140000), (1, 40, 300001), (130, 70, 131072), (20, 257, 65537), (300, 300, 20000)])
 def test_deep_products(T, N, K):
     """All codes at the end of the range: the sum leaves 32 bits."""
