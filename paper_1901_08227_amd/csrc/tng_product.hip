@@ -474,11 +474,15 @@ __global__ void __launch_bounds__(CW* TW* kWave) product_tile_kernel(Task p) {
   if (tile >= run.end) return;
   Spot s = spot_of<K>(p, tile, across, down);
   begin(s, 0);
+  // The first tile waits for its first stage only (what is asked for behind the stages makes it wait for a little more); large tiles have no
+  // registers for a second kind of wait.  48 x 8192 x 8192 18.8 -> 18.1 us.
+  constexpr bool kShortWait = CN <= 4;
+  if (kShortWait) wait_and_meet<(SLOTS - 1) * K::kLoads>();
   for (;;) {
     const uint32_t stages = (s.depth + kDepth - 1) / kDepth;
     const int left = (int)(s.depth - (stages - 1) * kDepth);
     const bool ragged = left < kDepth;
-    wait_and_meet<0>();
+    if (!kShortWait) wait_and_meet<0>();
     uint32_t slot = 0;
 #pragma unroll
     for (int b = 0; b < TN; ++b) read_t(0, b, 0);
@@ -523,6 +527,7 @@ __global__ void __launch_bounds__(CW* TW* kWave) product_tile_kernel(Task p) {
     write_tile<K, T, END, CN, TN>(p, done, sum, cw, tw, lane, reinterpret_cast<const float*>(lds + K::kRing + parity * K::kFactorBytes));
     if (!more) break;
     parity ^= 1u;
+    if (kShortWait) wait_and_meet<0>();
   }
 }
 
