@@ -108,7 +108,9 @@ __device__ __forceinline__ void place_in_plane(uint32_t tile, uint32_t across, u
   *n = in / high;
 }
 
-// Any alignment, any size: 64 x 64 results for a workgroup, 32 x 32 for each of its wavefronts, 64 codes deep at a time through LDS.
+// Any alignment, any size: 64 x 64 results for a workgroup, 32 x 32 for each of its wavefronts, 64 codes deep at a time through LDS, and through
+// registers on the way there (loads that go to LDS directly want aligned rows).  That way bounds it: 2048 x 2048 x 2047 45 us (0.38 POP/s; 14
+// where rows are 2048 apart), 200 x 8192 x 5000 from an odd address 55 (the next 64 codes under way meanwhile; 63 without).
 constexpr int kAnyTile = 64, kAnyDepth = 64;
 
 // Codes k .. k + 15 of a row, 0 past `end`.
@@ -139,12 +141,14 @@ __global__ void __launch_bounds__(kBlock) product_any_kernel(Task p) {
   const int8_t* a = static_cast<const int8_t*>(p.a.p) + m * p.a.pitch + min(t0 + row, p.rows - 1) * p.a.ld;
   const int8_t* b = static_cast<const int8_t*>(p.b.p) + m * p.b.pitch + min(n0 + row, p.channels - 1) * p.b.ld;
   v4i sum[2][2] = {};
+  v4i va = load16_any(a, begin + piece * 16, end), vb = load16_any(b, begin + piece * 16, end);
   for (uint64_t k = begin; k < end; k += kAnyDepth) {
-    const v4i va = load16_any(a, k + piece * 16, end), vb = load16_any(b, k + piece * 16, end);
     __syncthreads();
     *reinterpret_cast<v4i*>(tile_a + row * kPitch + piece * 16) = va;
     *reinterpret_cast<v4i*>(tile_b + row * kPitch + piece * 16) = vb;
     __syncthreads();
+    va = load16_any(a, k + kAnyDepth + piece * 16, end);  // (the next 64, under way while these are multiplied)
+    vb = load16_any(b, k + kAnyDepth + piece * 16, end);
     // the channels are the rows of the unit's result: a lane holds four of them, one after another, of one token
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -182,6 +186,12 @@ __global__ void __launch_bounds__(kBlock) product_any_kernel(Task p) {
 //   last groups of stage k           | read the beginning of stage k + 1; ask for stage k + SLOTS, in the place of stage k
 //
 // A workgroup takes tiles until there are no more, and asks for the next tile's first stages before it scales and writes a tile.
+//
+// What bounds it: of large tiles (256 x 256: 128 operations for each byte that comes from a cache) the matrix units, at the clock that
+// their power leaves.  8192 x 8192 x 8192 takes 406 us, 2.7 POP/s; the same instructions on registers alone reach 4.1 on random codes and 4.8 on
+// zeros.  Of small ones what the dies' caches hand to the CUs (some 13 TB/s: 2048 x 2048 x 2048 13 us), and of few the latency of a
+// stage.  Stages of 128 codes are whole lines of memory (rings of 64-code stages: 8192^3 in 550 us), eight wavefronts leave each 128 x 64
+// results (four of 128 x 128: 516), a load after each group keeps the memory and the matrix units busy together (two at a time: 501).
 constexpr int kDepth = 128;  // bytes of a stage's rows: eight 16-byte pieces
 
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
@@ -531,7 +541,7 @@ __global__ void __launch_bounds__(CW* TW* kWave) product_tile_kernel(Task p) {
   }
 }
 
-// ---- Few rows of a: the codes of b pass once, and that is the time.
+// ---- Few rows of a: the codes of b pass once, and that is the time (1 x 8192 x 8192 12.7 us, 5.3 TB/s; 1 x 4096 x 4096 4.3).
 //
 // A workgroup makes all tokens' results of CN x 16 channels; its eight wavefronts take 128 codes of depth each in turn (so that together
 // they read whole runs of a row) straight into registers, and their sums meet in LDS.  A lane takes 32 bytes of a row, the operands
@@ -730,7 +740,7 @@ __global__ void __launch_bounds__(kFewWaves* kWave) product_coded_kernel(Task p,
   }
 }
 
-// The splits' sums joined, four channels a lane.
+// The splits' sums joined, four channels a lane: a launch's latency and their bytes (48 x 8192 4 us).
 template <typename T>
 __global__ void __launch_bounds__(kBlock) product_join_kernel(Task p) {
   const uint32_t m = blockIdx.y, each = p.part_pitch / 4;
