@@ -53,8 +53,10 @@ tng::DropArgs drop_args(const tng_drop& d, uint32_t stream) {
 
 tng::View view(const tng_matrix* a) {
   if (a == nullptr) return tng::View{nullptr, 0, 0};
-  // strides that no index reaches are made what a matrix without gaps has
-  const uint64_t ld = a->rows > 1 ? a->ld : a->cols;
+  // Strides that no index reaches are made what suits the products: single rows of several workers lie as one worker's rows do, and one row
+  // by itself begins aligned as its address does.
+  uint64_t ld = a->ld;
+  if (a->rows <= 1) ld = a->workers > 1 && a->pitch < (1u << 23) ? a->pitch : (a->cols + 15) / 16 * 16;
   return tng::View{a->data, ld, a->workers > 1 ? a->pitch : a->rows * ld};
 }
 
