@@ -672,25 +672,31 @@ hipError_t quantize_grad_typed(const Extent& n, const DropArgs& key, const View&
   if (!none) grad_stats_kernel<T, NARROW><<<dim3(tiles * chunks, n.workers), kBlock, 0, s>>>(n.rows, n.cols, tiles, chunks, each, dy, col_scale, row_scale, g);
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   const GradResults out{q_scale, qt_scale, col_sum};
+  // Which kernel codes, and with it who puts the statistics together: from 1024 whole tiles on workgroups of two halves, whose statistics
+  // grad_finish_kernel makes (a step of 4 x 2048 tokens, 8192 channels would read the pieces 4096 times); of fewer, workgroups of one half, that join
+  // few pieces themselves (a step of 3 x 111 tokens, 1003 channels 48 -> 45 us).
+  enum class Codes { kTwoHalves, kOneHalf, kJoining };
   const uint32_t across = (uint32_t)((n.cols + kTile - 1) / kTile);
-  const uint64_t halves = (n.rows + 127) / 128 * across * n.workers >= 1024 ? 2 : 1, down = (n.rows + halves * 64 - 1) / (halves * 64);
-  // (a step of 3 x 111 tokens, 1003 channels 48 -> 45 us; of 4 x 2048, 8192 the pieces would be read 4096 times)
-  const bool joins = !none && down * across * n.workers <= 1024 && tiles <= 32 && chunks <= 64;
-  if (!joins) {
+  auto down = [&](uint64_t halves) { return (n.rows + halves * 64 - 1) / (halves * 64); };
+  Codes codes = Codes::kOneHalf;
+  if (down(2) * across * n.workers >= 1024)
+    codes = Codes::kTwoHalves;
+  else if (!none && down(1) * across * n.workers <= 1024 && tiles <= 32 && chunks <= 64)
+    codes = Codes::kJoining;
+  if (codes != Codes::kJoining) {
     const uint32_t row_blocks = (uint32_t)((n.rows + kBlock - 1) / kBlock), col_blocks = (uint32_t)((n.cols + kBlock - 1) / kBlock);
     grad_finish_kernel<<<dim3(row_blocks + col_blocks, n.workers), kBlock, 0, s>>>(n.rows, n.cols, tiles, chunks, row_blocks, g, out);
     if (hipError_t e = hipGetLastError(); e != hipSuccess || none) return e;
   }
-  auto launch = [&](auto half_count, auto joining) {
-    grad_codes_kernel<T, NARROW, half_count, joining><<<dim3(across, (uint32_t)down, n.workers), kBlock, 0, s>>>(
+  auto launch = [&](auto halves, auto joining) {
+    grad_codes_kernel<T, NARROW, halves, joining><<<dim3(across, (uint32_t)down(halves), n.workers), kBlock, 0, s>>>(
         n.rows, n.cols, key, dy, col_scale, row_scale, g, out, tiles, chunks, q, qt);
   };
-  if (halves == 2)
-    launch(std::integral_constant<int, 2>{}, std::false_type{});
-  else if (joins)
-    launch(std::integral_constant<int, 1>{}, std::true_type{});
-  else
-    launch(std::integral_constant<int, 1>{}, std::false_type{});
+  switch (codes) {
+    case Codes::kTwoHalves: launch(std::integral_constant<int, 2>{}, std::false_type{}); break;
+    case Codes::kOneHalf: launch(std::integral_constant<int, 1>{}, std::false_type{}); break;
+    case Codes::kJoining: launch(std::integral_constant<int, 1>{}, std::true_type{}); break;
+  }
   return hipGetLastError();
 }
 
