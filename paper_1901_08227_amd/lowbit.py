@@ -61,6 +61,11 @@ _CALLS = {
 }
 
 
+def _u32(n):
+    """n as 32 bits; what they do not hold as the largest number, which the library refuses for every field that this is used for."""
+    return n if 0 <= n < 1 << 32 else 0xFFFFFFFF
+
+
 def _matrix(t, dtypes, name):
     """The tng_matrix of a tensor."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
@@ -90,7 +95,7 @@ def _vector(t, n, name):
 
 
 def _drop(d):
-    return B.TngDrop(int(d[0]) & 0xFFFFFFFFFFFFFFFF, int(d[1]) & 0xFFFFFFFF, int(d[2]), float(d[3]), int(bool(d[4])))
+    return B.TngDrop(int(d[0]) & 0xFFFFFFFFFFFFFFFF, int(d[1]) & 0xFFFFFFFF, _u32(int(d[2])), float(d[3]), int(bool(d[4])))
 
 
 def _through_ctypes(name, kinds, names, device, stream, args):

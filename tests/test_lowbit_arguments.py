@@ -1,0 +1,18 @@
+"""What the layer calls' Python side hands to the library where 32 bits do not hold an argument (no GPU needed)."""
+import pytest
+
+from paper_1901_08227_amd import binding as B
+from paper_1901_08227_amd import lowbit
+
+
+def refused(drop, matrix=B.TngMatrix(None, B.TYPE_F32, 1, 0, 1, 1, 0)):
+    """Whether the library refuses them; nothing is ever written: there are no rows."""
+    status = B.lib().tng_dropout(None, drop, matrix, None, matrix)
+    assert status in (B.TNG_OK, B.TNG_ERR_INVALID_ARG)
+    return status == B.TNG_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("site,bad", [(0, False), ((1 << 24) - 1, False), (1 << 24, True), (-1, True), ((1 << 32) - 1, True), (1 << 32, True),
+                                      ((1 << 32) + 3, True), (-(1 << 32) + 3, True), (1 << 80, True)])
+def test_sites_do_not_wrap(site, bad):
+    assert refused(lowbit._drop(lowbit.Drop(1, 2, site, 0.5))) == bad
