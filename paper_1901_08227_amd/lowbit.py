@@ -77,7 +77,7 @@ def _matrix(t, dtypes, name):
     if len(shape) == 2:
         workers, pitch = 1, 0
     elif len(shape) == 3:
-        workers, pitch = shape[0], stride[0]
+        workers, pitch = _u32(shape[0]), stride[0]
     else:
         raise ValueError(f"{name}: expected [rows, cols] or [M, rows, cols], got {tuple(shape)}")
     if stride[-1] != 1 and shape[-1] > 1:

@@ -1,5 +1,6 @@
 """What the layer calls' Python side hands to the library where 32 bits do not hold an argument (no GPU needed)."""
 import pytest
+import torch
 
 from paper_1901_08227_amd import binding as B
 from paper_1901_08227_amd import lowbit
@@ -16,3 +17,16 @@ def refused(drop, matrix=B.TngMatrix(None, B.TYPE_F32, 1, 0, 1, 1, 0)):
                                       ((1 << 32) + 3, True), (-(1 << 32) + 3, True), (1 << 80, True)])
 def test_sites_do_not_wrap(site, bad):
     assert refused(lowbit._drop(lowbit.Drop(1, 2, site, 0.5))) == bad
+
+
+class OnTheGpu(torch.Tensor):
+    """A tensor of the host that says otherwise."""
+    is_cuda = True
+
+
+@pytest.mark.parametrize("workers,bad", [(1, False), (65535, False), (65536, True), ((1 << 32) + 1, True)])
+def test_numbers_of_workers_do_not_wrap(workers, bad):
+    x = torch.zeros((1, 0, 1)).as_subclass(OnTheGpu).expand(workers, 0, 1)
+    matrix = lowbit._matrix(x, lowbit._TYPES, "x")
+    matrix.pitch = 0  # (of no elements)
+    assert refused(lowbit._drop(lowbit.Drop(1, 2, 3, 0.5)), matrix) == bad
