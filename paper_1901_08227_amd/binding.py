@@ -84,9 +84,9 @@ def _load_extension():
     return module if getattr(module, "built_for", None) == build.call_target() else None
 
 
-def _load_call():
-    """tng_call.call of the extension, or _through_ctypes."""
-    return getattr(_load_extension(), "call", _through_ctypes)
+def _load_call(name="call"):
+    """A function of the extension, or _through_ctypes."""
+    return getattr(_load_extension(), name, _through_ctypes)
 
 
 def lib() -> ctypes.CDLL:
@@ -142,9 +142,7 @@ def lib() -> ctypes.CDLL:
         for name, argtypes in sigs.items():
             fn = getattr(L, name)
             fn.restype, fn.argtypes = ctypes.c_int, argtypes
-        extension = _load_extension()
-        _call, _layer, _linear, _linear_grad = (getattr(extension, name, _through_ctypes)
-                                                for name in ("call", "layer", "linear", "linear_grad"))
+        _call, _layer, _linear, _linear_grad = map(_load_call, ("call", "layer", "linear", "linear_grad"))
         _address = {name: ctypes.cast(getattr(L, name), vp).value
                     for name in ("tng_local_grad", "tng_normalize_encode", "tng_decode_aggregate", "tng_update_reference",
                                  "tng_step", "tng_dropout", "tng_dropout_grad", "tng_quantize_rows", "tng_quantize_grad",

@@ -3,7 +3,7 @@ import pytest
 import torch
 
 from paper_1901_08227_amd import binding as B
-from paper_1901_08227_amd import lowbit
+from paper_1901_08227_amd import build, lowbit
 
 
 def refused(drop, matrix=B.TngMatrix(None, B.TYPE_F32, 1, 0, 1, 1, 0)):
@@ -30,3 +30,29 @@ def test_numbers_of_workers_do_not_wrap(workers, bad):
     matrix = lowbit._matrix(x, lowbit._TYPES, "x")
     matrix.pitch = 0  # (of no elements)
     assert refused(lowbit._drop(lowbit.Drop(1, 2, 3, 0.5)), matrix) == bad
+
+
+def test_without_a_native_function_that_fits_layer_calls_go_through_ctypes(monkeypatch, tmp_path):
+    names = ("call", "layer", "linear", "linear_grad")
+    B.lib()
+    built = [getattr(B, "_" + name) for name in names]
+    assert B._through_ctypes not in built and len(set(built)) == 4  # (built here)
+
+    def loaded():
+        """The four as the library's first use would have them."""
+        with monkeypatch.context() as mp:
+            for name in ("_lib", "_address", *("_" + name for name in names)):
+                mp.setattr(B, name, None)
+            B.lib()
+            return [getattr(B, "_" + name) for name in names]
+
+    assert loaded() == built
+    with monkeypatch.context() as mp:  # built for another torch
+        mp.setattr(build, "call_target", lambda: "torch 1.0, cpython-27")
+        assert loaded() == [B._through_ctypes] * 4
+    with monkeypatch.context() as mp:  # no library
+        mp.setattr(B, "CALL_PATH", str(tmp_path / "tng_call.so"))
+        assert loaded() == [B._through_ctypes] * 4
+        (tmp_path / "tng_call.so").write_text("not a library")
+        assert loaded() == [B._through_ctypes] * 4
+    assert loaded() == built
