@@ -1,12 +1,13 @@
-"""The coders at the sizes where another kernel takes over, against the oracle."""
+"""The layer calls at the sizes where another kernel takes over and beyond 32 bits, against the oracle."""
 import numpy as np
 import pytest
 import torch
 
 from gpu_util import DEV, say
 from oracle import lowbit_oracle as L
+from oracle import tng_oracle as O
 from paper_1901_08227_amd import lowbit
-from test_gpu_lowbit import gen, host, normal
+from test_gpu_lowbit import gen, host, normal, product_close, random_codes, rounded, same, spread
 
 pytestmark = pytest.mark.gpu
 
@@ -56,3 +57,86 @@ def test_codes_of_a_gradient_where_another_kernel_takes_over(shape, dtype):
     most = max(rows // 4 - 1 + 3 + -(-T // rows) - 1 for rows in (8, 16, 32, 64))
     d = host(dy).astype(np.float64)
     assert np.all(np.abs(sums.cpu().numpy() - d.sum(1)) <= most * 2.0 ** -24 * 1.001 * np.abs(d).sum(1))
+
+
+# From 1024 rows on a wavefront takes a row and holds 2, 4 or 8 pieces of 512 columns; before, and up to 8192 columns, a workgroup does.
+ROWS = [(1, 1024, 513), (2, 520, 1024), (1, 1030, 1025), (3, 400, 2048), (1, 1024, 2049), (1, 1100, 4096), (1, 1024, 4097), (1, 1023, 1024), (2, 511, 4090)]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("shape", ROWS)
+def test_codes_of_rows_that_a_wavefront_holds(shape, dtype):
+    say(f"layer calls: codes of {shape[0]} x {shape[1]} x {shape[2]}")
+    x = normal(shape, dtype, 131)
+    x[0, 5] = 0.0
+    for drop in (None, lowbit.Drop(3, 4, 5, 0.25, True)):
+        v = host(x)
+        if drop is not None:
+            v = L.dropped(v, L.kept(3, 4, 5, drop.p, shape), drop.p, drop.relu)
+        want, scale = L.codes(v, 2)
+        for a in (x, spread(x, 0)):
+            q, s, qt = lowbit.quantize_rows(a, drop, turned=True)
+            assert np.array_equal(s.cpu().numpy(), scale[..., 0])
+            assert np.array_equal(q.cpu().numpy(), want)
+            assert np.array_equal(qt.cpu().numpy(), np.swapaxes(want, 1, 2))
+
+
+# ---- elements beyond the 32 bits of their number
+
+FAR = ((1 << 20) + 5, 4099)
+LAST = 40  # of the rows that are compared with the oracle
+
+
+def last_words(seed, it, site, stream):
+    rows, cols = FAR
+    return O._draw_words(seed, it, 0, stream | site << 8, (rows - LAST) * cols, LAST * cols).reshape(1, LAST, cols)
+
+
+def test_dropout_of_elements_beyond_32_bits():
+    rows, cols = FAR
+    assert (rows - LAST) * cols >= 1 << 32
+    say("layer calls: dropout of 2^32 elements")
+    d = lowbit.Drop(5, 6, 7, 0.5, True)
+    keep = (last_words(5, 6, 7, L.STREAM_DROPOUT) >> 8) * 2.0 ** -24 >= 0.5
+    row = normal((1, cols), torch.bfloat16, 141)
+    x = row.expand(rows, cols)              # no gaps where it is written, so by rows
+    end = np.repeat(host(row), LAST, 0)[None]
+    want = rounded(L.dropout(end, keep, 0.5, True), torch.bfloat16)[0]
+    by_rows = lowbit.dropout(x, d)
+    assert same(by_rows[-LAST:], want)
+    run = x.contiguous()                    # as one run
+    assert torch.equal(lowbit.dropout(run, d, out=run), by_rows)
+    assert same(lowbit.dropout_grad(by_rows, d, x)[-LAST:], rounded(L.dropout_grad(want[None].float().numpy(), keep, 0.5, True, end), torch.bfloat16)[0])
+
+
+def test_codes_of_elements_beyond_32_bits():
+    rows, cols = FAR
+    say("layer calls: codes of 2^32 elements")
+    row = normal((1, cols), torch.bfloat16, 142)
+    end = np.repeat(host(row), LAST, 0)[None]
+    x = row.expand(rows, cols)
+    q, s = lowbit.quantize_rows(x, lowbit.Drop(5, 6, 7, 0.5, True))
+    want, scale = L.codes(L.dropped(end, (last_words(5, 6, 7, L.STREAM_DROPOUT) >> 8) * 2.0 ** -24 >= 0.5, 0.5, True), 2)
+    assert np.array_equal(q[-LAST:].cpu().numpy(), want[0]) and np.array_equal(s[-LAST:].cpu().numpy(), scale[0, :, 0])
+    del q
+    rs = torch.rand(rows, generator=gen(143), device=DEV) + 0.5
+    rs[-LAST // 2] = 2.0                    # so the columns' largest products are in a row that is compared
+    q, qs, qt, qts, _ = lowbit.quantize_grad(x, None, rs, seed=8, iter=9, site=10, sums=False)
+    w = last_words(8, 9, 10, L.STREAM_ROUNDING)
+    want, scale = L.codes(end, 2, w >> 16)
+    assert np.array_equal(q[-LAST:].cpu().numpy(), want[0]) and np.array_equal(qs[-LAST:].cpu().numpy(), scale[0, :, 0])
+    want, scale = L.codes(end * host(rs)[None, -LAST:, None], 1, w & 0xFFFF)
+    assert np.array_equal(qt[:, -LAST:].cpu().numpy(), want[0].T) and np.array_equal(qts.cpu().numpy(), scale[0, 0])
+
+
+def test_results_beyond_32_bits():
+    rows, cols = FAR
+    say("layer calls: a product of 2^32 results")
+    a, b = random_codes((rows, 16), 144), random_codes((cols, 16), 145)
+    x = normal((1, cols), torch.bfloat16, 146).expand(rows, cols)
+    d = lowbit.Drop(5, 6, 7, 0.5, True)
+    keep = ((last_words(5, 6, 7, L.STREAM_DROPOUT) >> 8) * 2.0 ** -24 >= 0.5) & ~(host(x[-LAST:])[None] <= 0)
+    want = np.where(keep, 2.0 * (a[-LAST:].double() @ b.double().t()).cpu().numpy()[None], 0.0)
+    y = lowbit.matmul_i8(a, b, dtype=torch.bfloat16, drop=d, x=x)
+    assert product_close(y[None, -LAST:], want, None, None, None, torch.bfloat16, extra=1)
+    assert not y[-LAST:][torch.from_numpy(~keep[0]).to(DEV)].any()
