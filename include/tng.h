@@ -340,8 +340,10 @@ tng_status tng_quantize_grad(void* hip_stream, const tng_drop* key, const tng_ma
  * scales that are NULL are 1, bias NULL is 0.  rows, channels <= 2^22, workers * rows <= 2^23, depth <= 2^22.
  * drop, x: NULL, or the gradient of what stood in front of the layer: y is then multiplied by keep f'(x) / (1 - p), with x of y's
  * type and size as in tng_dropout_grad.
- * Rows of a and b that begin 16-byte aligned (data, and ld and pitch multiples of 16, ld < 2^23) take the fast kernels.  Those read a row to the
- * end of its last 16-byte piece; what lies there does not matter. */
+ * Rows of a and b that begin 16-byte aligned take the fast kernels: data is aligned, and ld (< 2^23) and pitch are multiples of 16, where ld
+ * does not count of single rows nor pitch of one worker.  Those kernels read whole 16-byte pieces: behind the last worker's last row, a single
+ * one too, to the end of the aligned piece that its last code lies in, behind other rows up to 127 bytes of what lies between them and the next.
+ * These bytes have to be readable; what they hold does not matter, and may change meanwhile. */
 size_t tng_matmul_i8_bytes(const tng_matrix* a, const tng_matrix* b, const tng_matrix* y);
 tng_status tng_matmul_i8(void* hip_stream, const tng_matrix* a, const float* a_scale, const tng_matrix* b, const float* b_scale,
                          const float* bias, const tng_drop* drop, const tng_matrix* x, const tng_matrix* y, void* workspace,

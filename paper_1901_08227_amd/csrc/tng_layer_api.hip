@@ -55,6 +55,8 @@ tng::View view(const tng_matrix* a) {
   if (a == nullptr) return tng::View{nullptr, 0, 0};
   // Strides that no index reaches are made what suits the products: single rows of several workers lie as one worker's rows do, and one row
   // by itself begins aligned as its address does.
+  // (The products' fast kernels then read its last codes as a whole aligned piece of 16 bytes, as they do every last row's; a page that holds
+  // one of them holds the piece.)
   uint64_t ld = a->ld;
   if (a->rows <= 1) ld = a->workers > 1 && a->pitch < (1u << 23) ? a->pitch : (a->cols + 15) / 16 * 16;
   return tng::View{a->data, ld, a->workers > 1 ? a->pitch : a->rows * ld};

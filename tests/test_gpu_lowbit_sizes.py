@@ -1,4 +1,4 @@
-"""The layer calls at the sizes where another kernel takes over and beyond 32 bits, against the oracle."""
+"""The layer calls at the sizes where another kernel takes over, beyond 32 bits, and with something else's bytes behind their rows, against the oracle."""
 import numpy as np
 import pytest
 import torch
@@ -7,7 +7,7 @@ from gpu_util import DEV, say
 from oracle import lowbit_oracle as L
 from oracle import tng_oracle as O
 from paper_1901_08227_amd import lowbit
-from test_gpu_lowbit import gen, host, normal, product_close, random_codes, rounded, same, spread
+from test_gpu_lowbit import gen, held, host, normal, product_close, random_codes, rounded, same, spread
 
 pytestmark = pytest.mark.gpu
 
@@ -140,3 +140,31 @@ def test_results_beyond_32_bits():
     y = lowbit.matmul_i8(a, b, dtype=torch.bfloat16, drop=d, x=x)
     assert product_close(y[None, -LAST:], want, None, None, None, torch.bfloat16, extra=1)
     assert not y[-LAST:][torch.from_numpy(~keep[0]).to(DEV)].any()
+
+
+# ---- what lies behind a row
+
+@pytest.mark.parametrize("M,T,N,K", [(1, 1, 1008, 1000), (1, 1, 40, 7), (1, 1, 513, 20001), (4, 1, 300, 1000), (1, 200, 1, 1000), (3, 100, 1, 77), (1, 1, 1, 130)])
+def test_what_lies_behind_a_single_row_does_not_matter(M, T, N, K):
+    """A matrix's only row counts as aligned by its address; its last 16 bytes, which are read as a piece, hold something else's codes."""
+    a, b = random_codes((M, T, K), 151), random_codes((M, N, K), 152)
+    sa, sb = torch.rand((M, T), generator=gen(153), device=DEV), torch.rand((M, N), generator=gen(154), device=DEV)
+    want = L.product(a.cpu().numpy(), b.cpu().numpy(), host(sa), host(sb))
+
+    def single(codes, other):
+        """[M, 1, K] codes, strides (16 bytes' multiple, K, 1)."""
+        big = random_codes((M, -(-K // 16) * 16 + 16), other, -128)
+        big[:, :K] = codes[:, 0]
+        view = big[:, :K].unsqueeze(1)
+        assert view.stride() == (big.shape[1], K, 1)
+        return view
+
+    for other in (155, 156):
+        u = single(a, other) if T == 1 else held(a)
+        v = single(b, other + 2) if N == 1 else held(b)
+        assert product_close(lowbit.matmul_i8(u, v, sa, sb), want, sa, sb, None, torch.float32)
+        if N == 1:  # and where the rows are coded on the way
+            x = normal((M, T, K), torch.float32, 157)
+            q, s = lowbit.quantize_rows(x)
+            got = [lowbit.linear(x, lowbit.Weight(w, sb)) for w in (v, b)]
+            assert torch.equal(*got) and product_close(got[0], L.product(q.cpu().numpy(), b.cpu().numpy(), host(s), host(sb)), s, sb, None, torch.float32)
