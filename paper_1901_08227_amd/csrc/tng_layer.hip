@@ -19,7 +19,7 @@ __device__ __forceinline__ float dropout_value(float x, float other, bool keep, 
   return pass ? x * d.scale : 0.f;
 }
 
-// 16 bytes of a run; STREAM: past the caches, where the whole is larger than they are.
+// 16 bytes of a run; STREAM: past the caches.
 template <typename T, int N, bool STREAM>
 __device__ __forceinline__ void run_in(const T* p, float (&x)[N]) {
   typedef T vec __attribute__((ext_vector_type(N), aligned(alignof(T))));
@@ -127,8 +127,12 @@ hipError_t dropout_typed(const Extent& n, const DropArgs& d, const View& x, cons
   const bool run = n.rows == 1 || (x.ld == n.cols && y.ld == n.cols && (!two || other.ld == n.cols));
   const uint64_t per = run ? kBlock * (16 / sizeof(T)) : kBlock * 4;
   const dim3 grid((uint32_t)((elements + per - 1) / per), n.workers);
-  // Past the caches from 32 MiB on, which is what the dies' own hold: 8 x 2048 x 4096 bfloat16 with a residual 69.6 -> 62.4 us (6.5 TB/s).
-  if (run && elements * n.workers * sizeof(T) >= (32u << 20))
+  // Past the caches where the operands together are more than the memory-side cache holds; of less, what comes next finds y in there.  Both sides, us,
+  // past / through the caches, bfloat16, the call alone and with the coder of y's rows behind it: with a residual 32 MiB each 16.2 / 16.9 and
+  // 29.7 / 26.5, 80 MiB 38.9 / 36.7 and 63.4 / 59.9, 96 MiB 46.9 / 52.5 and 75.9 / 73.6, 128 MiB 60.2 / 67.5 and 96.3 / 98.9; without one 128 MiB 42.3 /
+  // 41.8 and 76.0 / 73.2, 192 MiB 66.2 / 67.4 and 109.4 / 121.5.
+  const uint64_t bytes = elements * n.workers * sizeof(T) * (two ? 3 : 2);
+  if (run && bytes > (256u << 20))
     dropout_run_kernel<T, KIND, true><<<grid, kBlock, 0, s>>>(elements, d, x, other, y);
   else if (run)
     dropout_run_kernel<T, KIND, false><<<grid, kBlock, 0, s>>>(elements, d, x, other, y);

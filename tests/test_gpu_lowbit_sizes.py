@@ -92,6 +92,25 @@ def last_words(seed, it, site, stream):
     return O._draw_words(seed, it, 0, stream | site << 8, (rows - LAST) * cols, LAST * cols).reshape(1, LAST, cols)
 
 
+@pytest.mark.parametrize("dtype,shape", [(torch.bfloat16, (2, 8200, 4099)), (torch.float16, (1, 16500, 4096)), (torch.float32, (3, 3000, 4001))])
+def test_dropout_past_the_caches(dtype, shape):
+    """More than 256 MiB of operands; by rows, from operands with gaps, it takes another kernel."""
+    M, rows, cols = shape
+    say(f"layer calls: dropout of {M} x {rows} x {cols}")
+    x, res = normal(shape, dtype, 147), normal(shape, dtype, 148)
+    assert 2 * x.numel() * x.element_size() > 256 << 20
+    gap = spread(x, 0)
+    for relu in (False, True):
+        d = lowbit.Drop(5, 6, 7, 0.25, relu)
+        words = O._draw_words(5, 6, M - 1, L.STREAM_DROPOUT | 7 << 8, (rows - LAST) * cols, LAST * cols).reshape(LAST, cols)
+        keep = (words >> 8) * 2.0 ** -24 >= 0.25
+        xe, re = host(x[-1, -LAST:]), host(res[-1, -LAST:])
+        for got, by_rows, want in ((lowbit.dropout(x, d), lowbit.dropout(gap, d), L.dropout(xe, keep, 0.25, relu)),
+                                   (lowbit.dropout(x, d, res), lowbit.dropout(gap, d, res), L.dropout(xe, keep, 0.25, relu, re)),
+                                   (lowbit.dropout_grad(res, d, x), lowbit.dropout_grad(res, d, gap), L.dropout_grad(re, keep, 0.25, relu, xe))):
+            assert torch.equal(got, by_rows) and same(got[-1, -LAST:], rounded(want, dtype))
+
+
 def test_dropout_of_elements_beyond_32_bits():
     rows, cols = FAR
     assert (rows - LAST) * cols >= 1 << 32
