@@ -350,8 +350,8 @@ tng_status tng_matmul_i8(void* hip_stream, const tng_matrix* a, const float* a_s
                          size_t workspace_bytes);
 
 /* A layer that answers: tng_quantize_rows of x (of what drop makes of it) and tng_matmul_i8 of its codes with b, in one call; y of x's
- * type.  Up to eight rows are coded by the kernel that multiplies them (drop NULL, and their codes within 40 KB).  The same result, bit
- * for bit, as the two calls. */
+ * type.  Where that is sooner, which is up to four rows (of all workers together if they share b) and with drop NULL, the kernel that multiplies
+ * the rows codes them itself, and the workspace is not touched.  The same result, bit for bit, as the two calls. */
 size_t tng_linear_i8_bytes(const tng_matrix* x, const tng_matrix* b, const tng_matrix* y);
 tng_status tng_linear_i8(void* hip_stream, const tng_drop* drop, const tng_matrix* x, const tng_matrix* b, const float* b_scale,
                          const float* bias, const tng_matrix* y, void* workspace, size_t workspace_bytes);
