@@ -2,13 +2,17 @@
 include/tng.h on torch tensors).
 
 Tensors are [rows, cols] for one worker or [M, rows, cols] for M of them, float32, bfloat16 or float16, on the GPU, with contiguous
-rows; other strides are free.  Everything runs in the library's kernels on the current stream of the tensors' device; results and
-scratch come from torch's allocator.  A training step of a layer is
+rows.  The strides of rows and workers are free as long as a worker's matrix ends before the next one begins (inputs may also have
+strides of 0; workers whose rows alternate are refused).  Everything runs in the library's kernels on the current stream of the
+tensors' device; results and scratch come from torch's allocator.  A training step of a layer is
 
     y, saved = linear(x, weight, bias, drop, keep=True)
     dx, dw, db = linear_grad(dy, saved, weight, seed=..., iter=..., site=...)
 
-with dw and db of every worker, as the coder of the gradients takes them (out= puts them where g[M][d] has them).
+with dw and db of every worker, as the coder of the gradients takes them (out= puts dw where g[M][d] has it).
+
+Nothing here is recorded by autograd: what the calls make never requires a gradient, also where an argument does, and the backward
+pass is the calls above.
 """
 from __future__ import annotations
 
@@ -34,14 +38,16 @@ class Drop(NamedTuple):
 
 class Weight(NamedTuple):
     """Codes of a layer's weights [channels, depth], one scale for each channel; qt: the same codes turned, [depth, channels],
-    which the backward pass reads."""
+    which the backward pass reads.  With a leading M each worker has weights of its own: a layer then answers, but linear_grad
+    takes one set of weights for all workers only."""
     q: torch.Tensor
     scale: torch.Tensor
     qt: Optional[torch.Tensor] = None
 
 
 class Saved(NamedTuple):
-    """What the backward pass of a layer reads again of its forward pass."""
+    """What the backward pass of a layer reads again of its forward pass.  x is the caller's tensor, not a copy: what is written to it
+    before linear_grad changes which elements the relu lets through."""
     x: Optional[torch.Tensor]  # only where a relu's gradient needs it
     drop: Optional[Drop]
     scale: torch.Tensor        # of the tokens' codes, [M, rows]
