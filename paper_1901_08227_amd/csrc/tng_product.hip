@@ -189,8 +189,9 @@ __global__ void __launch_bounds__(kBlock) product_any_kernel(Task p) {
 //
 // What bounds it: of large tiles (256 x 256: 128 operations for each byte that comes from a cache) the matrix units, at the clock that
 // their power leaves.  8192 x 8192 x 8192 takes 406 us, 2.7 POP/s; the same instructions on registers alone reach 4.1 on random codes and 4.8 on
-// zeros.  Of small ones what the dies' caches hand to the CUs (some 13 TB/s: 2048 x 2048 x 2048 13 us), and of few the latency of a
-// stage.  Stages of 128 codes are whole lines of memory (rings of 64-code stages: 8192^3 in 550 us), eight wavefronts leave each 128 x 64
+// zeros.  Of small ones and of few the time of a stage, its requests to the die's cache: 2048 x 2048 x 2048 13 us, at 300 to 370 cycles a
+// request.  Rows that begin on no line of 128 bytes take up to twice as many: 200 x 8192 x 5000 23.7 us with rows 5008 apart, 18.4 with 5120.
+// Stages of 128 codes are whole lines of memory where rows are (rings of 64-code stages: 8192^3 in 550 us), eight wavefronts leave each 128 x 64
 // results (four of 128 x 128: 516), a load after each group keeps the memory and the matrix units busy together (two at a time: 501).
 constexpr int kDepth = 128;  // bytes of a stage's rows: eight 16-byte pieces
 
@@ -793,9 +794,8 @@ uint64_t over(uint64_t n, uint64_t by) { return (n + by - 1) / by; }
 uint64_t part_pitch(const Product& p) { return over(p.channels, 8) * 8; }  // (rows of partial sums hold whole runs)
 
 // Which tiles, and how many splits of the depth.  Estimated, in us, from what was measured: a stage takes a fixed time where few CUs work (the
-// loads' latency) and more where all do (what the dies' caches hand out, some 13 TB/s in all); each tile of a workgroup has its time
-// beside its stages (first loads, scaling, writing); joining splits takes 5 and their bytes at 4 TB/s.  All sides, us, tokens x channels x depth,
-// narrow (64 channels x 128 tokens) / small (128 x 128) / large tiles (256 x 256): 333 x 1003 x 1000 6.9 / 8.7 / 12; 200 x 8192 x 5000 22.7 / 26 / 58;
+// loads' latency) and more where all do; each tile of a workgroup has its time beside its stages (first loads, scaling, writing); joining splits
+// takes 5 and their bytes at 4 TB/s.  All sides, us, tokens x channels x depth, narrow (64 channels x 128 tokens) / small (128 x 128) / large tiles (256 x 256): 333 x 1003 x 1000 6.9 / 8.7 / 12; 200 x 8192 x 5000 22.7 / 26 / 58;
 // 1024 x 1024 x 8192 24.4 / 31.7 / 75; 2048 x 2048 x 2048 18.6 / 14.7 / 26.7; 8192 x 8192 x 1024 166 / 134 / 94; 8192 x 8192 x 8192 - / 585 /
 // 407; one / two splits of the small: 1024 x 1024 x 8192 31 / 25; 4096 x 512 x 4096 19.8 / 24.6.  Flat tiles (128 x 64) against narrow: 64 x 16384 x
 // 4096 14.3 / 16.5; 64 x 32768 x 512 5.7 / 6.6; 129 x 8192 x 8192 23.5 / 27.1.
