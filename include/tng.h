@@ -288,7 +288,9 @@ typedef enum {
   TNG_TYPE_F32 = 0,
   TNG_TYPE_BF16 = 1, /* the upper half of a binary32 */
   TNG_TYPE_F16 = 2,  /* IEEE binary16 */
-  TNG_TYPE_I8 = 3
+  TNG_TYPE_I8 = 3,
+  TNG_TYPE_I32 = 4, /* tokens */
+  TNG_TYPE_I64 = 5
 } tng_type;
 
 typedef struct {
@@ -355,6 +357,41 @@ tng_status tng_matmul_i8(void* hip_stream, const tng_matrix* a, const float* a_s
 size_t tng_linear_i8_bytes(const tng_matrix* x, const tng_matrix* b, const tng_matrix* y);
 tng_status tng_linear_i8(void* hip_stream, const tng_drop* drop, const tng_matrix* x, const tng_matrix* b, const float* b_scale,
                          const float* bias, const tng_matrix* y, void* workspace, size_t workspace_bytes);
+
+/* Root-mean-square norm of rows, with the addition of a residual in front:
+ *   h = x + residual (NULL: x), rounded to x's type;  s = 1 / sqrt(mean h^2 + eps);  y = h s weight
+ * in binary32, from h as it is stored: the same, bit for bit, as an addition by itself and the norm of its result.  A row of h that holds an infinity or
+ * a NaN gives NaN; squares beyond binary32 are none of those (they are taken of h 2^-70 then).  Sums of a row: binary32, in a fixed order. */
+typedef struct {
+  const float* weight; /* device float[cols], one for all workers; NULL: 1     */
+  float eps;           /* at least FLT_MIN, finite: rows of zeros give zeros   */
+} tng_rms;
+
+/* Matrices of one type (F32, BF16, F16) and size, limits as for tng_quantize_rows; residual and h may be NULL (h: not wanted).  h and y may each be x or
+ * residual. */
+tng_status tng_rms_norm(void* hip_stream, const tng_matrix* x, const tng_matrix* residual, const tng_rms* norm, const tng_matrix* h,
+                        const tng_matrix* y);
+/* The rows of y, before a rounding to x's type, as tng_quantize_rows codes them: q, scale[workers][rows], and with qt (NULL: not wanted) the same
+ * codes turned. */
+tng_status tng_rms_norm_codes(void* hip_stream, const tng_matrix* x, const tng_matrix* residual, const tng_rms* norm, const tng_matrix* h,
+                              const tng_matrix* q, float* scale, const tng_matrix* qt);
+/* With g = weight dy:  dx = s (g - h s^2 mean(g h)) + dresidual,  dw[m] = sum over worker m's rows of dy h s.
+ * dy: the gradient of y; h: as above; dresidual: what reaches h on the way past the norm (NULL: nothing); dx: the gradient of x, which is the residual's
+ * too, and may be dy, h or dresidual; dw: device float[workers][cols], binary32 in a fixed order, NULL: not wanted. */
+size_t tng_rms_norm_grad_bytes(const tng_matrix* dy);
+tng_status tng_rms_norm_grad(void* hip_stream, const tng_matrix* dy, const tng_matrix* h, const tng_matrix* dresidual, const tng_rms* norm,
+                             const tng_matrix* dx, float* dw, void* workspace, size_t workspace_bytes);
+
+/* Rows of a table by tokens: y[m][t] = scale table[id[m][t]], a product in binary32 rounded to y's type.
+ * ids: I32 or I64, rows = tokens of each worker (as x's rows above), cols = 1, any ld; table: F32, BF16 or F16 [vocabulary][cols], one for all workers
+ * (workers = 1) or one for each, vocabulary and cols <= 2^22; y: F32, BF16 or F16, not in the table's place; scale: host, NULL: 1.
+ * A token below 0 or from `vocabulary` on stands for nothing: its row of y is zeros, and no gradient comes of it. */
+tng_status tng_embed(void* hip_stream, const tng_matrix* ids, const tng_matrix* table, const float* scale, const tng_matrix* y);
+/* dtable[m][v] = scale times the sum of dy[m][t] over the tokens of v, in binary32 and in a fixed order; rows of no token are zeros.  dtable: F32
+ * [vocabulary][cols] of each worker. */
+size_t tng_embed_grad_bytes(const tng_matrix* ids, const tng_matrix* dy, const tng_matrix* dtable);
+tng_status tng_embed_grad(void* hip_stream, const tng_matrix* ids, const tng_matrix* dy, const float* scale, const tng_matrix* dtable, void* workspace,
+                          size_t workspace_bytes);
 
 #ifdef __cplusplus
 }

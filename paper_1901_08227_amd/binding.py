@@ -30,7 +30,7 @@ NORM_NONE, NORM_SUB, NORM_QUOT, NORM_COMB, NORM_MEAN = 0, 1, 2, 3, 4
 SCALE_MAX, SCALE_L2 = 0, 1
 REF_ZERO, REF_LAST_AVG, REF_WINDOW_AVG = 0, 1, 2
 PROB_EXTERNAL, PROB_LOGREG_DENSE, PROB_LOGREG_CSR, PROB_ROSENBROCK = 0, 1, 2, 3
-TYPE_F32, TYPE_BF16, TYPE_F16, TYPE_I8 = 0, 1, 2, 3
+TYPE_F32, TYPE_BF16, TYPE_F16, TYPE_I8, TYPE_I32, TYPE_I64 = 0, 1, 2, 3, 4, 5
 
 
 class TngConfig(ctypes.Structure):
@@ -52,6 +52,10 @@ class TngMatrix(ctypes.Structure):
 class TngDrop(ctypes.Structure):
     _fields_ = [("seed", ctypes.c_uint64), ("iter", ctypes.c_uint32), ("site", ctypes.c_uint32), ("p", ctypes.c_float),
                 ("relu", ctypes.c_int32)]
+
+
+class TngRms(ctypes.Structure):
+    _fields_ = [("weight", ctypes.c_void_p), ("eps", ctypes.c_float)]
 
 
 class TngError(RuntimeError):
@@ -127,7 +131,8 @@ def lib() -> ctypes.CDLL:
             "tng_update_reference": [vp, u32, vp, vp],
             "tng_step": [vp, u32, vp, vp, vp, vp, vp, vp],
         }
-        matp, dropp = ctypes.POINTER(TngMatrix), ctypes.POINTER(TngDrop)
+        matp, dropp, rmsp = ctypes.POINTER(TngMatrix), ctypes.POINTER(TngDrop), ctypes.POINTER(TngRms)
+        floatp = ctypes.POINTER(ctypes.c_float)
         sigs.update({  # the layer calls: a stream in the place of a context
             "tng_dropout": [vp, dropp, matp, matp, matp],
             "tng_dropout_grad": [vp, dropp, matp, matp, matp],
@@ -135,9 +140,15 @@ def lib() -> ctypes.CDLL:
             "tng_quantize_grad": [vp, dropp, matp, vp, vp, matp, vp, matp, vp, vp, vp, ctypes.c_size_t],
             "tng_matmul_i8": [vp, matp, vp, matp, vp, vp, dropp, matp, matp, vp, ctypes.c_size_t],
             "tng_linear_i8": [vp, dropp, matp, matp, vp, vp, matp, vp, ctypes.c_size_t],
+            "tng_rms_norm": [vp, matp, matp, rmsp, matp, matp],
+            "tng_rms_norm_codes": [vp, matp, matp, rmsp, matp, matp, vp, matp],
+            "tng_rms_norm_grad": [vp, matp, matp, matp, rmsp, matp, vp, vp, ctypes.c_size_t],
+            "tng_embed": [vp, matp, matp, floatp, matp],
+            "tng_embed_grad": [vp, matp, matp, floatp, matp, vp, ctypes.c_size_t],
         })
-        L.tng_quantize_grad_bytes.restype, L.tng_quantize_grad_bytes.argtypes = ctypes.c_size_t, [matp]
-        for name in ("tng_matmul_i8_bytes", "tng_linear_i8_bytes"):
+        for name in ("tng_quantize_grad_bytes", "tng_rms_norm_grad_bytes"):
+            getattr(L, name).restype, getattr(L, name).argtypes = ctypes.c_size_t, [matp]
+        for name in ("tng_matmul_i8_bytes", "tng_linear_i8_bytes", "tng_embed_grad_bytes"):
             getattr(L, name).restype, getattr(L, name).argtypes = ctypes.c_size_t, [matp, matp, matp]
         for name, argtypes in sigs.items():
             fn = getattr(L, name)
@@ -147,7 +158,8 @@ def lib() -> ctypes.CDLL:
                     for name in ("tng_local_grad", "tng_normalize_encode", "tng_decode_aggregate", "tng_update_reference",
                                  "tng_step", "tng_dropout", "tng_dropout_grad", "tng_quantize_rows", "tng_quantize_grad",
                                  "tng_quantize_grad_bytes", "tng_matmul_i8", "tng_matmul_i8_bytes", "tng_linear_i8",
-                                 "tng_linear_i8_bytes")}
+                                 "tng_linear_i8_bytes", "tng_rms_norm", "tng_rms_norm_codes", "tng_rms_norm_grad",
+                                 "tng_rms_norm_grad_bytes", "tng_embed", "tng_embed_grad", "tng_embed_grad_bytes")}
         _lib = L
     return _lib
 

@@ -123,6 +123,8 @@ struct LayerCall {
   tng_matrix matrix[8];
   int matrices = 0;
   tng_drop drop;
+  tng_rms norm;
+  float number;
   c10::Device device{c10::kCPU};
   bool have_device = false;
   PyObject* first = nullptr;  // the first matrix
@@ -174,8 +176,41 @@ struct LayerCall {
     at::Tensor t;
     if (matrices == 0 || !tensor(obj, &t) || t.scalar_type() != at::kFloat || !t.is_contiguous()) return false;
     const tng_matrix& m = matrix[matrices - 1];
-    if ((uint64_t)t.numel() != (kind == 'r' ? m.workers * m.rows : kind == 'n' ? m.rows : m.cols)) return false;
+    if ((uint64_t)t.numel() != (kind == 'r' ? m.workers * m.rows : kind == 'e' ? m.workers * m.cols : kind == 'n' ? m.rows : m.cols)) return false;
     *out = reinterpret_cast<uintptr_t>(t.data_ptr());
+    return true;
+  }
+
+  // Tokens [T] or [M, T]: a column of each worker.
+  bool as_tokens(PyObject* obj, uintptr_t* out) {
+    at::Tensor t;
+    if (matrices == 8 || !tensor(obj, &t) || (t.scalar_type() != at::kInt && t.scalar_type() != at::kLong)) return false;
+    const int64_t dim = t.dim();
+    if (dim != 1 && dim != 2) return false;
+    const auto sizes = t.sizes();
+    const auto strides = t.strides();
+    if (dim == 2 && (sizes[0] < 1 || sizes[0] > 65535)) return false;
+    tng_matrix& m = matrix[matrices];
+    m = tng_matrix{t.data_ptr(), t.scalar_type() == at::kInt ? TNG_TYPE_I32 : TNG_TYPE_I64, dim == 2 ? (uint32_t)sizes[0] : 1u,
+                   (uint64_t)sizes[dim - 1], 1u, (uint64_t)strides[dim - 1], dim == 2 ? (uint64_t)strides[0] : 0u};
+    if (matrices++ == 0) first = obj;
+    *out = reinterpret_cast<uintptr_t>(&m);
+    return true;
+  }
+
+  bool as_norm(PyObject* obj, uintptr_t* out) {
+    if (!PyTuple_Check(obj) || PyTuple_GET_SIZE(obj) != 2 || !PyFloat_CheckExact(PyTuple_GET_ITEM(obj, 1))) return false;
+    uintptr_t weight = 0;
+    if (PyTuple_GET_ITEM(obj, 0) != Py_None && !as_vector(PyTuple_GET_ITEM(obj, 0), 'c', &weight)) return false;
+    norm = tng_rms{reinterpret_cast<const float*>(weight), (float)PyFloat_AS_DOUBLE(PyTuple_GET_ITEM(obj, 1))};
+    *out = reinterpret_cast<uintptr_t>(&norm);
+    return true;
+  }
+
+  bool as_number(PyObject* obj, uintptr_t* out) {
+    if (!PyFloat_CheckExact(obj)) return false;
+    number = (float)PyFloat_AS_DOUBLE(obj);
+    *out = reinterpret_cast<uintptr_t>(&number);
     return true;
   }
 
@@ -241,7 +276,12 @@ PyObject* layer(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
         continue;
       }
       const char k = kinds[i];
-      const bool plain = k == 'd' ? c.as_drop(obj, &a[n]) : k == 'm' || k == 'i' ? c.as_matrix(obj, k == 'i', &a[n]) : c.as_vector(obj, k, &a[n]);
+      const bool plain = k == 'd'               ? c.as_drop(obj, &a[n])
+                         : k == 'm' || k == 'i' ? c.as_matrix(obj, k == 'i', &a[n])
+                         : k == 't'             ? c.as_tokens(obj, &a[n])
+                         : k == 'g'             ? c.as_norm(obj, &a[n])
+                         : k == 'f'             ? c.as_number(obj, &a[n])
+                                                : c.as_vector(obj, k, &a[n]);
       if (!plain) Py_RETURN_NONE;
     }
     at::Tensor held;
@@ -260,6 +300,8 @@ PyObject* layer(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     switch (n) {
       case 5: status = enter_layer(f, a, std::make_index_sequence<5>{}); break;
       case 6: status = enter_layer(f, a, std::make_index_sequence<6>{}); break;
+      case 7: status = enter_layer(f, a, std::make_index_sequence<7>{}); break;
+      case 8: status = enter_layer(f, a, std::make_index_sequence<8>{}); break;
       case 9: status = enter_layer(f, a, std::make_index_sequence<9>{}); break;
       case 11: status = enter_layer(f, a, std::make_index_sequence<11>{}); break;
       case 12: status = enter_layer(f, a, std::make_index_sequence<12>{}); break;

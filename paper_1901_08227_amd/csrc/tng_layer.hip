@@ -730,6 +730,10 @@ hipError_t launch_quantize_rows(tng_type type, const Extent& n, const DropArgs* 
       drop ? quantize_rows_typed<f16_t, true>(n, d, x, q, scale, s) : quantize_rows_typed<f16_t, false>(n, d, x, q, scale, s);
   }
   if (hipError_t e = hipGetLastError(); e != hipSuccess || qt.p == nullptr) return e;
+  return launch_turn_codes(n, q, qt, s);
+}
+
+hipError_t launch_turn_codes(const Extent& n, const View& q, const View& qt, hipStream_t s) {
   const dim3 grid((uint32_t)((n.cols + kTile - 1) / kTile), (uint32_t)((n.rows + kTile - 1) / kTile), n.workers);
   turn_codes_kernel<<<grid, kBlock, 0, s>>>(n.rows, n.cols, q, qt);
   return hipGetLastError();

@@ -3,6 +3,7 @@
 
 #include "tng_layer_kernels.hpp"
 
+#include <cfloat>
 #include <cmath>
 
 namespace {
@@ -12,14 +13,17 @@ constexpr uint64_t kMaxStride = 1ull << 40;  // (products of strides and indexes
 
 inline size_t round_up(size_t v) { return (v + 255) / 256 * 256; }
 inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
-inline size_t size_of(int32_t type) { return type == TNG_TYPE_I8 ? 1 : type == TNG_TYPE_F32 ? 4 : 2; }
+inline size_t size_of(int32_t type) {
+  return type == TNG_TYPE_I8 ? 1 : type == TNG_TYPE_I64 ? 8 : type == TNG_TYPE_F32 || type == TNG_TYPE_I32 ? 4 : 2;
+}
+inline bool is_ids(int32_t type) { return type == TNG_TYPE_I32 || type == TNG_TYPE_I64; }
 inline bool is_float(int32_t type) { return type == TNG_TYPE_F32 || type == TNG_TYPE_BF16 || type == TNG_TYPE_F16; }
 inline bool empty(const tng_matrix& a) { return a.rows == 0 || a.cols == 0; }
 
 // Whether the matrix can be worked on: sizes, strides, address.
 bool sound(const tng_matrix* a, bool output) {
   if (a == nullptr || a->workers == 0 || a->workers > 65535u) return false;
-  if (a->type < TNG_TYPE_F32 || a->type > TNG_TYPE_I8) return false;
+  if (a->type < TNG_TYPE_F32 || a->type > TNG_TYPE_I64) return false;
   if (a->rows > kMaxDrawn || a->cols > kMaxDrawn || a->ld > kMaxStride || a->pitch > kMaxStride) return false;
   if (empty(*a)) return true;
   if (a->rows > kMaxDrawn / a->cols) return false;
@@ -104,6 +108,33 @@ bool linear_scratch(const tng_matrix* x, const tng_matrix* b, const tng_matrix* 
   l->bytes = l->rest_at + 256 + tng::product_scratch_bytes(l->product);
   return true;
 }
+
+bool norm_ok(const tng_rms* n) {
+  return n != nullptr && n->eps >= FLT_MIN && n->eps <= FLT_MAX && aligned(n->weight, 4);
+}
+
+tng::NormArgs norm_args(const tng_rms& n) { return tng::NormArgs{n.weight, n.eps}; }
+
+// x and what goes with it in front of a norm; the matrices that may be absent are of x's type and size where they are there.
+bool normed_ok(const tng_matrix* x, const tng_matrix* residual, const tng_rms* norm, const tng_matrix* h) {
+  if (!norm_ok(norm) || !sound(x, false) || !is_float(x->type) || !sides_ok(x)) return false;
+  if (residual != nullptr && (!sound(residual, false) || residual->type != x->type || !same_size(x, residual))) return false;
+  return h == nullptr || (sound(h, true) && h->type == x->type && same_size(x, h));
+}
+
+// Tokens and the matrix with a row for each of them.
+bool tokens_ok(const tng_matrix* ids, const tng_matrix* rows, bool output) {
+  if (!sound(ids, false) || !is_ids(ids->type) || ids->cols != 1) return false;
+  if (!sound(rows, output) || !is_float(rows->type) || !sides_ok(rows)) return false;
+  return rows->workers == ids->workers && rows->rows == ids->rows;
+}
+
+bool embed_grad_ok(const tng_matrix* ids, const tng_matrix* dy, const tng_matrix* dtable) {
+  if (!tokens_ok(ids, dy, false) || !sound(dtable, true) || dtable->type != TNG_TYPE_F32) return false;
+  return dtable->workers == dy->workers && dtable->cols == dy->cols && dtable->rows <= kMaxSide;
+}
+
+bool scale_ok(const float* scale) { return scale == nullptr || std::isfinite(*scale); }
 
 }  // namespace
 
@@ -218,6 +249,69 @@ tng_status tng_linear_i8(void* hip_stream, const tng_drop* drop, const tng_matri
   const tng_status s = tng_quantize_rows(hip_stream, drop, x, &l.q, scale, nullptr);
   if (s != TNG_OK) return s;
   return tng_matmul_i8(hip_stream, &l.q, scale, b, b_scale, bias, nullptr, nullptr, y, at + l.rest_at, workspace_bytes - l.rest_at);
+}
+
+tng_status tng_rms_norm(void* hip_stream, const tng_matrix* x, const tng_matrix* residual, const tng_rms* norm, const tng_matrix* h,
+                        const tng_matrix* y) {
+  if (!normed_ok(x, residual, norm, h) || !sound(y, true) || y->type != x->type || !same_size(x, y)) return TNG_ERR_INVALID_ARG;
+  if (empty(*x)) return TNG_OK;
+  return hip_status(tng::launch_rms_norm((tng_type)x->type, extent(x), view(x), view(residual), norm_args(*norm), view(h), view(y), nullptr,
+                                         static_cast<hipStream_t>(hip_stream)));
+}
+
+tng_status tng_rms_norm_codes(void* hip_stream, const tng_matrix* x, const tng_matrix* residual, const tng_rms* norm, const tng_matrix* h,
+                              const tng_matrix* q, float* scale, const tng_matrix* qt) {
+  if (!normed_ok(x, residual, norm, h) || !sound(q, true) || q->type != TNG_TYPE_I8 || !same_size(x, q)) return TNG_ERR_INVALID_ARG;
+  if (qt != nullptr && (!sound(qt, true) || qt->type != TNG_TYPE_I8 || qt->workers != x->workers || qt->rows != x->cols || qt->cols != x->rows))
+    return TNG_ERR_INVALID_ARG;
+  if (x->rows == 0) return TNG_OK;
+  if (scale == nullptr || !aligned(scale, 4)) return TNG_ERR_INVALID_ARG;
+  const hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  if (x->cols == 0)  // (rows without elements: their scales are 0)
+    return hip_status(tng::launch_quantize_rows((tng_type)x->type, extent(x), nullptr, view(x), view(q), scale, tng::View{nullptr, 0, 0}, s));
+  const hipError_t e =
+      tng::launch_rms_norm((tng_type)x->type, extent(x), view(x), view(residual), norm_args(*norm), view(h), view(q), scale, s);
+  return hip_status(e != hipSuccess || qt == nullptr ? e : tng::launch_turn_codes(extent(x), view(q), view(qt), s));
+}
+
+size_t tng_rms_norm_grad_bytes(const tng_matrix* dy) {
+  if (dy == nullptr || !is_float(dy->type) || dy->workers == 0 || dy->workers > 65535u || !sides_ok(dy)) return 0;
+  return 256 + tng::rms_norm_grad_floats((tng_type)dy->type, extent(dy)) * sizeof(float);
+}
+
+tng_status tng_rms_norm_grad(void* hip_stream, const tng_matrix* dy, const tng_matrix* h, const tng_matrix* dresidual, const tng_rms* norm,
+                             const tng_matrix* dx, float* dw, void* workspace, size_t workspace_bytes) {
+  if (!normed_ok(dy, h, norm, dx) || h == nullptr || dx == nullptr || !aligned(dw, 4)) return TNG_ERR_INVALID_ARG;
+  if (dresidual != nullptr && (!sound(dresidual, false) || dresidual->type != dy->type || !same_size(dy, dresidual))) return TNG_ERR_INVALID_ARG;
+  if (dy->cols == 0 || (dy->rows == 0 && dw == nullptr)) return TNG_OK;
+  if (workspace == nullptr || !aligned(workspace, 256) || workspace_bytes < tng_rms_norm_grad_bytes(dy)) return TNG_ERR_WORKSPACE;
+  return hip_status(tng::launch_rms_norm_grad((tng_type)dy->type, extent(dy), view(dy), view(h), view(dresidual), norm_args(*norm), view(dx), dw,
+                                              static_cast<float*>(workspace), static_cast<hipStream_t>(hip_stream)));
+}
+
+tng_status tng_embed(void* hip_stream, const tng_matrix* ids, const tng_matrix* table, const float* scale, const tng_matrix* y) {
+  if (!tokens_ok(ids, y, true) || !scale_ok(scale) || !sound(table, false) || !is_float(table->type)) return TNG_ERR_INVALID_ARG;
+  if (table->rows > kMaxSide || table->cols != y->cols || (table->workers != 1 && table->workers != y->workers)) return TNG_ERR_INVALID_ARG;
+  if (empty(*y)) return TNG_OK;
+  tng::View rows = view(table);
+  if (table->workers == 1) rows.pitch = 0;
+  return hip_status(tng::launch_embed((tng_type)ids->type, (tng_type)table->type, (tng_type)y->type, y->workers, y->rows, y->cols, table->rows,
+                                      view(ids), rows, scale != nullptr ? *scale : 1.f, view(y), static_cast<hipStream_t>(hip_stream)));
+}
+
+size_t tng_embed_grad_bytes(const tng_matrix* ids, const tng_matrix* dy, const tng_matrix* dtable) {
+  if (!embed_grad_ok(ids, dy, dtable)) return 0;
+  return 256 + tng::embed_grad_words(dy->workers, dy->rows, dy->cols, dtable->rows) * sizeof(uint32_t);
+}
+
+tng_status tng_embed_grad(void* hip_stream, const tng_matrix* ids, const tng_matrix* dy, const float* scale, const tng_matrix* dtable, void* workspace,
+                          size_t workspace_bytes) {
+  if (!embed_grad_ok(ids, dy, dtable) || !scale_ok(scale)) return TNG_ERR_INVALID_ARG;
+  if (empty(*dtable)) return TNG_OK;
+  if (workspace == nullptr || !aligned(workspace, 256) || workspace_bytes < tng_embed_grad_bytes(ids, dy, dtable)) return TNG_ERR_WORKSPACE;
+  return hip_status(tng::launch_embed_grad((tng_type)ids->type, (tng_type)dy->type, dy->workers, dy->rows, dy->cols, dtable->rows, view(ids),
+                                           view(dy), scale != nullptr ? *scale : 1.f, view(dtable), static_cast<uint32_t*>(workspace),
+                                           static_cast<hipStream_t>(hip_stream)));
 }
 
 }  // extern "C"

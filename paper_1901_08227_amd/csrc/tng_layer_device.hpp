@@ -9,6 +9,13 @@ namespace tng {
 using bf16_t = __bf16;
 using f16_t = _Float16;
 
+// A number of 32 bits as it is.  (An operation and the conversion of its result to 16 bits may become one instruction, which rounds once: where results are
+// compared bit for bit they are two.)
+__device__ __forceinline__ float pinned(float x) {
+  asm("" : "+v"(x));
+  return x;
+}
+
 // Eight (or N) consecutive elements at an address of the element's own alignment, as 32-bit numbers.  Rows of odd length start
 // anywhere; loads of 16 bytes are legal there on this target.
 template <typename T, int N>

@@ -67,4 +67,27 @@ hipError_t launch_product(const Product& p, void* scratch, hipStream_t s);
 bool coded_product_applies(const Product& p, const View& x);
 hipError_t launch_coded_product(const Product& p, const View& x, hipStream_t s);
 
+// The same codes turned, as launch_quantize_rows' qt.
+hipError_t launch_turn_codes(const Extent& n, const View& q, const View& qt, hipStream_t s);
+
+struct NormArgs {
+  const float* weight;  // may be null
+  float eps;
+};
+// y = norm(x + residual); residual.p and h.p may be null.  scale not null: y is codes.
+hipError_t launch_rms_norm(tng_type type, const Extent& n, const View& x, const View& residual, const NormArgs& norm, const View& h, const View& y,
+                           float* scale, hipStream_t s);
+// residual.p and dw may be null.  Scratch: rms_norm_grad_floats() floats.
+size_t rms_norm_grad_floats(tng_type type, const Extent& n);
+hipError_t launch_rms_norm_grad(tng_type type, const Extent& n, const View& dy, const View& h, const View& residual, const NormArgs& norm,
+                                const View& dx, float* dw, float* scratch, hipStream_t s);
+
+// rows: tokens of a worker.  table.pitch 0: one table for all workers.
+hipError_t launch_embed(tng_type of_ids, tng_type of_table, tng_type type, uint32_t workers, uint64_t rows, uint64_t cols, uint64_t vocabulary,
+                        const View& ids, const View& table, float scale, const View& y, hipStream_t s);
+// Scratch: embed_grad_words() words of 32 bits.
+size_t embed_grad_words(uint32_t workers, uint64_t rows, uint64_t cols, uint64_t vocabulary);
+hipError_t launch_embed_grad(tng_type of_ids, tng_type type, uint32_t workers, uint64_t rows, uint64_t cols, uint64_t vocabulary, const View& ids,
+                             const View& dy, float scale, const View& dtable, uint32_t* scratch, hipStream_t s);
+
 }  // namespace tng

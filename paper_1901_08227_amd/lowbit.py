@@ -1,5 +1,5 @@
-"""Linear layers of libtng's simulated workers in 8-bit codes, and dropout whose mask is never stored (the layer calls of
-include/tng.h on torch tensors).
+"""Linear layers of libtng's simulated workers in 8-bit codes, and what stands around them: dropout whose mask is never stored, norms
+with a residual, embedding tables (the layer calls of include/tng.h on torch tensors).
 
 Tensors are [rows, cols] for one worker or [M, rows, cols] for M of them, float32, bfloat16 or float16, on the GPU, with contiguous
 rows.  The strides of rows and workers are free as long as a worker's matrix ends before the next one begins (inputs may also have
@@ -10,6 +10,13 @@ tensors' device; results and scratch come from torch's allocator.  A training st
     dx, dw, db = linear_grad(dy, saved, weight, seed=..., iter=..., site=...)
 
 with dw and db of every worker, as the coder of the gradients takes them (out= puts dw where g[M][d] has it).
+
+A block with a residual in front of such a layer takes the layer's codes from the norm, and goes back through it:
+
+    n = rms_norm_codes(x, gain, residual=r, turned=True)         # n.h = x + r goes on past the layer
+    y = matmul_i8(n.q, weight.q, n.scale, weight.scale, bias, dtype=x.dtype)
+    d, dw, db = linear_grad(dy, Saved(None, None, n.scale, n.qt), weight, seed=..., iter=..., site=...)
+    dx, dgain = rms_norm_grad(d, n.h, gain, dresidual=dh)        # dx is x's gradient, and r's
 
 Nothing here is recorded by autograd: what the calls make never requires a gradient, also where an argument does, and the backward
 pass is the calls above.
@@ -54,7 +61,16 @@ class Saved(NamedTuple):
     qt: torch.Tensor           # the tokens' codes turned, [M, depth, rows]
 
 
+class NormCodes(NamedTuple):
+    """Codes of a norm's rows, a scale for each row, what was normalised, and the codes turned (where asked for)."""
+    q: torch.Tensor
+    scale: torch.Tensor
+    h: torch.Tensor
+    qt: Optional[torch.Tensor] = None
+
+
 _I8 = {torch.int8: B.TYPE_I8}
+_IDS = {torch.int32: B.TYPE_I32, torch.int64: B.TYPE_I64}
 # The arguments of the layer calls behind the stream, a letter each (see csrc/tng_call.cpp), what they are called here, and the letters of a
 # call that makes its result.
 _CALLS = {
@@ -64,6 +80,11 @@ _CALLS = {
     "tng_quantize_grad": ("dmcririrrw", ("key", "dy", "col_scale", "row_scale", "q", "q_scale", "qt", "qt_scale", "col_sum"), None),
     "tng_matmul_i8": ("irirndmmW", ("a", "a_scale", "b", "b_scale", "bias", "drop", "x", "out"), None),
     "tng_linear_i8": ("dmirnmW", ("drop", "x", "codes", "scale", "bias", "out"), "dmirnpW"),
+    "tng_rms_norm": ("mmgmm", ("x", "residual", "weight", "h", "out"), "mmgmo"),
+    "tng_rms_norm_codes": ("mmgmiri", ("x", "residual", "weight", "h", "q", "scale", "qt"), None),
+    "tng_rms_norm_grad": ("mmmgmew", ("dy", "h", "dresidual", "weight", "out", "dw"), None),
+    "tng_embed": ("tmfm", ("ids", "table", "scale", "out"), None),
+    "tng_embed_grad": ("tmfmW", ("ids", "dy", "scale", "out"), None),
 }
 
 
@@ -91,6 +112,19 @@ def _matrix(t, dtypes, name):
     return B.TngMatrix(t.data_ptr(), kind, workers, shape[-2], shape[-1], stride[-2], pitch)
 
 
+def _tokens(t, name):
+    """The tng_matrix of tokens [T] or [M, T]: a column of each worker."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name}: expected a CUDA tensor")
+    kind = _IDS.get(t.dtype)
+    if kind is None:
+        raise TypeError(f"{name}: {t.dtype} is not one of {', '.join(map(str, _IDS))}")
+    if t.dim() not in (1, 2):
+        raise ValueError(f"{name}: expected [T] or [M, T], got {tuple(t.shape)}")
+    workers, pitch = (_u32(t.shape[0]), t.stride(0)) if t.dim() == 2 else (1, 0)
+    return B.TngMatrix(t.data_ptr(), kind, workers, t.shape[-1], 1, t.stride(-1), pitch)
+
+
 def _vector(t, n, name):
     """Address of a contiguous float32 tensor of n elements."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != torch.float32 or not t.is_contiguous():
@@ -108,18 +142,26 @@ def _through_ctypes(name, kinds, names, device, stream, args):
     """The call with arguments that the native function does not take as plain: converts them, or says what is wrong."""
     L, values, matrices = B.lib(), [], []
     for kind, what, arg in zip(kinds, names, args):
-        if isinstance(arg, torch.Tensor) and arg.is_cuda and arg.device != device:
-            raise ValueError(f"{what}: on {arg.device}, the others on {device}")
+        tensor = arg[0] if kind == "g" else arg
+        if isinstance(tensor, torch.Tensor) and tensor.is_cuda and tensor.device != device:
+            raise ValueError(f"{what}: on {tensor.device}, the others on {device}")
         if arg is None:
             values.append(None)
         elif kind == "d":
             values.append(_drop(arg))
+        elif kind == "f":
+            values.append(ctypes.c_float(arg))
+        elif kind == "g":
+            values.append(B.TngRms(None if arg[0] is None else _vector(arg[0], matrices[-1].cols, what), float(arg[1])))
+        elif kind == "t":
+            values.append(_tokens(arg, what))
+            matrices.append(values[-1])
         elif kind in "mi":
             values.append(_matrix(arg, _TYPES if kind == "m" else _I8, what))
             matrices.append(values[-1])
         else:
             m = matrices[-1]
-            values.append(_vector(arg, {"r": m.workers * m.rows, "n": m.rows, "c": m.cols}[kind], what))
+            values.append(_vector(arg, {"r": m.workers * m.rows, "e": m.workers * m.cols, "n": m.rows, "c": m.cols}[kind], what))
     if kinds[-1] in "wW":  # (the library sizes what it refuses as 0, and says so when it is called)
         sized = matrices[:1] if kinds[-1] == "w" else [*matrices[:2], matrices[-1]]
         scratch = torch.empty(getattr(L, name + "_bytes")(*sized), dtype=torch.uint8, device=device)
@@ -162,7 +204,7 @@ def _run(name, device, *args, made=None):
     status = B._layer(B._address[name], B._address.get(name + "_bytes", 0), stream, makes if made else kinds, *args)
     if status is None:
         if made:
-            args = (*args, torch.empty(made, dtype=args[1].dtype, device=device))
+            args = (*args, torch.empty(made, dtype=next(a for a in args if isinstance(a, torch.Tensor)).dtype, device=device))
         status = _through_ctypes(name, kinds, names, device, stream, args)
     elif not isinstance(status, int):
         return status
@@ -237,6 +279,54 @@ def matmul_i8(a, b, a_scale=None, b_scale=None, bias=None, dtype=torch.float32, 
     drop, x: the result is a gradient that goes on through that dropout (and its relu, of x)."""
     out = _out(out, (*_dims(a, "a")[:-1], _dims(b, "b")[-2]), dtype, a.device)
     return _run("tng_matmul_i8", a.device, a, a_scale, b, b_scale, bias, drop, x, out)
+
+
+def rms_norm(x, weight=None, residual=None, eps=1e-6, out=None):
+    """The rows of h = x + residual, each divided by the root of its mean square (plus eps), times the weights [cols] (float32).  With a
+    residual: (result, h)."""
+    if residual is None:
+        if out is None:
+            return _run("tng_rms_norm", x.device, x, None, (weight, float(eps)), None, made=x.shape)
+        return _run("tng_rms_norm", x.device, x, None, (weight, float(eps)), None, _out(out, x.shape, x.dtype, x.device))
+    h = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    out = _out(out, x.shape, x.dtype, x.device)
+    return _run("tng_rms_norm", x.device, x, residual, (weight, float(eps)), h, out), h
+
+
+def rms_norm_codes(x, weight=None, residual=None, eps=1e-6, turned=False):
+    """The codes of rms_norm's result, which is itself written nowhere: NormCodes(q, scale, h, qt).  h is x where there is no residual."""
+    shape, device = _dims(x, "x"), x.device
+    q, scale = _codes(shape, device), _floats(shape[:-1], device)
+    qt = _codes((*shape[:-2], shape[-1], shape[-2]), device) if turned else None
+    h = torch.empty(shape, dtype=x.dtype, device=device) if residual is not None else None
+    _run("tng_rms_norm_codes", device, x, residual, (weight, float(eps)), h, q, scale, qt)
+    return NormCodes(q, scale, x if h is None else h, qt)
+
+
+def rms_norm_grad(dy, h, weight=None, dresidual=None, eps=1e-6, out=None):
+    """(dx, dw) from the gradient dy of rms_norm's result (or of what its codes stand for) and h, what was normalised.  dresidual: the gradient that
+    reaches h past the norm.  dx is the gradient of x, and of the residual; dw [M, cols] float32 (without the M where dy has none), None without
+    weights."""
+    dx = _out(out, dy.shape, dy.dtype, dy.device)
+    (*lead, _, cols), dw = _dims(dy, "dy"), None
+    if weight is not None:
+        dw = _floats((*lead, cols), dy.device)
+    _run("tng_rms_norm_grad", dy.device, dy, h, dresidual, (weight, float(eps)), dx, dw)
+    return dx, dw
+
+
+def embed(ids, table, scale=1.0, dtype=None, out=None):
+    """scale table[ids] of the table's type, or of dtype: tokens [T] or [M, T], int32 or int64, a table [vocabulary, cols] for all workers or [M,
+    vocabulary, cols].  A token outside the table (-1, say) gets a row of zeros."""
+    return _run("tng_embed", ids.device, ids, table, float(scale),
+                _out(out, (*ids.shape, table.shape[-1]), (table if out is None else out).dtype if dtype is None else dtype, ids.device))
+
+
+def embed_grad(ids, dy, vocabulary, scale=1.0, out=None):
+    """The gradient of each worker's table [M, vocabulary, cols] (without the M where ids have none), float32, from that of embed's result.  Every
+    row is written, those of no token with zeros.  out: where it is written, any pitch."""
+    out = _out(out, (*_dims(dy, "dy")[:-2], vocabulary, dy.shape[-1]), torch.float32, dy.device)
+    return _run("tng_embed_grad", dy.device, ids, dy, float(scale), out)
 
 
 def linear(x, weight, bias=None, drop=None, keep=False):
