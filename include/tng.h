@@ -393,6 +393,27 @@ size_t tng_embed_grad_bytes(const tng_matrix* ids, const tng_matrix* dy, const t
 tng_status tng_embed_grad(void* hip_stream, const tng_matrix* ids, const tng_matrix* dy, const float* scale, const tng_matrix* dtable, void* workspace,
                           size_t workspace_bytes);
 
+/* ---- The update of a matrix -----------------------------------------------------------------------------------------
+ * A decoded average (or what a momentum makes of it) whose singular values are brought near 1 before the step:
+ *   X = x / (||x|| + eps);  for each of the steps, with its a, b, c:  G = X X^T,  X = (a + b G + c G G) X;  y = scale X
+ * ||x||: the root of the sum of squares, in binary64.  Products are of pairs of binary16 that hold 22 bits of a number and more, but nothing
+ * below 2^-39, summed in binary32.  A
+ * matrix that holds an infinity or a NaN gives NaN; one of zeros gives zeros.  The coefficients have to keep the singular values, which begin at 1 or
+ * below, under 2, and a + b s^2 + c s^4 of them within 8 (TNG_ERR_UNSUPPORTED otherwise); the optimiser Muon's (3.4445, -4.775, 2.0315), and
+ * (1.5, -0.5, 0) and (1.875, -1.25, 0.375), whose values approach 1, do. */
+typedef struct {
+  const float* coefficients; /* host float[steps][3], finite */
+  uint32_t steps;            /* 1 .. 64                      */
+  float eps;                 /* at least FLT_MIN, finite     */
+  float scale;               /* finite                       */
+} tng_orthogonal;
+
+/* Each worker's matrix by itself.  x, y: F32, BF16 or F16, of one size, workers * rows <= 2^23, rows and cols <= 65536; y may be x.  No context, stream
+ * and workspace as for the layer calls. */
+size_t tng_orthogonalize_bytes(const tng_matrix* x);
+tng_status tng_orthogonalize(void* hip_stream, const tng_matrix* x, const tng_orthogonal* plan, const tng_matrix* y, void* workspace,
+                             size_t workspace_bytes);
+
 #ifdef __cplusplus
 }
 #endif

@@ -58,6 +58,10 @@ class TngRms(ctypes.Structure):
     _fields_ = [("weight", ctypes.c_void_p), ("eps", ctypes.c_float)]
 
 
+class TngOrthogonal(ctypes.Structure):
+    _fields_ = [("coefficients", ctypes.POINTER(ctypes.c_float)), ("steps", ctypes.c_uint32), ("eps", ctypes.c_float), ("scale", ctypes.c_float)]
+
+
 class TngError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -145,8 +149,9 @@ def lib() -> ctypes.CDLL:
             "tng_rms_norm_grad": [vp, matp, matp, matp, rmsp, matp, vp, vp, ctypes.c_size_t],
             "tng_embed": [vp, matp, matp, floatp, matp],
             "tng_embed_grad": [vp, matp, matp, floatp, matp, vp, ctypes.c_size_t],
+            "tng_orthogonalize": [vp, matp, ctypes.POINTER(TngOrthogonal), matp, vp, ctypes.c_size_t],
         })
-        for name in ("tng_quantize_grad_bytes", "tng_rms_norm_grad_bytes"):
+        for name in ("tng_quantize_grad_bytes", "tng_rms_norm_grad_bytes", "tng_orthogonalize_bytes"):
             getattr(L, name).restype, getattr(L, name).argtypes = ctypes.c_size_t, [matp]
         for name in ("tng_matmul_i8_bytes", "tng_linear_i8_bytes", "tng_embed_grad_bytes"):
             getattr(L, name).restype, getattr(L, name).argtypes = ctypes.c_size_t, [matp, matp, matp]

@@ -22,7 +22,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libtng.so")
 CALL = os.path.join(HERE, "tng_call.so")
-SOURCES = ["tng_api.hip", "tng_codec.hip", "tng_grad.hip", "tng_layer.hip", "tng_norm.hip", "tng_embed.hip", "tng_product.hip", "tng_layer_api.hip"]
+SOURCES = ["tng_api.hip", "tng_codec.hip", "tng_grad.hip", "tng_layer.hip", "tng_norm.hip", "tng_embed.hip", "tng_product.hip", "tng_update.hip", "tng_layer_api.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     "-ffp-contract=off", "-fno-fast-math",

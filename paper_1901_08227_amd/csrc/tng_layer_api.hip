@@ -134,6 +134,12 @@ bool embed_grad_ok(const tng_matrix* ids, const tng_matrix* dy, const tng_matrix
   return dtable->workers == dy->workers && dtable->cols == dy->cols && dtable->rows <= kMaxSide;
 }
 
+// Matrices that are orthogonalised, apart from where they lie.
+bool update_ok(const tng_matrix* x) {
+  return x != nullptr && is_float(x->type) && x->workers != 0 && x->workers <= 65535u && x->rows <= 65536 && x->cols <= 65536 &&
+         x->workers * x->rows <= kMaxRows;
+}
+
 bool scale_ok(const float* scale) { return scale == nullptr || std::isfinite(*scale); }
 
 }  // namespace
@@ -312,6 +318,22 @@ tng_status tng_embed_grad(void* hip_stream, const tng_matrix* ids, const tng_mat
   return hip_status(tng::launch_embed_grad((tng_type)ids->type, (tng_type)dy->type, dy->workers, dy->rows, dy->cols, dtable->rows, view(ids),
                                            view(dy), scale != nullptr ? *scale : 1.f, view(dtable), static_cast<uint32_t*>(workspace),
                                            static_cast<hipStream_t>(hip_stream)));
+}
+
+size_t tng_orthogonalize_bytes(const tng_matrix* x) { return update_ok(x) ? 256 + tng::orthogonal_bytes(extent(x)) : 0; }
+
+tng_status tng_orthogonalize(void* hip_stream, const tng_matrix* x, const tng_orthogonal* plan, const tng_matrix* y, void* workspace,
+                             size_t workspace_bytes) {
+  if (!sound(x, false) || !sound(y, true) || !update_ok(x) || !is_float(y->type) || !same_size(x, y)) return TNG_ERR_INVALID_ARG;
+  if (plan == nullptr || plan->coefficients == nullptr || plan->steps < 1 || plan->steps > 64) return TNG_ERR_INVALID_ARG;
+  if (!(plan->eps >= FLT_MIN && plan->eps <= FLT_MAX) || !std::isfinite(plan->scale)) return TNG_ERR_INVALID_ARG;
+  for (uint32_t k = 0; k < 3 * plan->steps; ++k)
+    if (!std::isfinite(plan->coefficients[k])) return TNG_ERR_INVALID_ARG;
+  if (!tng::orthogonal_in_range(plan->coefficients, plan->steps)) return TNG_ERR_UNSUPPORTED;
+  if (empty(*x)) return TNG_OK;
+  if (workspace == nullptr || !aligned(workspace, 256) || workspace_bytes < tng_orthogonalize_bytes(x)) return TNG_ERR_WORKSPACE;
+  return hip_status(tng::launch_orthogonalize((tng_type)x->type, (tng_type)y->type, extent(x), view(x), plan->coefficients, plan->steps, plan->eps,
+                                              plan->scale, view(y), static_cast<char*>(workspace), static_cast<hipStream_t>(hip_stream)));
 }
 
 }  // extern "C"

@@ -131,4 +131,36 @@ __device__ __forceinline__ uint32_t pack4(uint32_t a, uint32_t b, uint32_t c, ui
   return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0C0C0400u), __builtin_amdgcn_perm(b, a, 0x0C0C0400u), 0x05040100u);
 }
 
+// ---- Tiles of the products: loads that go to LDS directly.
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+
+// 16 (4) bytes for each lane, from base + its offset to LDS, one lane's behind the other from `lds` on; what lies past `bytes` reads as 0.
+// The compiler does not count these loads: wait_and_meet does.  (s_mov and s_nop 3: as long as a scalar register written by the vector unit needs.)
+__device__ __forceinline__ void load_to_lds(uint64_t base, uint32_t bytes, uint32_t offset, uint32_t lds) {
+  const v4u rsrc = {(uint32_t)base, (uint32_t)(base >> 32) & 0xFFFFu, bytes, 0x00020000u};
+  asm volatile(
+      "s_mov_b32 m0, %0\n\t"
+      "s_nop 3\n\t"
+      "buffer_load_dwordx4 %1, %2, 0 offen lds"
+      :
+      : "s"(lds), "v"(offset), "s"(rsrc)
+      : "memory");
+}
+__device__ __forceinline__ void load_words_to_lds(uint64_t base, uint32_t bytes, uint32_t offset, uint32_t lds) {
+  const v4u rsrc = {(uint32_t)base, (uint32_t)(base >> 32) & 0xFFFFu, bytes, 0x00020000u};
+  asm volatile(
+      "s_mov_b32 m0, %0\n\t"
+      "s_nop 3\n\t"
+      "buffer_load_dword %1, %2, 0 offen lds"
+      :
+      : "s"(lds), "v"(offset), "s"(rsrc)
+      : "memory");
+}
+
+// All but the last `left` loads of every wavefront are in LDS, and every wavefront has what it reads there.
+template <int left>
+__device__ __forceinline__ void wait_and_meet() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(left) : "memory");
+}
+
 }  // namespace tng

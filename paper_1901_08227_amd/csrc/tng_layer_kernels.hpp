@@ -90,4 +90,10 @@ size_t embed_grad_words(uint32_t workers, uint64_t rows, uint64_t cols, uint64_t
 hipError_t launch_embed_grad(tng_type of_ids, tng_type type, uint32_t workers, uint64_t rows, uint64_t cols, uint64_t vocabulary, const View& ids,
                              const View& dy, float scale, const View& dtable, uint32_t* scratch, hipStream_t s);
 
+// Whether no pair leaves binary16 with these coefficients [steps][3].
+bool orthogonal_in_range(const float* coefficients, uint32_t steps);
+size_t orthogonal_bytes(const Extent& e);
+hipError_t launch_orthogonalize(tng_type of_x, tng_type of_y, const Extent& e, const View& x, const float* coefficients, uint32_t steps, float eps,
+                                float scale, const View& y, char* scratch, hipStream_t s);
+
 }  // namespace tng

@@ -195,37 +195,6 @@ __global__ void __launch_bounds__(kBlock) product_any_kernel(Task p) {
 // results (four of 128 x 128: 516), a load after each group keeps the memory and the matrix units busy together (two at a time: 501).
 constexpr int kDepth = 128;  // bytes of a stage's rows: eight 16-byte pieces
 
-typedef uint32_t v4u __attribute__((ext_vector_type(4)));
-
-// 16 (4) bytes for each lane, from base + its offset to LDS, one lane's behind the other from `lds` on; what lies past `bytes` reads as 0.
-// The compiler does not count these loads: wait_and_meet does.  (s_mov and s_nop 3: as long as a scalar register written by the vector unit needs.)
-__device__ __forceinline__ void load_to_lds(uint64_t base, uint32_t bytes, uint32_t offset, uint32_t lds) {
-  const v4u rsrc = {(uint32_t)base, (uint32_t)(base >> 32) & 0xFFFFu, bytes, 0x00020000u};
-  asm volatile(
-      "s_mov_b32 m0, %0\n\t"
-      "s_nop 3\n\t"
-      "buffer_load_dwordx4 %1, %2, 0 offen lds"
-      :
-      : "s"(lds), "v"(offset), "s"(rsrc)
-      : "memory");
-}
-__device__ __forceinline__ void load_words_to_lds(uint64_t base, uint32_t bytes, uint32_t offset, uint32_t lds) {
-  const v4u rsrc = {(uint32_t)base, (uint32_t)(base >> 32) & 0xFFFFu, bytes, 0x00020000u};
-  asm volatile(
-      "s_mov_b32 m0, %0\n\t"
-      "s_nop 3\n\t"
-      "buffer_load_dword %1, %2, 0 offen lds"
-      :
-      : "s"(lds), "v"(offset), "s"(rsrc)
-      : "memory");
-}
-
-// All but the last `left` loads of every wavefront are in LDS, and every wavefront has what it reads there.
-template <int left>
-__device__ __forceinline__ void wait_and_meet() {
-  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(left) : "memory");
-}
-
 // A tile's row has its eight 16-byte pieces moved, piece c to c ^ moved_by, so that the 16 lanes that read one piece of 16 rows meet in
 // no bank (rows are 32 banks long, of 64).  Those are rows 16 a + i, or with kWide 32 (a / 2) + 8 (i / 4) + 4 (a % 2) + i % 4.
 template <bool kWide>

@@ -1,0 +1,131 @@
+"""Orthogonalised updates on the GPU against the oracle in binary64.
+
+A stored pair is within 2^-21 of its number (two roundings of 2^-11 each), or within 2^-39: the low part's subnormal numbers lie 2^-24 apart, of which a
+rounding is off by half, and stand for 2^-14 of themselves.  Low low products that are left out another 2^-22.  A sum of k products is one of 3 k / 32 matrix instructions' results, each rounded
+(or cut) by 2^-23: summed(k) = (3 k / 32 + 8) 2^-23 + 3 2^-21 of the sum of the magnitudes.  The oracle follows these through the steps."""
+import numpy as np
+import pytest
+import torch
+
+from gpu_util import DEV, say
+from oracle import update_oracle as O
+from paper_1901_08227_amd import binding as B
+from paper_1901_08227_amd import lowbit, update
+from test_gpu_lowbit import TYPES, host, normal, same, spread
+
+pytestmark = pytest.mark.gpu
+
+QUINTIC = (update.QUINTIC,) * 5
+CUBIC = ((1.5, -0.5, 0.0),) * 3
+ONE = (update.QUINTIC,)
+SHAPES = [(1, 1, 1), (1, 1, 7), (2, 9, 1), (3, 5, 8), (2, 31, 33), (1, 64, 64), (2, 65, 32), (1, 100, 257), (5, 130, 96), (1, 300, 200), (40, 64, 130)]
+
+
+def roundings():
+    return 2.0 ** -21, 2.0 ** -39, lambda k: (3 * k / 32 + 8) * 2.0 ** -23 + 3 * 2.0 ** -21
+
+
+def near(got, x, coefficients, eps, scale):
+    got = got.double().cpu().numpy()
+    half = torch.finfo(torch.float32).eps / 2
+    for g, a in zip(got, x):
+        want, error = O.orthogonalize(a, coefficients, eps, scale, roundings())
+        if not np.linalg.norm(g - want) <= error + half * np.linalg.norm(want):
+            return False
+    return True
+
+
+@pytest.mark.parametrize("coefficients", [QUINTIC, CUBIC, ONE])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_against_binary64(shape, coefficients):
+    x = normal(shape, torch.float32, 1, 1e-3)
+    y = update.orthogonalize(x, coefficients, eps=1e-7, scale=1.25)
+    assert near(y, host(x), coefficients, 1e-7, 1.25)
+    out = spread(torch.zeros_like(x), 0)
+    assert update.orthogonalize(spread(x, 0), coefficients, scale=1.25, out=out) is out and torch.equal(out, y)
+    assert torch.equal(update.orthogonalize(x, coefficients, scale=1.25), y)
+    a = x.clone()
+    assert update.orthogonalize(a, coefficients, scale=1.25, out=a) is a and torch.equal(a, y)
+    assert torch.equal(update.orthogonalize(x[0], coefficients, scale=1.25), y[0])
+    # a turned matrix's result is the result turned (sums of other orders: both are near)
+    assert near(update.orthogonalize(x.transpose(1, 2).contiguous(), coefficients, scale=1.25).transpose(1, 2), host(x), coefficients, 1e-7, 1.25)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("to", TYPES)
+def test_types(dtype, to):
+    x = normal((2, 70, 150), dtype, 2)
+    wide = update.orthogonalize(x.float())
+    out = torch.empty(x.shape, dtype=to, device=DEV)
+    assert same(update.orthogonalize(x, out=out), wide.to(to).cpu())
+    assert update.orthogonalize(x).dtype == dtype
+
+
+def test_large_tiles():
+    # more tiles of 128 x 128 than CUs, none of them whole at the edges
+    x = normal((9, 700, 777), torch.float32, 3)
+    y = update.orthogonalize(x, ONE)
+    say("update: 9 x 700 x 777")
+    assert near(y[:2], host(x[:2]), ONE, 1e-7, 1.0) and near(y[8:], host(x[8:]), ONE, 1e-7, 1.0)
+    z = update.orthogonalize(x.transpose(1, 2).contiguous(), QUINTIC)
+    assert near(z[:1].transpose(1, 2), host(x[:1]), QUINTIC, 1e-7, 1.0)
+    # as accurate as binary32 itself, within a factor of four
+    want = torch.from_numpy(O.orthogonalize(host(x[0]), QUINTIC, 1e-7, 1.0))
+    v = x[0] / (x[0].norm() + 1e-7)
+    for a, b, c in QUINTIC:
+        g = v @ v.t()
+        v = a * v + (b * g + c * (g @ g)) @ v
+    assert (z[0].t().double().cpu() - want).norm() <= 4 * (v.double().cpu() - want).norm()
+
+
+@pytest.mark.parametrize("size", [1e-30, 1e-9, 1.0, 1e30])
+def test_sizes_of_the_input(size):
+    x = normal((1, 40, 60), torch.float32, 4).clamp(-3, 3) * size
+    assert near(update.orthogonalize(x, QUINTIC, eps=1e-30), host(x), QUINTIC, 1e-30, 1.0)
+    assert near(update.orthogonalize(x, QUINTIC, eps=0.5), host(x), QUINTIC, 0.5, 1.0)
+
+
+def test_one_direction_and_zeros_and_what_is_not_finite():
+    x = normal((4, 50, 80), torch.float32, 5)
+    x[1] = torch.outer(normal((50,), torch.float32, 6), normal((80,), torch.float32, 7))  # its singular value begins at 1
+    x[2] = 0
+    clean = update.orthogonalize(x)
+    assert near(clean[:2], host(x[:2]), QUINTIC, 1e-7, 1.0) and clean[2].eq(0).all()
+    bad = x.clone()
+    bad[0, 3, 3], bad[3, 49, 79] = float("inf"), float("nan")
+    got = update.orthogonalize(bad)
+    assert got[[0, 3]].isnan().all() and torch.equal(got[1:3], clean[1:3])
+
+
+def test_broadcast_and_nothing_and_refusals():
+    x = normal((30, 20), torch.bfloat16, 8)
+    got = update.orthogonalize(x.expand(3, 30, 20))
+    assert torch.equal(got, update.orthogonalize(x).expand(3, 30, 20))
+    for shape in ((0, 5), (5, 0), (2, 0, 5)):
+        assert update.orthogonalize(torch.empty(shape, device=DEV)).shape == shape
+    with pytest.raises(B.TngError):
+        update.orthogonalize(x, ((2.5, 0.0, 0.0),))
+    with pytest.raises(ValueError):
+        update.orthogonalize(x, ((1.5, 0.0),))
+    with pytest.raises(ValueError):
+        update.orthogonalize(x, out=torch.empty((30, 21), device=DEV))
+    with pytest.raises(TypeError):
+        update.orthogonalize(x.to(torch.int8))
+
+
+def test_graph_and_another_stream():
+    x = normal((3, 100, 90), torch.float32, 9)
+    want = update.orthogonalize(x)
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = update.orthogonalize(x)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(got, want)
+    with torch.cuda.graph(graph):
+        got = update.orthogonalize(x)
+    for k in range(3):
+        x.copy_(normal(x.shape, torch.float32, 20 + k))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got, update.orthogonalize(x))
