@@ -17,11 +17,15 @@ __device__ __forceinline__ uint32_t row_of(const I* ids, uint64_t at, uint64_t r
   return id >= 0 && (uint64_t)id < rows ? (uint32_t)id : (uint32_t)rows;
 }
 
+// Results of more bytes are written past the caches: the memory-side cache does not hold them.
+constexpr uint64_t kPast = 128u << 20;
+
 struct EmbedTask {
   uint64_t rows, cols, eights;  // tokens of a worker; columns; lanes that a row takes
   uint64_t vocabulary;
   View ids, table, y;
   float scale;
+  bool past;  // y is written past the caches
 };
 
 // y = scale table[id].  A lane takes eight columns of kMany tokens' rows (the row's last eight where it ends inside them: what two lanes write of
@@ -66,6 +70,8 @@ __global__ void __launch_bounds__(kBlock) embed_kernel(EmbedTask p) {
 #pragma unroll
       for (uint32_t i = 0; i < 8; ++i)
         if (i < p.cols) to[i] = v[i];
+    } else if (p.past) {
+      __builtin_nontemporal_store(v, reinterpret_cast<Vec8<T>*>(to));
     } else {
       *reinterpret_cast<Vec8<T>*>(to) = v;
     }
@@ -116,11 +122,12 @@ void embed_from(tng_type table, tng_type type, uint32_t workers, EmbedTask& p, h
 // ---- the gradient of the table
 //
 // A row's gradient is the sum of its tokens' rows of dy.  Tokens are sorted, kSorted at a time, by a workgroup each, in LDS: the tokens of a row lie
-// together then, in the order that they came in, whatever ran first.  Sums are taken in that order: of pieces of kPiece sorted places that are
-// all one row's (for rows that many tokens ask for), of kPiece such pieces, and then of a row.  Every row of the table is written, those of no token with zeros.
+// together then, a run, in the order that they came in, whatever ran first.  Sums are taken in that order.  Runs that cross the ends of pieces of kPiece sorted
+// places are summed by pieces first, and those that cross the ends of kPiece pieces by such wholes: whatever tokens come, no sum is a long chain, and
+// each row of dy is read once.  Every row of the table is written, those of no token with zeros.
 constexpr uint32_t kSorted = 8192, kSortThreads = 1024, kSortWaves = kSortThreads / kWave;
+constexpr uint32_t kFewSorted = 256;                        // so many are sorted by counting for each those before it
 constexpr uint32_t kPiece = 32, kWhole = kPiece * kPiece;  // places of a piece, and of a piece of pieces
-constexpr uint32_t kRowsOfGroup = 16;                       // rows of the table that a workgroup writes
 constexpr uint32_t kMostBins = 256;
 
 struct EmbedGradTask {
@@ -129,11 +136,29 @@ struct EmbedGradTask {
   float scale;
   uint32_t bits;          // of a row's number; the largest number they hold stands for no row
   uint32_t blocks;        // of kSorted tokens, of a worker
-  uint32_t groups;        // of rows of the table
-  uint32_t *row, *token;  // [worker][blocks kSorted]: sorted rows, and the token's number
+  uint32_t places;        // of a block that are written: those behind the last token hold no row
+  uint32_t each, groups;  // rows of the table that a workgroup writes, and how many such groups there are
+  uint32_t *row, *token;  // [worker][block][kSorted]: sorted rows, and the token's number
   uint32_t* begin;        // [worker][block][groups + 1]: where a group's rows begin in a block
-  float *piece, *whole;   // [worker][blocks kSorted / kPiece][cols], and / kWhole
+  float *piece, *whole;   // [worker][block][places / kPiece][2][cols], and / kWhole: of the run that comes in, and of the one that goes out; or null
+  bool past;              // dtable is written past the caches
 };
+
+// Where each group of rows begins in a block: the first place whose row is no less.
+__device__ __forceinline__ void groups_begin(const EmbedGradTask& p, uint32_t m, const uint32_t* keys, uint32_t places) {
+  for (uint32_t g = threadIdx.x; g <= p.groups; g += blockDim.x) {
+    const uint64_t want = min((uint64_t)g * p.each, p.vocabulary);
+    uint32_t low = 0u, high = places;
+    while (low < high) {
+      const uint32_t mid = (low + high) / 2;
+      if (keys[mid] < want)
+        low = mid + 1;
+      else
+        high = mid;
+    }
+    p.begin[((uint64_t)m * p.blocks + blockIdx.x) * (p.groups + 1) + g] = low;
+  }
+}
 
 // Least significant digits first, of 2^digit bins.  A wavefront takes consecutive places, 64 at a time: lanes of one digit find each other by ballots, and
 // the wavefront's counter of that digit says how many came before them.  That all is in one CU's LDS is what bounds it.
@@ -146,7 +171,7 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(EmbedGradTask 
   const uint32_t m = blockIdx.y, lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, bins = 1u << digit;
   const uint64_t first = (uint64_t)blockIdx.x * kSorted;
   const I* ids = static_cast<const I*>(p.ids.p) + m * p.ids.pitch;
-  const uint32_t none = p.bits < 32 ? (1u << p.bits) - 1u : ~0u, base = wave * (ITEMS * kWave) + lane;
+  const uint32_t none = (1u << p.bits) - 1u, base = wave * (ITEMS * kWave) + lane;
   uint32_t key[ITEMS], at[ITEMS], place[ITEMS];
 #pragma unroll
   for (int i = 0; i < ITEMS; ++i) {
@@ -220,113 +245,194 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(EmbedGradTask 
     p.row[to + base + i * kWave] = key[i];
     p.token[to + base + i * kWave] = (uint32_t)(first + at[i]);
   }
-  // where each group of rows begins: the first place whose row is no less
-  for (uint32_t g = threadIdx.x; g <= p.groups; g += kSortThreads) {
-    const uint64_t want = min((uint64_t)g * kRowsOfGroup, p.vocabulary);
-    uint32_t low = 0u, high = ITEMS * kSortThreads;
-    while (low < high) {
-      const uint32_t mid = (low + high) / 2;
-      if (keys[mid] < want)
-        low = mid + 1;
-      else
-        high = mid;
-    }
-    p.begin[((uint64_t)m * p.blocks + blockIdx.x) * (p.groups + 1) + g] = low;
-  }
+  groups_begin(p, m, keys, ITEMS * kSortThreads);
 }
 
-// Eight columns of the rows of `token`s first .. end - 1 added to sum, kMany rows on the way at a time.
-template <typename T, bool NARROW>
-__device__ __forceinline__ void add_rows(const T* dy, uint64_t ld, const uint32_t* token, uint32_t first, uint32_t end, uint64_t cols, float (&sum)[8]) {
-  constexpr uint32_t kMany = 8;
-  for (; first < end; first += kMany) {
-    Vec8<T> v[kMany];
+// The same of few tokens: each counts those that come before it.
+template <typename I>
+__global__ void __launch_bounds__(kFewSorted) embed_sort_few_kernel(EmbedGradTask p) {
+  typedef uint32_t four __attribute__((ext_vector_type(4)));
+  __shared__ __align__(16) uint32_t keys[kFewSorted];  // a row, and below it the token's place: no two are the same
+  __shared__ uint32_t sorted[kFewSorted];
+  const uint32_t m = blockIdx.y, t = threadIdx.x, none = (1u << p.bits) - 1u;
+  const I* ids = static_cast<const I*>(p.ids.p) + m * p.ids.pitch;
+  const uint32_t r = row_of<I>(ids, min((uint64_t)t, p.rows - 1) * p.ids.ld, p.vocabulary), row = t < p.rows && r < p.vocabulary ? r : none;
+  const uint32_t key = row * kFewSorted + t;
+  keys[t] = key;
+  __syncthreads();
+  uint32_t to = 0u;
+#pragma unroll 8
+  for (uint32_t j = 0; j < kFewSorted; j += 4) {
+    const four k = *reinterpret_cast<const four*>(keys + j);
 #pragma unroll
-    for (uint32_t k = 0; k < kMany; ++k) {  // (past the end: the last one again, which is not counted)
-      const T* row = dy + (uint64_t)token[min(first + k, end - 1)] * ld;
+    for (uint32_t n = 0; n < 4; ++n) to += k[n] < key ? 1u : 0u;
+  }
+  sorted[to] = row;
+  const uint64_t at = (uint64_t)m * kSorted + to;
+  p.row[at] = row;
+  p.token[at] = t;
+  __syncthreads();
+  groups_begin(p, m, sorted, kFewSorted);
+}
+static_assert(kFewSorted <= 256, "a row of 23 bits and a place of 8 are a key");
+
+// What a lane has of a row: Q times four columns, LANES fours apart, so that a wavefront's accesses have no gaps.  Where a row ends inside a four, the row's
+// last four are taken (what two lanes have of one column is the same).  NARROW: rows of less than four columns.
+template <int Q>
+struct Columns {
+  uint64_t at[Q];
+  bool has[Q];
+};
+template <int LANES, int Q, bool NARROW>
+__device__ __forceinline__ Columns<Q> columns_of(uint32_t chunk, uint32_t lane, uint64_t cols) {
+  Columns<Q> c;
+#pragma unroll
+  for (int q = 0; q < Q; ++q) {
+    c.at[q] = ((uint64_t)chunk * (LANES * Q) + q * LANES + lane) * 4;
+    c.has[q] = c.at[q] < cols;
+    c.at[q] = NARROW ? 0 : min(c.at[q], cols - 4);
+  }
+  return c;
+}
+
+template <typename T, int Q, bool NARROW>
+struct Some {
+  typedef T vec __attribute__((ext_vector_type(4), aligned(alignof(T))));
+  vec v[Q];
+  __device__ __forceinline__ void load(const T* row, const Columns<Q>& c, uint64_t cols) {
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
       if (NARROW) {
 #pragma unroll
-        for (uint32_t i = 0; i < 8; ++i) v[k][i] = i < cols ? row[i] : (T)0.f;
+        for (uint32_t i = 0; i < 4; ++i) v[q][i] = i < cols ? row[i] : (T)0.f;
       } else {
-        v[k] = *reinterpret_cast<GlobalPtr<Vec8<T>>>((GlobalPtr<T>)row);
+        v[q] = *reinterpret_cast<GlobalPtr<vec>>((GlobalPtr<T>)(row + c.at[q]));
       }
     }
+  }
+  __device__ __forceinline__ void add_to(float (&sum)[Q][4], bool counted) const {
 #pragma unroll
-    for (uint32_t k = 0; k < kMany; ++k)
+    for (int q = 0; q < Q; ++q)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) sum[i] += first + k < end ? (float)v[k][i] : 0.f;
+      for (int i = 0; i < 4; ++i) sum[q][i] += counted ? (float)v[q][i] : 0.f;
+  }
+};
+
+// Numbers f(0) .. f(count - 1), the same for a wavefront, many on the way at a time; past the end the last one again, which is not counted.
+template <int MANY, typename T, int Q, bool NARROW, typename F>
+__device__ __forceinline__ void add_many(F row, uint32_t& first, uint32_t count, const Columns<Q>& c, uint64_t cols, float (&sum)[Q][4]) {
+  Some<T, Q, NARROW> some[MANY];
+#pragma unroll
+  for (uint32_t k = 0; k < MANY; ++k) some[k].load(row(min(first + k, count - 1)), c, cols);
+#pragma unroll
+  for (uint32_t k = 0; k < MANY; ++k) some[k].add_to(sum, first + k < count);
+  first += MANY;
+}
+template <typename T, int Q, bool NARROW, typename F>
+__device__ __forceinline__ void add_all(F row, uint32_t count, const Columns<Q>& c, uint64_t cols, float (&sum)[Q][4]) {
+  constexpr int kMany = sizeof(T) == 4 ? 8 : 16;
+  uint32_t k = 0;
+  while (k + kMany / 2 < count) add_many<kMany, T, Q, NARROW>(row, k, count, c, cols, sum);
+  while (k < count) add_many<2, T, Q, NARROW>(row, k, count, c, cols, sum);
+}
+
+// The rows of dy of tokens first .. end - 1.  A wavefront reads 32 tokens at a time, a lane one.
+template <typename T, int Q, bool NARROW>
+__device__ __forceinline__ void add_rows(const T* dy, uint64_t ld, const uint32_t* token, uint32_t first, uint32_t end, const Columns<Q>& c, uint64_t cols,
+                                         float (&sum)[Q][4]) {
+  for (; first < end; first += kPiece) {
+    const uint32_t count = min(end - first, kPiece), mine = token[first + min(threadIdx.x % kPiece, count - 1)];
+    add_all<T, Q, NARROW>([&](uint32_t k) { return dy + (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)mine, (int)k) * ld; }, count, c, cols, sum);
   }
 }
 
-template <bool NARROW>
-__device__ __forceinline__ void add_parts(const float* part, uint64_t cols, uint32_t count, float (&sum)[8]) {
-  constexpr uint32_t kMany = 8;
-  for (uint32_t first = 0; first < count; first += kMany) {
-    Vec8<float> v[kMany];
+// Parts that lie `stride` apart.
+template <int Q, bool NARROW>
+__device__ __forceinline__ void add_parts(const float* part, uint64_t stride, uint32_t count, const Columns<Q>& c, uint64_t cols, float (&sum)[Q][4]) {
+  add_all<float, Q, NARROW>([&](uint32_t k) { return part + k * stride; }, count, c, cols, sum);
+}
+
+template <int Q, bool NARROW>
+__device__ __forceinline__ void store_sum(float* to, const Columns<Q>& c, uint64_t cols, const float (&sum)[Q][4], float scale, bool past) {
+  typedef float four __attribute__((ext_vector_type(4), aligned(4)));
 #pragma unroll
-    for (uint32_t k = 0; k < kMany; ++k) {
-      const float* row = part + (uint64_t)min(first + k, count - 1) * cols;
-      if (NARROW) {
+  for (int q = 0; q < Q; ++q) {
+    if (!c.has[q]) continue;
+    four v;
 #pragma unroll
-        for (uint32_t i = 0; i < 8; ++i) v[k][i] = i < cols ? row[i] : 0.f;
-      } else {
-        v[k] = *reinterpret_cast<GlobalPtr<Vec8<float>>>((GlobalPtr<float>)row);
-      }
+    for (uint32_t i = 0; i < 4; ++i) v[i] = sum[q][i] * scale;
+    if (NARROW) {
+#pragma unroll
+      for (uint32_t i = 0; i < 4; ++i)
+        if (i < cols) to[i] = v[i];
+    } else if (past) {
+      __builtin_nontemporal_store(v, reinterpret_cast<four*>(to + c.at[q]));
+    } else {
+      *reinterpret_cast<four*>(to + c.at[q]) = v;
     }
-#pragma unroll
-    for (uint32_t k = 0; k < kMany; ++k)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) sum[i] += first + k < count ? v[k][i] : 0.f;
   }
 }
 
-template <bool NARROW>
-__device__ __forceinline__ void store_sum(float* to, uint64_t cols, const float (&sum)[8], float scale) {
-  Vec8<float> v;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = sum[i] * scale;
-  if (NARROW) {
-#pragma unroll
-    for (uint32_t i = 0; i < 8; ++i)
-      if (i < cols) to[i] = v[i];
-  } else {
-    *reinterpret_cast<Vec8<float>*>(to) = v;
-  }
-}
-
-// Pieces (or pieces of pieces) that are all one row's: their sums.  The others are not looked at.
-template <typename T, bool WHOLE, bool NARROW>
+// The two runs that cross the ends of a piece (or of a piece of pieces): the sum of the one that comes in, as far as it goes, and of the one that
+// begins here and goes on.  LANES take a piece.
+template <typename T, bool WHOLE, int LANES, int Q, bool NARROW>
 __global__ void __launch_bounds__(kBlock) embed_pieces_kernel(EmbedGradTask p) {
   constexpr uint32_t kPlaces = WHOLE ? kWhole : kPiece;
-  const uint32_t m = blockIdx.z, number = blockIdx.x;
-  const uint64_t at = (uint64_t)m * p.blocks * kSorted, first = (uint64_t)number * kPlaces;
-  const uint32_t row = p.row[at + first];
-  if (row >= p.vocabulary || p.row[at + first + kPlaces - 1] != row) return;
-  uint64_t c = ((uint64_t)blockIdx.y * kBlock + threadIdx.x) * 8;
-  if (c >= p.cols) return;
-  if (!NARROW) c = min(c, p.cols - 8);
-  float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  const uint64_t pieces = (uint64_t)p.blocks * (kSorted / kPiece), wholes = (uint64_t)p.blocks * (kSorted / kWhole);
+  const uint32_t m = blockIdx.z, each = p.places / kPlaces, lane = threadIdx.x % LANES;
+  const uint32_t number = blockIdx.x * (kBlock / LANES) + __builtin_amdgcn_readfirstlane(threadIdx.x / LANES);
+  if (number >= p.blocks * each) return;
+  const uint32_t block = number / each, in = number - block * each, first = in * kPlaces;
+  const uint64_t all = ((uint64_t)m * p.blocks + block) * kSorted;
+  const uint32_t* row = p.row + all;
+  // (a row that is none is nobody's run)
+  const uint32_t before = first > 0u ? row[first - 1] : ~0u, after = first + kPlaces < p.places ? row[first + kPlaces] : ~0u;
+  uint32_t starts, ends;  // of a piece's places; of a piece of pieces, each piece's first place and its last
   if (WHOLE) {
-    add_parts<NARROW>(p.piece + (m * pieces + number * kPiece) * p.cols + c, p.cols, kPiece, sum);
-    store_sum<NARROW>(p.whole + (m * wholes + number) * p.cols + c, p.cols, sum, 1.f);
+    starts = row[first + threadIdx.x % kPiece * kPiece];
+    ends = row[first + threadIdx.x % kPiece * kPiece + kPiece - 1];
   } else {
-    add_rows<T, NARROW>(static_cast<const T*>(p.dy.p) + m * p.dy.pitch + c, p.dy.ld, p.token + at + first, 0, kPiece, p.cols, sum);
-    store_sum<NARROW>(p.piece + (m * pieces + number) * p.cols + c, p.cols, sum, 1.f);
+    starts = ends = row[first + threadIdx.x % kPiece];
+  }
+  const uint32_t coming = before < p.vocabulary ? __popc((uint32_t)__ballot(starts == before)) : 0u;
+  const uint32_t going = after < p.vocabulary && after != before ? __popc((uint32_t)__ballot(ends == after)) : 0u;
+  const Columns<Q> c = columns_of<LANES, Q, NARROW>(blockIdx.y, lane, p.cols);
+  const uint64_t stride = 2 * p.cols;
+  float* to = (WHOLE ? p.whole : p.piece) + ((uint64_t)m * p.blocks * each + number) * stride;
+  const float* piece = WHOLE ? p.piece + (((uint64_t)m * p.blocks + block) * (p.places / kPiece) + in * kPiece) * stride : nullptr;
+  const T* dy = static_cast<const T*>(p.dy.p) + m * p.dy.pitch;
+  const uint32_t* token = p.token + all + first;
+  if (coming > 0u) {
+    float sum[Q][4] = {};
+    if (WHOLE)
+      add_parts<Q, NARROW>(piece, stride, coming, c, p.cols, sum);
+    else
+      add_rows<T, Q, NARROW>(dy, p.dy.ld, token, 0, coming, c, p.cols, sum);
+    store_sum<Q, NARROW>(to, c, p.cols, sum, 1.f, false);
+  }
+  if (going > 0u) {
+    float sum[Q][4] = {};
+    if (WHOLE) {
+      const float* from = piece + (kPiece - going) * stride;
+      add_parts<Q, NARROW>(from + p.cols, stride, 1, c, p.cols, sum);
+      add_parts<Q, NARROW>(from + stride, stride, going - 1, c, p.cols, sum);
+    } else {
+      add_rows<T, Q, NARROW>(dy, p.dy.ld, token, kPiece - going, kPiece, c, p.cols, sum);
+    }
+    store_sum<Q, NARROW>(to + p.cols, c, p.cols, sum, 1.f, false);
   }
 }
 
-// Rows of the table, kRowsOfGroup for a workgroup, LANES for each at a time.  What it has to write bounds it.
-template <typename T, int LANES, bool NARROW>
+// Rows of the table, p.each for a workgroup, LANES for each at a time.  What it has to write bounds it.
+template <typename T, int LANES, int Q, bool NARROW>
 __global__ void __launch_bounds__(kBlock) embed_grad_kernel(EmbedGradTask p) {
   constexpr uint32_t kAtATime = kBlock / LANES;
-  extern __shared__ uint32_t bound[];  // [block][kRowsOfGroup + 1]: where each row's places begin
-  const uint32_t m = blockIdx.z, group = blockIdx.x, sub = threadIdx.x / LANES, lane = threadIdx.x % LANES;
-  const uint64_t v0 = (uint64_t)group * kRowsOfGroup;
-  const uint32_t rows = (uint32_t)min(p.vocabulary - v0, (uint64_t)kRowsOfGroup);
+  extern __shared__ uint32_t bound[];  // [block][each + 1]: where each row's places begin
+  const uint32_t m = blockIdx.z, group = blockIdx.x, sub = __builtin_amdgcn_readfirstlane(threadIdx.x / LANES), lane = threadIdx.x % LANES, bounds = p.each + 1;
+  const uint64_t v0 = (uint64_t)group * p.each;
+  const uint32_t rows = (uint32_t)min(p.vocabulary - v0, (uint64_t)p.each);
   const uint64_t all = (uint64_t)m * p.blocks * kSorted;
-  for (uint32_t k = threadIdx.x; k < p.blocks * (kRowsOfGroup + 1); k += kBlock) {
-    const uint32_t block = k / (kRowsOfGroup + 1), r = k - block * (kRowsOfGroup + 1);
+  for (uint32_t k = threadIdx.x; k < p.blocks * bounds; k += kBlock) {
+    const uint32_t block = k / bounds, r = k - block * bounds;
     const uint32_t* begin = p.begin + ((uint64_t)m * p.blocks + block) * (p.groups + 1) + group;
     const uint32_t* row = p.row + all + (uint64_t)block * kSorted;
     uint32_t low = begin[0], high = begin[1];
@@ -340,36 +446,27 @@ __global__ void __launch_bounds__(kBlock) embed_grad_kernel(EmbedGradTask p) {
     bound[k] = low;
   }
   __syncthreads();
-  uint64_t c = ((uint64_t)blockIdx.y * LANES + lane) * 8;
-  if (c >= p.cols) return;
-  if (!NARROW) c = min(c, p.cols - 8);
-  const T* dy = static_cast<const T*>(p.dy.p) + m * p.dy.pitch + c;
-  const uint64_t pieces = (uint64_t)p.blocks * (kSorted / kPiece), wholes = (uint64_t)p.blocks * (kSorted / kWhole);
+  const Columns<Q> c = columns_of<LANES, Q, NARROW>(blockIdx.y, lane, p.cols);
+  const T* dy = static_cast<const T*>(p.dy.p) + m * p.dy.pitch;
+  const uint64_t stride = 2 * p.cols;
   for (uint32_t r = sub; r < rows; r += kAtATime) {
-    float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    float sum[Q][4] = {};
     for (uint32_t block = 0; block < p.blocks; ++block) {
-      uint32_t a = bound[block * (kRowsOfGroup + 1) + r];
-      const uint32_t b = bound[block * (kRowsOfGroup + 1) + r + 1];
-      const uint32_t* token = p.token + all + (uint64_t)block * kSorted;
-      // tokens up to a whole piece, pieces up to a piece of pieces, those, and the same down again
-      const uint32_t piece_a = (a + kPiece - 1) / kPiece, piece_b = b / kPiece;
-      if (piece_a >= piece_b) {
-        add_rows<T, NARROW>(dy, p.dy.ld, token, a, b, p.cols, sum);
+      const uint32_t a = __builtin_amdgcn_readfirstlane(bound[block * bounds + r]), b = __builtin_amdgcn_readfirstlane(bound[block * bounds + r + 1]);
+      if (a == b) continue;
+      const uint32_t piece_a = a / kPiece, piece_b = (b - 1) / kPiece, whole_a = a / kWhole, whole_b = (b - 1) / kWhole;
+      if (p.piece == nullptr || piece_a == piece_b) {
+        add_rows<T, Q, NARROW>(dy, p.dy.ld, p.token + all + (uint64_t)block * kSorted, a, b, c, p.cols, sum);
         continue;
       }
-      add_rows<T, NARROW>(dy, p.dy.ld, token, a, piece_a * kPiece, p.cols, sum);
-      const float* piece = p.piece + (m * pieces + block * (kSorted / kPiece)) * p.cols + c;
-      const uint32_t whole_a = (piece_a + kPiece - 1) / kPiece, whole_b = piece_b / kPiece;
-      if (whole_a >= whole_b) {
-        add_parts<NARROW>(piece + (uint64_t)piece_a * p.cols, p.cols, piece_b - piece_a, sum);
-      } else {
-        add_parts<NARROW>(piece + (uint64_t)piece_a * p.cols, p.cols, whole_a * kPiece - piece_a, sum);
-        add_parts<NARROW>(p.whole + (m * wholes + block * (kSorted / kWhole) + whole_a) * p.cols + c, p.cols, whole_b - whole_a, sum);
-        add_parts<NARROW>(piece + (uint64_t)whole_b * kPiece * p.cols, p.cols, piece_b - whole_b * kPiece, sum);
-      }
-      add_rows<T, NARROW>(dy, p.dy.ld, token, piece_b * kPiece, b, p.cols, sum);
+      // the run goes out of its first piece (or piece of pieces), and comes into the others
+      const bool whole = whole_a != whole_b;
+      const uint32_t from = whole ? whole_a : piece_a, to = whole ? whole_b : piece_b, each = p.places / (whole ? kWhole : kPiece);
+      const float* part = (whole ? p.whole : p.piece) + (((uint64_t)m * p.blocks + block) * each + from) * stride;
+      add_parts<Q, NARROW>(part + p.cols, stride, 1, c, p.cols, sum);
+      add_parts<Q, NARROW>(part + stride, stride, to - from, c, p.cols, sum);
     }
-    store_sum<NARROW>(static_cast<float*>(p.dtable.p) + m * p.dtable.pitch + (v0 + r) * p.dtable.ld + c, p.cols, sum, p.scale);
+    store_sum<Q, NARROW>(static_cast<float*>(p.dtable.p) + m * p.dtable.pitch + (v0 + r) * p.dtable.ld, c, p.cols, sum, p.scale, p.past);
   }
 }
 
@@ -380,25 +477,39 @@ __global__ void __launch_bounds__(kBlock) embed_grad_nothing_kernel(uint64_t row
   static_cast<float*>(y.p)[blockIdx.y * y.pitch + r * y.ld + (e - r * cols)] = 0.f;
 }
 
+// How many of a block's places are written, and whether sums of pieces are taken (of few tokens no chain is long).
+uint32_t places_of(uint64_t rows) {
+  if (rows <= kFewSorted) return kFewSorted;
+  for (const uint32_t n : {1024u, 2048u, 4096u})
+    if (rows <= n) return n;
+  return kSorted;
+}
+constexpr uint64_t kPiecesFrom = 4 * kPiece;
+
 // What the gradient keeps, in words of 32 bits.
 uint64_t embed_grad_layout(EmbedGradTask& p, uint32_t workers, uint32_t* scratch) {
   p.blocks = (uint32_t)((p.rows + kSorted - 1) / kSorted);
-  p.groups = (uint32_t)((p.vocabulary + kRowsOfGroup - 1) / kRowsOfGroup);
+  p.places = places_of(p.rows);
+  // Where rows have tokens they take time one after another; where most have none, what a workgroup does before its first one counts.
+  p.each = p.rows * 4 >= p.vocabulary ? 4 : 16;
+  p.groups = (uint32_t)((p.vocabulary + p.each - 1) / p.each);
   p.bits = 1;
-  while (p.bits < 32 && p.vocabulary >> p.bits != 0) ++p.bits;
-  const uint64_t places = (uint64_t)workers * p.blocks * kSorted;
+  while (p.vocabulary >> p.bits != 0) ++p.bits;
+  const uint64_t blocks = (uint64_t)workers * p.blocks;
   uint64_t at = 0;
   auto take = [&](uint64_t words) {
     uint32_t* here = scratch + at;
     at += (words + 63) / 64 * 64;
     return here;
   };
-  p.row = take(places);
-  p.token = take(places);
-  p.begin = take((uint64_t)workers * p.blocks * (p.groups + 1));
-  const bool pieces = p.rows >= kPiece, wholes = p.rows >= kWhole;
-  p.piece = reinterpret_cast<float*>(take(pieces ? places / kPiece * p.cols : 0));
-  p.whole = reinterpret_cast<float*>(take(wholes ? places / kWhole * p.cols : 0));
+  p.row = take(blocks * kSorted);
+  p.token = take(blocks * kSorted);
+  p.begin = take(blocks * (p.groups + 1));
+  p.piece = p.whole = nullptr;
+  if (p.rows >= kPiecesFrom) {
+    p.piece = reinterpret_cast<float*>(take(blocks * (p.places / kPiece) * 2 * p.cols));
+    p.whole = reinterpret_cast<float*>(take(blocks * (p.places / kWhole) * 2 * p.cols));
+  }
   return at;
 }
 
@@ -407,41 +518,46 @@ void sort_typed(uint32_t workers, const EmbedGradTask& p, hipStream_t s) {
   const uint32_t passes = (p.bits + 7) / 8, digit = (p.bits + passes - 1) / passes;
   const dim3 grid(p.blocks, workers);
   auto launch = [&](auto items) { embed_sort_kernel<I, items><<<grid, kSortThreads, 0, s>>>(p, digit, passes); };
-  if (p.rows <= 1024)
-    launch(std::integral_constant<int, 1>{});
-  else if (p.rows <= 2048)
-    launch(std::integral_constant<int, 2>{});
-  else if (p.rows <= 4096)
-    launch(std::integral_constant<int, 4>{});
-  else
-    launch(std::integral_constant<int, 8>{});
+  switch (p.places) {
+    case kFewSorted: embed_sort_few_kernel<I><<<grid, kFewSorted, 0, s>>>(p); break;
+    case 1024: launch(std::integral_constant<int, 1>{}); break;
+    case 2048: launch(std::integral_constant<int, 2>{}); break;
+    case 4096: launch(std::integral_constant<int, 4>{}); break;
+    default: launch(std::integral_constant<int, 8>{});
+  }
 }
 
 template <typename T, bool NARROW>
 void embed_grad_typed(uint32_t workers, const EmbedGradTask& p, hipStream_t s) {
-  const uint64_t eights = (p.cols + 7) / 8;
-  const uint32_t across = (uint32_t)((eights + kBlock - 1) / kBlock);
-  // (places behind the last sorted ones of a short block are never written, and belong to no piece that is looked at)
-  const uint32_t places = (uint32_t)(p.rows <= 4096 ? (p.rows + kSortThreads - 1) / kSortThreads * kSortThreads : (uint64_t)p.blocks * kSorted);
-  if (p.rows >= kPiece) embed_pieces_kernel<T, false, NARROW><<<dim3(std::min<uint32_t>(places / kPiece, (uint32_t)(p.rows / kPiece) + 1), across, workers), kBlock, 0, s>>>(p);
-  if (p.rows >= kWhole) embed_pieces_kernel<T, true, NARROW><<<dim3(places / kWhole, across, workers), kBlock, 0, s>>>(p);
-  const size_t lds = p.blocks * (kRowsOfGroup + 1) * sizeof(uint32_t);
-  auto launch = [&](auto lanes) {
-    embed_grad_kernel<T, lanes, NARROW><<<dim3(p.groups, (uint32_t)((eights + lanes - 1) / lanes), workers), kBlock, lds, s>>>(p);
+  const size_t lds = p.blocks * (p.each + 1) * sizeof(uint32_t);
+  auto launch = [&](auto lanes, auto fours) {
+    const uint32_t across = (uint32_t)((p.cols + lanes * fours * 4 - 1) / (lanes * fours * 4)), at_a_time = kBlock / lanes;
+    const uint32_t pieces = p.blocks * (p.places / kPiece), wholes = p.blocks * (p.places / kWhole);
+    if (p.piece != nullptr) {
+      embed_pieces_kernel<T, false, lanes, fours, NARROW><<<dim3((pieces + at_a_time - 1) / at_a_time, across, workers), kBlock, 0, s>>>(p);
+      if (p.places > kWhole)
+        embed_pieces_kernel<T, true, lanes, fours, NARROW><<<dim3((wholes + at_a_time - 1) / at_a_time, across, workers), kBlock, 0, s>>>(p);
+    }
+    embed_grad_kernel<T, lanes, fours, NARROW><<<dim3(p.groups, across, workers), kBlock, lds, s>>>(p);
   };
-  if (eights <= 64)
-    launch(std::integral_constant<int, 64>{});
-  else if (eights <= 128)
-    launch(std::integral_constant<int, 128>{});
+  constexpr std::integral_constant<int, 1> one;
+  constexpr std::integral_constant<int, 2> two;
+  if (p.cols <= 256)
+    launch(std::integral_constant<int, 64>{}, one);
+  else if (p.cols <= 512)
+    launch(std::integral_constant<int, 64>{}, two);
+  else if (p.cols <= 1024)
+    launch(std::integral_constant<int, 128>{}, two);
   else
-    launch(std::integral_constant<int, 256>{});
+    launch(std::integral_constant<int, 256>{}, two);
 }
 
 }  // namespace
 
 hipError_t launch_embed(tng_type of_ids, tng_type of_table, tng_type type, uint32_t workers, uint64_t rows, uint64_t cols, uint64_t vocabulary,
                         const View& ids, const View& table, float scale, const View& y, hipStream_t s) {
-  EmbedTask p{rows, cols, 0, vocabulary, ids, table, y, scale};
+  EmbedTask p{rows, cols, 0, vocabulary, ids, table, y, scale, false};
+  p.past = (uint64_t)workers * rows * cols * (type == TNG_TYPE_F32 ? 4 : 2) > kPast;
   if (of_ids == TNG_TYPE_I32)
     embed_from<int32_t>(of_table, type, workers, p, s);
   else
@@ -471,6 +587,7 @@ hipError_t launch_embed_grad(tng_type of_ids, tng_type type, uint32_t workers, u
   p.dy = dy;
   p.dtable = dtable;
   p.scale = scale;
+  p.past = (uint64_t)workers * vocabulary * cols * sizeof(float) > kPast;
   embed_grad_layout(p, workers, scratch);
   if (of_ids == TNG_TYPE_I32)
     sort_typed<int32_t>(workers, p, s);
@@ -483,7 +600,7 @@ hipError_t launch_embed_grad(tng_type of_ids, tng_type type, uint32_t workers, u
       default: embed_grad_typed<f16_t, narrow>(workers, p, s); break;
     }
   };
-  if (cols < 8)
+  if (cols < 4)
     grad(std::true_type{});
   else
     grad(std::false_type{});
