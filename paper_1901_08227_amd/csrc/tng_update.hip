@@ -154,6 +154,8 @@ struct PairTask {
   Pairs by_r, by_c;         // results as rows of r, and turned, as rows of c
   View y;                   // kLast: rows of c
   float scale;
+  uint32_t full, splits;  // tiles before number `full` are made whole, the others by `splits` workgroups each, and joined
+  float* part;            // [tile from full on][split][kRows kCols]
 };
 
 // The tile of a number, in columns of kGroup tiles of rows, which are about square; HALF: only tiles with c <= r.
@@ -190,6 +192,8 @@ __device__ __forceinline__ uint32_t number_of(uint32_t block, uint32_t all) {
   return die * each + min(die, more) + block / kDies;
 }
 
+constexpr uint32_t turn_pitch(int tiles) { return tiles * 16 + 4; }
+
 // A wavefront makes RN x CN tiles of 16 x 16 results, WR x WC of them a workgroup's tile.  A stage is 32 columns of the operands' rows, 128 bytes each; SLOTS of them lie
 // in LDS.  While the products of a stage run, the next one's fragments are read into registers, and the loads of the stage that follows the last one in LDS
 // are asked for, in the place of the one that has been read: one wait and one barrier a stage.
@@ -200,48 +204,229 @@ struct PairKernel {
   static constexpr int kLoads = (kRows + kCols) / 8 / kWaves, kLoadsOfA = kRows / 8 / kWaves;
   static_assert(kRows % (8 * kWaves) == 0 && kCols % (8 * kWaves) == 0, "loads divide evenly");
   // Behind the stages: the results of 32 rows of each wavefront at a time, turned.  (Four words more a row: a wavefront's four groups of rows meet in no bank.)
-  static constexpr int kTurnPitch = CN * 16 + 4, kTurnBytes = 32 * kTurnPitch * 4;
+  static constexpr int kTurnBytes = 32 * turn_pitch(CN) * 4;
   static_assert(RN % 2 == 0 && kTurnBytes * kWaves <= kRing, "results are turned in the stages' place");
 };
+
+// What becomes of two tiles of rows, from r_first on, of a wavefront's results; turn: its place in LDS.  both: results go both ways round.
+template <typename T, int END, int CN>
+__device__ __forceinline__ void finish_rows(const PairTask& p, uint32_t plane, bool both, uint32_t r_first, uint32_t c_first, const v4f (&sum)[2][CN],
+                                            uint32_t* turn, uint32_t lane) {
+  constexpr uint32_t kPitch = turn_pitch(CN);
+  // A lane has four results of consecutive r for one c.
+  const uint32_t i = lane % 16, r_in = r_first + lane / 16 * 4, c_in = c_first + i;
+  const uint32_t end_r = (p.rows + kBlockCols - 1) / kBlockCols * kBlockCols, end_c = (p.cols + kBlockCols - 1) / kBlockCols * kBlockCols;
+#pragma unroll
+  for (int a = 0; a < 2; ++a)
+#pragma unroll
+    for (int b = 0; b < CN; ++b) {
+      const uint32_t r = r_in + a * 16, c = c_in + b * 16;
+      float v[4];
+      if (END == kLast) {
+        if (r >= p.rows || c >= p.cols) continue;
+#pragma unroll
+        for (int n = 0; n < 4; ++n) v[n] = sum[a][b][n] * p.scale;
+        store_n_within<T, 4>(static_cast<T*>(p.y.p) + plane * p.y.pitch + c * p.y.ld + r, p.rows - r, v);
+        continue;
+      }
+      const bool in = c < p.cols && r < end_r;
+      if (END == kPoly) {
+        v4h g_high = {}, g_low = {};
+        if (in) {
+          const char* at = p.gram.p + plane * p.gram.pitch + c * p.gram.ld + pair_at(r);
+          g_high = *reinterpret_cast<const v4h*>(at);
+          g_low = *reinterpret_cast<const v4h*>(at + 64);
+        }
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+          const float gram = ((float)g_high[n] + (float)g_low[n]) * (1.f / kOfGram), square = sum[a][b][n] * (1.f / (kOfGram * kOfGram));
+          v[n] = (p.times * gram + p.square * square + (r + n == c ? p.plus : 0.f)) * kOfPoly;
+        }
+      } else {
+        constexpr float kUnit = END == kGram ? kOfGram / (kOfX * kOfX) : kOfX / (kOfPoly * kOfX);
+#pragma unroll
+        for (int n = 0; n < 4; ++n) v[n] = sum[a][b][n] * kUnit;
+      }
+      v4h high, low;
+#pragma unroll
+      for (int n = 0; n < 4; ++n) {
+        f16_t h, l;
+        split(r + n < p.rows && c < p.cols ? v[n] : 0.f, h, l);
+        high[n] = h;
+        low[n] = l;
+        if (both)
+          turn[(a * 16 + lane / 16 * 4 + n) * kPitch + b * 16 + i] =
+              (uint32_t)__builtin_bit_cast(uint16_t, h) | (uint32_t)__builtin_bit_cast(uint16_t, l) << 16;
+      }
+      if (in) {
+        char* at = p.by_c.p + plane * p.by_c.pitch + c * p.by_c.ld + pair_at(r);
+        *reinterpret_cast<v4h*>(at) = high;
+        *reinterpret_cast<v4h*>(at + 64) = low;
+      }
+    }
+  if (END == kLast || !both) return;
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (a wavefront's own: what its lanes have written is there)
+  constexpr uint32_t kEights = CN * 2;                // of a row
+  static_assert(32 * kEights % kWave == 0, "a row's eights are divided evenly");
+#pragma unroll
+  for (uint32_t piece = 0; piece < 32 * kEights; piece += kWave) {
+    const uint32_t row = (piece + lane) / kEights, eight = (piece + lane) % kEights, r = r_first + row, c = c_first + eight * 8;
+    const uint32_t* from = turn + row * kPitch + eight * 8;
+    typedef uint32_t four __attribute__((ext_vector_type(4)));
+    const four w0 = *reinterpret_cast<const four*>(from), w1 = *reinterpret_cast<const four*>(from + 4);
+    four high, low;
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      high[n] = __builtin_amdgcn_perm(w0[2 * n + 1], w0[2 * n], 0x05040100u);
+      low[n] = __builtin_amdgcn_perm(w0[2 * n + 1], w0[2 * n], 0x07060302u);
+      high[n + 2] = __builtin_amdgcn_perm(w1[2 * n + 1], w1[2 * n], 0x05040100u);
+      low[n + 2] = __builtin_amdgcn_perm(w1[2 * n + 1], w1[2 * n], 0x07060302u);
+    }
+    if (r < p.rows && c < end_c) {
+      char* at = p.by_r.p + plane * p.by_r.pitch + r * p.by_r.ld + pair_at(c);
+      *reinterpret_cast<four*>(at) = high;
+      *reinterpret_cast<four*>(at + 64) = low;
+    }
+  }
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+}
+
+// What a workgroup does: a tile, or a piece of the depth of one, whose sums go to p.part.
+struct Work {
+  uint32_t plane, first, stages;
+  int part;  // -1: the whole tile
+  Place place;
+};
+template <typename K, bool HALF>
+__device__ __forceinline__ Work work_of(const PairTask& p) {
+  const uint32_t down = (p.rows + K::kRows - 1) / K::kRows, across = (p.cols + K::kCols - 1) / K::kCols, each = HALF ? down * (down + 1) / 2 : down * across;
+  Work w{0, 0, p.stages, -1, {}};
+  uint32_t number;
+  if (blockIdx.x < p.full) {
+    number = number_of(blockIdx.x, p.full);
+  } else {
+    w.part = (int)(blockIdx.x - p.full);
+    const uint32_t tile = (uint32_t)w.part / p.splits, s = (uint32_t)w.part - tile * p.splits;
+    number = p.full + tile;
+    w.first = p.stages * s / p.splits;
+    w.stages = p.stages * (s + 1) / p.splits - w.first;
+  }
+  w.plane = number / each;
+  w.place = place_of<HALF>(number - w.plane * each, down, across);
+  return w;
+}
+
+// What becomes of a workgroup's sums.  lds: of the stages, which nobody reads any more.
+template <typename T, int END, typename K, int RN, int CN, int WC>
+__device__ __forceinline__ void finish_tile(const PairTask& p, const Work& w, const v4f (&sum)[RN][CN], char* lds, uint32_t lane, uint32_t wave) {
+  if (w.part >= 0) {  // as they lie in the registers
+    float* to = p.part + (uint64_t)w.part * (K::kRows * K::kCols) + wave * (RN * CN * 256) + lane * 4;
+#pragma unroll
+    for (int a = 0; a < RN; ++a)
+#pragma unroll
+      for (int b = 0; b < CN; ++b) *reinterpret_cast<v4f*>(to + (a * CN + b) * 256) = sum[a][b];
+    return;
+  }
+  const bool both = !(END == kGram || END == kPoly) || w.place.r != w.place.c;
+  uint32_t* turn = reinterpret_cast<uint32_t*>(lds + wave * K::kTurnBytes);
+#pragma unroll
+  for (int a = 0; a < RN; a += 2) {
+    v4f two[2][CN];
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int b = 0; b < CN; ++b) two[k][b] = sum[a + k][b];
+    finish_rows<T, END, CN>(p, w.plane, both, w.place.r * K::kRows + (wave / WC * RN + a) * 16, w.place.c * K::kCols + wave % WC * CN * 16, two, turn, lane);
+  }
+}
+
+// Pieces of a tile's depth joined, in their order, two tiles of rows of each wavefront.
+template <typename T, int END, int RN, int CN, int WR, int WC>
+__global__ void __launch_bounds__(WR* WC* kWave) pair_join_kernel(PairTask p) {
+  using K = PairKernel<RN, CN, WR, WC, 2>;
+  constexpr bool kHalf = END == kGram || END == kPoly;
+  __shared__ __align__(16) char lds[K::kTurnBytes * K::kWaves];
+  const uint32_t lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), a = blockIdx.y * 2;
+  const uint32_t down = (p.rows + K::kRows - 1) / K::kRows, across = (p.cols + K::kCols - 1) / K::kCols, each = kHalf ? down * (down + 1) / 2 : down * across;
+  const uint32_t number = p.full + blockIdx.x, plane = number / each;
+  const Place place = place_of<kHalf>(number - plane * each, down, across);
+  v4f sum[2][CN] = {};
+  const float* from = p.part + (uint64_t)blockIdx.x * p.splits * (K::kRows * K::kCols) + wave * (RN * CN * 256) + a * CN * 256 + lane * 4;
+  for (uint32_t s = 0; s < p.splits; ++s, from += K::kRows * K::kCols)
+#pragma unroll
+    for (int k = 0; k < 2 * CN; ++k) sum[k / CN][k % CN] += *reinterpret_cast<const v4f*>(from + k * 256);
+  finish_rows<T, END, CN>(p, plane, !kHalf || place.r != place.c, place.r * K::kRows + (wave / WC * RN + a) * 16, place.c * K::kCols + wave % WC * CN * 16, sum,
+                          reinterpret_cast<uint32_t*>(lds + wave * K::kTurnBytes), lane);
+}
+
+// 16 bytes for each lane to LDS, as load_to_lds; from: bytes more, the same for all lanes.
+__device__ __forceinline__ void load_rows_to_lds(uint64_t base, uint32_t bytes, uint32_t offset, uint32_t from, uint32_t lds) {
+  const v4u rsrc = {(uint32_t)base, (uint32_t)(base >> 32) & 0xFFFFu, bytes, 0x00020000u};
+  asm volatile(
+      "s_mov_b32 m0, %0\n\t"
+      "s_nop 3\n\t"
+      "buffer_load_dwordx4 %1, %2, %3 offen lds"
+      :
+      : "s"(lds), "v"(offset), "s"(rsrc), "s"(from)
+      : "memory");
+}
+
+// A workgroup's operands: number j of a wavefront's loads takes 8 rows, a row eight lanes.  Rows behind the last one, and stages behind the last one, are out
+// of bounds: nothing is read, and what the loads clear belongs to no result.
+template <typename K>
+struct Operands {
+  uint64_t a, b;
+  uint32_t bytes_a, bytes_b, offset_a, offset_b, step_a, step_b, lds;
+  int left;  // stages not asked for
+  __device__ __forceinline__ Operands(const PairTask& p, const Work& w, uint32_t lane, uint32_t wave, const char* at) {
+    const uint32_t r0 = w.place.r * K::kRows, c0 = w.place.c * K::kCols;
+    a = reinterpret_cast<uint64_t>(p.a.p) + w.plane * p.a.pitch + r0 * p.a.ld + w.first * 128ull;
+    b = reinterpret_cast<uint64_t>(p.b.p) + w.plane * p.b.pitch + c0 * p.b.ld + w.first * 128ull;
+    bytes_a = (min(p.rows - r0, (uint32_t)K::kRows) - 1) * (uint32_t)p.a.ld + w.stages * 128u;
+    bytes_b = (min(p.cols - c0, (uint32_t)K::kCols) - 1) * (uint32_t)p.b.ld + w.stages * 128u;
+    const uint32_t r = wave * 8 + lane / 8, in_row = (lane % 8 ^ (r >> 1 & 7u)) * 16;  // (rows that loads are apart do not change what pieces are moved by)
+    offset_a = r * (uint32_t)p.a.ld + in_row;
+    offset_b = r * (uint32_t)p.b.ld + in_row;
+    step_a = K::kWaves * 8 * (uint32_t)p.a.ld;
+    step_b = K::kWaves * 8 * (uint32_t)p.b.ld;
+    left = (int)w.stages;
+    lds = (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const char*)at) + wave * 1024;
+  }
+  __device__ __forceinline__ void load(int j, uint32_t slot) const {
+    const bool of_a = j < K::kLoadsOfA;
+    load_rows_to_lds(of_a ? a : b, left > 0 ? (of_a ? bytes_a : bytes_b) : 0u, of_a ? offset_a : offset_b, of_a ? j * step_a : (j - K::kLoadsOfA) * step_b,
+                     lds + slot + j * K::kWaves * 1024);
+  }
+  __device__ __forceinline__ void next() {
+    --left;
+    a += 128;
+    b += 128;
+    bytes_a -= 128;
+    bytes_b -= 128;
+  }
+};
+
+// One tile of rows times the columns' tiles: three products of each pair.
+template <int CN>
+__device__ __forceinline__ void multiply(v4f (&sum)[CN], const v8h (&a)[2], const v8h (&b)[CN][2]) {
+#pragma unroll
+  for (int k = 0; k < CN; ++k) sum[k] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[0], b[k][1], sum[k], 0, 0, 0);
+#pragma unroll
+  for (int k = 0; k < CN; ++k) sum[k] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[1], b[k][0], sum[k], 0, 0, 0);
+#pragma unroll
+  for (int k = 0; k < CN; ++k) sum[k] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[0], b[k][0], sum[k], 0, 0, 0);
+  __builtin_amdgcn_sched_barrier(0);
+}
 
 template <typename T, int END, int RN, int CN, int WR, int WC, int SLOTS>
 __global__ void __launch_bounds__(WR* WC* kWave) pair_kernel(PairTask p) {
   using K = PairKernel<RN, CN, WR, WC, SLOTS>;
   constexpr bool kHalf = END == kGram || END == kPoly;
   __shared__ __align__(1024) char lds[K::kRing];
-  const uint32_t lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), wr = wave / WC, wc = wave % WC;
-  const uint32_t lds0 = (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)lds);
-  const uint32_t down = (p.rows + K::kRows - 1) / K::kRows, across = (p.cols + K::kCols - 1) / K::kCols;
-  const uint32_t each = kHalf ? down * (down + 1) / 2 : down * across, number = number_of(blockIdx.x, each * p.planes), plane = number / each;
-  const Place place = place_of<kHalf>(number - plane * each, down, across);
-  const uint32_t r0 = place.r * K::kRows, c0 = place.c * K::kCols;
-
-  // number j of a wavefront's loads takes 8 rows, a row eight lanes; past the last stage nothing is read, and what the loads clear is not looked at
-  uint64_t base_a = reinterpret_cast<uint64_t>(p.a.p) + plane * p.a.pitch + r0 * p.a.ld, base_b = reinterpret_cast<uint64_t>(p.b.p) + plane * p.b.pitch + c0 * p.b.ld;
-  const uint32_t rows = min(p.rows - r0, (uint32_t)K::kRows), cols = min(p.cols - c0, (uint32_t)K::kCols);
-  uint32_t bytes_a = (rows - 1) * (uint32_t)p.a.ld + p.stages * 128u, bytes_b = (cols - 1) * (uint32_t)p.b.ld + p.stages * 128u;
-  uint32_t offset[K::kLoads];
-#pragma unroll
-  for (int j = 0; j < K::kLoads; ++j) {
-    const bool of_a = j < K::kLoadsOfA;
-    const uint32_t r = ((of_a ? j : j - K::kLoadsOfA) * K::kWaves + wave) * 8 + lane / 8;
-    offset[j] = min(r, (of_a ? rows : cols) - 1) * (uint32_t)(of_a ? p.a.ld : p.b.ld) + (lane % 8 ^ (r >> 1 & 7u)) * 16;
-  }
-  int ahead = (int)p.stages;  // stages not asked for
-  auto load_one = [&](int j, uint32_t slot) {
-    const bool of_a = j < K::kLoadsOfA;
-    load_to_lds(of_a ? base_a : base_b, ahead > 0 ? (of_a ? bytes_a : bytes_b) : 0u, offset[j], lds0 + slot + (j * K::kWaves + wave) * 1024);
-  };
-  auto asked_one = [&]() {
-    --ahead;
-    base_a += 128;
-    base_b += 128;
-    bytes_a -= 128;
-    bytes_b -= 128;
-  };
-
+  const uint32_t lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), wr = wave / WC, wc = wave % WC, i = lane % 16;
+  const Work w = work_of<K, kHalf>(p);
+  Operands<K> of(p, w, lane, wave, lds);
   // Where a lane reads its rows' pieces; the low parts are four pieces on.
-  const uint32_t i = lane % 16;
   const uint32_t at_a = (wr * RN * 16 + i) * 128 + (lane / 16 ^ (i >> 1 & 7u)) * 16;
   const uint32_t at_b = (K::kRows + wc * CN * 16 + i) * 128 + (lane / 16 ^ (i >> 1 & 7u)) * 16;
   struct Fragments {
@@ -260,12 +445,11 @@ __global__ void __launch_bounds__(WR* WC* kWave) pair_kernel(PairTask p) {
   for (int a = 0; a < RN; ++a)
 #pragma unroll
     for (int b = 0; b < CN; ++b) sum[a][b] = v4f{0.f, 0.f, 0.f, 0.f};
-
 #pragma unroll
   for (int k = 0; k < SLOTS; ++k) {
 #pragma unroll
-    for (int j = 0; j < K::kLoads; ++j) load_one(j, k * K::kStageBytes);
-    asked_one();
+    for (int j = 0; j < K::kLoads; ++j) of.load(j, k * K::kStageBytes);
+    of.next();
   }
   Fragments even, odd;
   wait_and_meet<(SLOTS - 1) * K::kLoads>();
@@ -285,127 +469,159 @@ __global__ void __launch_bounds__(WR* WC* kWave) pair_kernel(PairTask p) {
 #pragma unroll
       for (int k = g * kReads; k < (g + 1) * kReads && k < CN; ++k) read_b(then, k, next);
 #pragma unroll
-      for (int j = g * kAsks; j < (g + 1) * kAsks && j < K::kLoads; ++j) load_one(j, slot);
-#pragma unroll
-      for (int b = 0; b < CN; ++b) sum[g][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(now.a[g][0], now.b[b][1], sum[g][b], 0, 0, 0);
-#pragma unroll
-      for (int b = 0; b < CN; ++b) sum[g][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(now.a[g][1], now.b[b][0], sum[g][b], 0, 0, 0);
-#pragma unroll
-      for (int b = 0; b < CN; ++b) sum[g][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(now.a[g][0], now.b[b][0], sum[g][b], 0, 0, 0);
-      __builtin_amdgcn_sched_barrier(0);
+      for (int j = g * kAsks; j < (g + 1) * kAsks && j < K::kLoads; ++j) of.load(j, slot);
+      multiply<CN>(sum[g], now.a[g], now.b);
     }
-    asked_one();
+    of.next();
     slot = next;
   };
   uint32_t k = 0;
-  for (; k + 2 <= p.stages; k += 2) {
+  for (; k + 2 <= w.stages; k += 2) {
     stage(even, odd);
     stage(odd, even);
   }
-  if (k < p.stages) stage(even, odd);
+  if (k < w.stages) stage(even, odd);
   wait_and_meet<0>();  // (the loads that found nothing are done, and LDS is read everywhere)
+  finish_tile<T, END, K, RN, CN, WC>(p, w, sum, lds, lane, wave);
+}
 
-  // A lane has four results of consecutive r for one c.
-  const uint32_t r_in = r0 + wr * RN * 16 + lane / 16 * 4, c_in = c0 + wc * CN * 16 + i;
-  if (END == kLast) {
+// The same with tiles whose wavefronts have no registers for a second stage's fragments of the rows: those are read two groups ahead.  Before the last two groups
+// of a stage nothing of it is left in LDS to read, and all meet: the next stage is there, and the place of this one is free.  EARLY: loads after each
+// of the last two groups; the others follow the first groups of the next stage.
+template <typename T, int END, int RN, int CN, int WR, int WC, int SLOTS, int EARLY>
+__global__ void __launch_bounds__(WR* WC* kWave) pair_large_kernel(PairTask p) {
+  using K = PairKernel<RN, CN, WR, WC, SLOTS>;
+  constexpr bool kHalf = END == kGram || END == kPoly;
+  constexpr int kAhead = 2, kRingOfA = RN % 4 == 0 ? 4 : 3, kMeet = RN - kAhead, kFirst = kAhead * EARLY, kLate = (K::kLoads - kFirst + kMeet - 1) / kMeet;
+  static_assert(RN % kRingOfA == 0 && kFirst <= K::kLoads, "fragments and loads divide evenly");
+  __shared__ __align__(1024) char lds[K::kRing];
+  const uint32_t lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), wr = wave / WC, wc = wave % WC, i = lane % 16;
+  const Work w = work_of<K, kHalf>(p);
+  Operands<K> of(p, w, lane, wave, lds);
+  const uint32_t at_a = (wr * RN * 16 + i) * 128 + (lane / 16 ^ (i >> 1 & 7u)) * 16;
+  const uint32_t at_b = (K::kRows + wc * CN * 16 + i) * 128 + (lane / 16 ^ (i >> 1 & 7u)) * 16;
+  v8h a[kRingOfA][2], b[2][CN][2];
+  auto read_a = [&](int g, uint32_t slot) {
+    a[g % kRingOfA][0] = *reinterpret_cast<const v8h*>(lds + slot + at_a + g % RN * 2048);
+    a[g % kRingOfA][1] = *reinterpret_cast<const v8h*>(lds + slot + (at_a ^ 64u) + g % RN * 2048);
+  };
+  auto read_b = [&](int set, int k, uint32_t slot) {
+    b[set][k][0] = *reinterpret_cast<const v8h*>(lds + slot + at_b + k * 2048);
+    b[set][k][1] = *reinterpret_cast<const v8h*>(lds + slot + (at_b ^ 64u) + k * 2048);
+  };
+  v4f sum[RN][CN];
 #pragma unroll
-    for (int a = 0; a < RN; ++a)
+  for (int k = 0; k < RN; ++k)
 #pragma unroll
-      for (int b = 0; b < CN; ++b) {
-        const uint32_t r = r_in + a * 16, c = c_in + b * 16;
-        if (r >= p.rows || c >= p.cols) continue;
-        float v[4];
+    for (int n = 0; n < CN; ++n) sum[k][n] = v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int n = 0; n < 4; ++n) v[n] = sum[a][b][n] * p.scale;
-        store_n_within<T, 4>(static_cast<T*>(p.y.p) + plane * p.y.pitch + c * p.y.ld + r, p.rows - r, v);
-      }
-    return;
+  for (int k = 0; k < SLOTS - 1; ++k) {
+#pragma unroll
+    for (int j = 0; j < K::kLoads; ++j) of.load(j, k * K::kStageBytes);
+    of.next();
   }
-  const uint32_t end_r = (p.rows + kBlockCols - 1) / kBlockCols * kBlockCols, end_c = (p.cols + kBlockCols - 1) / kBlockCols * kBlockCols;
-  const bool both = !kHalf || place.r != place.c;
-  uint32_t* turn = reinterpret_cast<uint32_t*>(lds + wave * K::kTurnBytes);
 #pragma unroll
-  for (int half = 0; half < RN; half += 2) {
+  for (int j = 0; j < kFirst; ++j) of.load(j, (SLOTS - 1) * K::kStageBytes);
+  wait_and_meet<(SLOTS - 2) * K::kLoads + kFirst>();
 #pragma unroll
-    for (int a = half; a < half + 2; ++a)
+  for (int k = 0; k < CN; ++k) read_b(0, k, 0);
 #pragma unroll
-      for (int b = 0; b < CN; ++b) {
-        const uint32_t r = r_in + a * 16, c = c_in + b * 16;
-        const bool in = c < p.cols && r < end_r;
-        v4h high, low;
-        float v[4];
-        if (END == kPoly) {
-          v4h g_high = {}, g_low = {};
-          if (in) {
-            const char* at = p.gram.p + plane * p.gram.pitch + c * p.gram.ld + pair_at(r);
-            g_high = *reinterpret_cast<const v4h*>(at);
-            g_low = *reinterpret_cast<const v4h*>(at + 64);
-          }
+  for (int k = 0; k < kAhead; ++k) read_a(k, 0);
+  uint32_t here = 0;
+  auto stage = [&](int set) {
+    const uint32_t next = here + K::kStageBytes == K::kRing ? 0u : here + K::kStageBytes, before = here == 0u ? K::kRing - K::kStageBytes : here - K::kStageBytes;
 #pragma unroll
-          for (int n = 0; n < 4; ++n) {
-            const float gram = ((float)g_high[n] + (float)g_low[n]) * (1.f / kOfGram), square = sum[a][b][n] * (1.f / (kOfGram * kOfGram));
-            v[n] = (p.times * gram + p.square * square + (r + n == c ? p.plus : 0.f)) * kOfPoly;
-          }
-        } else {
-          constexpr float kUnit = END == kGram ? kOfGram / (kOfX * kOfX) : kOfX / (kOfPoly * kOfX);
+    for (int g = 0; g < kMeet; ++g) {
+      read_a(g + kAhead, here);
 #pragma unroll
-          for (int n = 0; n < 4; ++n) v[n] = sum[a][b][n] * kUnit;
-        }
-#pragma unroll
-        for (int n = 0; n < 4; ++n) {
-          f16_t h, l;
-          split(r + n < p.rows && c < p.cols ? v[n] : 0.f, h, l);
-          high[n] = h;
-          low[n] = l;
-          if (both)
-            turn[((a - half) * 16 + lane / 16 * 4 + n) * K::kTurnPitch + b * 16 + i] =
-                (uint32_t)__builtin_bit_cast(uint16_t, h) | (uint32_t)__builtin_bit_cast(uint16_t, l) << 16;
-        }
-        if (in) {
-          char* at = p.by_c.p + plane * p.by_c.pitch + c * p.by_c.ld + pair_at(r);
-          *reinterpret_cast<v4h*>(at) = high;
-          *reinterpret_cast<v4h*>(at + 64) = low;
-        }
-      }
-    if (!both) continue;
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (a wavefront's own: what its lanes have written is there)
-    constexpr uint32_t kEights = CN * 2;  // of a row
-#pragma unroll
-    for (uint32_t piece = 0; piece < 32 * kEights; piece += kWave) {
-      const uint32_t row = (piece + lane) / kEights, eight = (piece + lane) % kEights;
-      const uint32_t r = r0 + (wr * RN + half) * 16 + row, c = c0 + wc * CN * 16 + eight * 8;
-      const uint32_t* from = turn + row * K::kTurnPitch + eight * 8;
-      typedef uint32_t four __attribute__((ext_vector_type(4)));
-      const four w0 = *reinterpret_cast<const four*>(from), w1 = *reinterpret_cast<const four*>(from + 4);
-      four high, low;
-#pragma unroll
-      for (int n = 0; n < 2; ++n) {
-        high[n] = __builtin_amdgcn_perm(w0[2 * n + 1], w0[2 * n], 0x05040100u);
-        low[n] = __builtin_amdgcn_perm(w0[2 * n + 1], w0[2 * n], 0x07060302u);
-        high[n + 2] = __builtin_amdgcn_perm(w1[2 * n + 1], w1[2 * n], 0x05040100u);
-        low[n + 2] = __builtin_amdgcn_perm(w1[2 * n + 1], w1[2 * n], 0x07060302u);
-      }
-      if (r < p.rows && c < end_c) {
-        char* at = p.by_r.p + plane * p.by_r.pitch + r * p.by_r.ld + pair_at(c);
-        *reinterpret_cast<four*>(at) = high;
-        *reinterpret_cast<four*>(at + 64) = low;
-      }
+      for (int j = kFirst + g * kLate; j < kFirst + (g + 1) * kLate && j < K::kLoads; ++j) of.load(j, before);
+      multiply<CN>(sum[g], a[g % kRingOfA], b[set]);
     }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    of.next();
+    wait_and_meet<(SLOTS - 2) * K::kLoads>();
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int g = kMeet; g < RN; ++g) {
+      read_a(g + kAhead, next);
+#pragma unroll
+      for (int k = (g - kMeet) * CN / kAhead; k < (g - kMeet + 1) * CN / kAhead; ++k) read_b(1 - set, k, next);
+#pragma unroll
+      for (int j = (g - kMeet) * EARLY; j < (g - kMeet + 1) * EARLY; ++j) of.load(j, here);
+      multiply<CN>(sum[g], a[g % kRingOfA], b[set]);
+    }
+    here = next;
+  };
+  uint32_t k = 0;
+  for (; k + 2 <= w.stages; k += 2) {
+    stage(0);
+    stage(1);
   }
+  if (k < w.stages) stage(0);
+  wait_and_meet<0>();
+  finish_tile<T, END, K, RN, CN, WC>(p, w, sum, lds, lane, wave);
+}
+
+// The tiles that there are: how many run at a time, what one takes for a stage while as many do, and while no CU has two of them, and what it takes
+// besides (us; from products of 64 to 4096 rows, 64 to 4096 deep).
+struct Shape {
+  uint32_t side, slots;
+  double stage, alone, rest;
+};
+constexpr uint32_t kCus = 256;
+constexpr Shape kShapes[] = {{256, 256, 2.0, 2.0, 10.}, {192, 256, 1.25, 1.25, 9.}, {128, 256, 0.55, 0.55, 8.}, {64, 512, 0.34, 0.25, 4.}};
+
+// How a product is made: whatever tiles, and pieces of the tiles that would have the chip to themselves at the end, an estimate of the time says.  (Four
+// steps' products of one size with one kind of tile, us: 4096 x 4096 with 256, 192, 128 and 64: 3890, 3500, 4290, 4790, and 3270 by the estimate; 256 x 4096: 1330,
+// 830, 490, 240, the last in eight pieces 140.)
+struct Plan {
+  int shape;
+  uint32_t full, rest, splits;  // tiles made whole; others, each by so many workgroups
+};
+Plan plan_of(bool half, uint32_t rows, uint32_t cols, uint32_t planes, uint32_t stages) {
+  Plan best{};
+  double least = 1e30;
+  int k = 0;
+  for (const Shape& s : kShapes) {
+    const uint32_t tiles = tiles_of(half, (rows + s.side - 1) / s.side, (cols + s.side - 1) / s.side) * planes;
+    // `count` workgroups, each of so many stages
+    auto time = [&](uint32_t count, double deep) {
+      const uint32_t turns = count / s.slots, left = count - turns * s.slots;
+      return turns * (deep * s.stage + s.rest) + (left == 0 ? 0. : deep * (left > kCus ? s.stage : s.alone) + s.rest);
+    };
+    auto consider = [&](uint32_t full, uint32_t splits, double t) {
+      if (t < least) {
+        least = t;
+        best = Plan{k, full, tiles - full, splits};
+      }
+    };
+    consider(tiles, 1, time(tiles, stages));
+    const uint32_t full = tiles / s.slots * s.slots, rest = tiles - full;
+    for (uint32_t n = 2; n <= 16 && rest > 0 && stages / n >= 4; ++n)  // (a launch that joins them, and their sums out and in)
+      consider(full, n, time(full, stages) + time(rest * n, (double)stages / n) + 5. + rest * n * (s.side * s.side * 8.) / 3e6);
+    ++k;
+  }
+  return best;
+}
+size_t part_bytes(const Plan& plan) {
+  const uint64_t side = kShapes[plan.shape].side;
+  return plan.splits > 1 ? plan.rest * (uint64_t)plan.splits * side * side * sizeof(float) : 0;
 }
 
 template <typename T, int END>
-void product(const PairTask& p, hipStream_t s) {
-  constexpr bool half = END == kGram || END == kPoly;
-  auto launch = [&](auto kernel, uint32_t tile, uint32_t threads) {
-    kernel<<<dim3(tiles_of(half, (p.rows + tile - 1) / tile, (p.cols + tile - 1) / tile) * p.planes), threads, 0, s>>>(p);
+void product(PairTask p, hipStream_t s) {
+  const Plan plan = plan_of(END == kGram || END == kPoly, p.rows, p.cols, p.planes, p.stages);
+  p.full = plan.full;
+  p.splits = plan.splits;
+  auto launch = [&](auto kernel, auto join, uint32_t threads, uint32_t halves) {
+    kernel<<<dim3(plan.full + plan.rest * plan.splits), threads, 0, s>>>(p);
+    if (plan.rest > 0) join<<<dim3(plan.rest, halves), threads, 0, s>>>(p);
   };
-  // tiles of 128 x 128 where there is one for every CU at least
-  if ((uint64_t)tiles_of(half, (p.rows + 127) / 128, (p.cols + 127) / 128) * p.planes >= 256)
-    launch(pair_kernel<T, END, 4, 4, 2, 2, 2>, 128, 256);
-  else
-    launch(pair_kernel<T, END, 2, 2, 2, 2, 4>, 64, 256);
+  switch (plan.shape) {
+    case 0: launch(pair_large_kernel<T, END, 8, 4, 2, 4, 2, 2>, pair_join_kernel<T, END, 8, 4, 2, 4>, 512, 4); break;
+    case 1: launch(pair_large_kernel<T, END, 6, 3, 2, 4, 3, 1>, pair_join_kernel<T, END, 6, 3, 2, 4>, 512, 3); break;
+    case 2: launch(pair_kernel<T, END, 4, 2, 2, 4, 4>, pair_join_kernel<T, END, 4, 2, 2, 4>, 512, 2); break;
+    default: launch(pair_kernel<T, END, 2, 2, 2, 2, 4>, pair_join_kernel<T, END, 2, 2, 2, 2>, 256, 1); break;
+  }
 }
 
 struct Layout {
@@ -414,6 +630,7 @@ struct Layout {
   uint32_t parts;
   Pairs x_by_n, x_by_m[2], gram, poly;
   double* part;
+  float* sums;  // of tiles that are made in pieces
   uint64_t bytes;
 };
 
@@ -438,6 +655,9 @@ Layout layout_of(const Extent& e, char* scratch) {
   for (Pairs& x : l.x_by_m) x = pairs(l.m, l.n);
   l.gram = pairs(l.n, l.n);
   l.poly = pairs(l.n, l.n);
+  const uint32_t n = (uint32_t)l.n, m = (uint32_t)l.m, n_stages = (n + kBlockCols - 1) / kBlockCols, m_stages = (m + kBlockCols - 1) / kBlockCols;
+  l.sums = reinterpret_cast<float*>(take(std::max({part_bytes(plan_of(true, n, n, e.workers, m_stages)), part_bytes(plan_of(true, n, n, e.workers, n_stages)),
+                                                   part_bytes(plan_of(false, n, m, e.workers, n_stages)), part_bytes(plan_of(false, m, n, e.workers, n_stages))})));
   return l;
 }
 
@@ -501,6 +721,7 @@ hipError_t launch_orthogonalize(tng_type of_x, tng_type of_y, const Extent& e, c
     gram.planes = e.workers;
     gram.a = gram.b = l.x_by_n;
     gram.by_r = gram.by_c = l.gram;
+    gram.part = l.sums;
     product<float, kGram>(gram, s);
     PairTask poly = gram;
     poly.stages = n_stages;
@@ -512,6 +733,7 @@ hipError_t launch_orthogonalize(tng_type of_x, tng_type of_y, const Extent& e, c
     product<float, kPoly>(poly, s);
     PairTask apply{};
     apply.planes = e.workers;
+    apply.part = l.sums;
     apply.stages = n_stages;
     const bool last = k + 1 == steps;
     // (the last one's results lie along r where y's rows do)
