@@ -624,6 +624,257 @@ void product(PairTask p, hipStream_t s) {
   }
 }
 
+// ---- Small matrices: a workgroup each, everything in one launch.
+//
+// A wavefront holds CT tiles of 16 columns of X, all NT of their tiles of rows, as its matrix instructions leave them: four consecutive rows of a column a
+// lane.  P X takes them from there: which of P's columns meets which of X's rows in a lane's eight is free as long as both sides agree, so a lane's
+// two fours of rows are its eight, and P's are read from LDS in that order.  Only X X^T wants rows of X, through LDS, where a word is a pair.
+constexpr int kSmallWaves = 8, kSmallSteps = 64;
+
+struct SmallTask {
+  uint32_t n, m, steps;
+  bool tall;
+  View x, y;
+  tng_type of_x, of_y;
+  float eps, scale;
+  float abc[3 * kSmallSteps];
+};
+
+// Eight pairs, or four and four, as fragments.
+__device__ __forceinline__ void fragments_of(const uint32_t* first, const uint32_t* second, v8h& high, v8h& low) {
+  typedef uint32_t four __attribute__((ext_vector_type(4)));
+  const four a = *reinterpret_cast<const four*>(first), b = *reinterpret_cast<const four*>(second);
+  four h, l;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    h[k] = __builtin_amdgcn_perm(a[2 * k + 1], a[2 * k], 0x05040100u);
+    l[k] = __builtin_amdgcn_perm(a[2 * k + 1], a[2 * k], 0x07060302u);
+    h[k + 2] = __builtin_amdgcn_perm(b[2 * k + 1], b[2 * k], 0x05040100u);
+    l[k + 2] = __builtin_amdgcn_perm(b[2 * k + 1], b[2 * k], 0x07060302u);
+  }
+  high = __builtin_bit_cast(v8h, h);
+  low = __builtin_bit_cast(v8h, l);
+}
+__device__ __forceinline__ uint32_t pair_of(float v) {
+  f16_t h, l;
+  split(v, h, l);
+  return (uint32_t)__builtin_bit_cast(uint16_t, h) | (uint32_t)__builtin_bit_cast(uint16_t, l) << 16;
+}
+
+template <int NT, int CT>
+__global__ void __launch_bounds__(kSmallWaves* kWave) small_kernel(SmallTask p) {
+  static_assert(NT % 2 == 0, "a lane's eight are two tiles' fours");
+  constexpr int kRows = NT * 16, kCols = CT * 16 * kSmallWaves, kPitch = kCols + 4, kSquare = kRows + 4, kTiles = NT * (NT + 1) / 2;
+  constexpr int kMine = (kTiles + kSmallWaves - 1) / kSmallWaves;
+  typedef uint32_t four __attribute__((ext_vector_type(4)));
+  __shared__ __align__(16) uint32_t of_x[kRows * kPitch];
+  __shared__ __align__(16) uint32_t of_p[kRows * kSquare];  // G, then P
+  __shared__ double of_wave[kSmallWaves];
+  const uint32_t lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), i = lane % 16, g = lane / 16, m = blockIdx.x;
+  const uint32_t c_in = wave * CT * 16 + i, r_in = g * 4;
+  const uint64_t by_r = p.tall ? 1 : p.x.ld, by_c = p.tall ? p.x.ld : 1;
+
+  v4f x[NT][CT];
+  auto load = [&](auto of) {
+    using T = decltype(of);
+    const T* from = static_cast<const T*>(p.x.p) + m * p.x.pitch;
+#pragma unroll
+    for (int a = 0; a < NT; ++a)
+#pragma unroll
+      for (int b = 0; b < CT; ++b)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const uint32_t r = r_in + a * 16 + k, c = c_in + b * 16;  // (past the end: the last one, which is not used)
+          x[a][b][k] = (float)from[min(r, p.n - 1) * by_r + min(c, p.m - 1) * by_c];
+          if (b == CT - 1 && k == 3) __builtin_amdgcn_sched_barrier(0);
+        }
+  };
+  switch (p.of_x) {
+    case TNG_TYPE_F32: load(float{}); break;
+    case TNG_TYPE_BF16: load(bf16_t{}); break;
+    default: load(f16_t{}); break;
+  }
+  double sum = 0.;
+#pragma unroll
+  for (int a = 0; a < NT; ++a)
+#pragma unroll
+    for (int b = 0; b < CT; ++b)
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (r_in + a * 16 + k < p.n && c_in + b * 16 < p.m) sum += (double)x[a][b][k] * (double)x[a][b][k];
+  for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, kWave);
+  if (lane == 0) of_wave[wave] = sum;
+  __syncthreads();
+  sum = 0.;
+  for (int k = 0; k < kSmallWaves; ++k) sum += of_wave[k];
+  const double inv = (sum < __builtin_inf() ? 1. / (sqrt(sum) + (double)p.eps) : __builtin_nan("")) * (double)kOfX;
+#pragma unroll
+  for (int a = 0; a < NT; ++a)
+#pragma unroll
+    for (int b = 0; b < CT; ++b)
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        x[a][b][k] = r_in + a * 16 + k < p.n && c_in + b * 16 < p.m ? (float)((double)x[a][b][k] * inv) : 0.f;
+
+  // The tile of a number: rows first, c <= r.
+  auto place = [](uint32_t number, uint32_t* r, uint32_t* c) {
+    uint32_t row = 0;
+    while (number > row) number -= ++row;
+    *r = row;
+    *c = number;
+  };
+  v8h high[NT / 2][CT], low[NT / 2][CT];
+  for (uint32_t step = 0; step < p.steps; ++step) {
+    const float plus = p.abc[3 * step], times = p.abc[3 * step + 1], square = p.abc[3 * step + 2];
+    // X as fragments here, and as pairs in LDS
+#pragma unroll
+    for (int a = 0; a < NT; ++a)
+#pragma unroll
+      for (int b = 0; b < CT; ++b)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          f16_t h, l;
+          split(x[a][b][k], h, l);
+          high[a / 2][b][a % 2 * 4 + k] = h;
+          low[a / 2][b][a % 2 * 4 + k] = l;
+          of_x[(a * 16 + r_in + k) * kPitch + c_in + b * 16] = (uint32_t)__builtin_bit_cast(uint16_t, h) | (uint32_t)__builtin_bit_cast(uint16_t, l) << 16;
+        }
+    __syncthreads();
+    // G: of each wavefront's tiles
+#pragma unroll 1
+    for (uint32_t t = wave; t < kTiles; t += kSmallWaves) {
+      uint32_t tr, tc;
+      place(t, &tr, &tc);
+      v4f main = {0.f, 0.f, 0.f, 0.f}, cross = {0.f, 0.f, 0.f, 0.f};
+      const uint32_t *ra = of_x + (tr * 16 + i) * kPitch + g * 8, *rb = of_x + (tc * 16 + i) * kPitch + g * 8;
+#pragma unroll 2
+      for (uint32_t k = 0; k < kCols; k += 32) {
+        v8h ah, al, bh, bl;
+        fragments_of(ra + k, ra + k + 4, ah, al);
+        fragments_of(rb + k, rb + k + 4, bh, bl);
+        cross = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah, bl, cross, 0, 0, 0);
+        main = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah, bh, main, 0, 0, 0);
+        cross = __builtin_amdgcn_mfma_f32_16x16x32_f16(al, bh, cross, 0, 0, 0);
+      }
+      four pair;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        pair[k] = pair_of((main[k] + cross[k]) * (kOfGram / (kOfX * kOfX)));
+        of_p[(tr * 16 + r_in + k) * kSquare + tc * 16 + i] = pair[k];
+      }
+      if (tr != tc) *reinterpret_cast<four*>(of_p + (tc * 16 + i) * kSquare + tr * 16 + r_in) = pair;
+    }
+    __syncthreads();
+    // P, in the place of G
+    four made[kMine];
+#pragma unroll
+    for (int n = 0; n < kMine; ++n) {
+      const uint32_t t = wave + n * kSmallWaves;
+      if (t >= kTiles) continue;
+      uint32_t tr, tc;
+      place(t, &tr, &tc);
+      v4f all = {0.f, 0.f, 0.f, 0.f};
+      const uint32_t *ra = of_p + (tr * 16 + i) * kSquare + g * 8, *rb = of_p + (tc * 16 + i) * kSquare + g * 8;
+#pragma unroll
+      for (uint32_t k = 0; k < kRows; k += 32) {
+        v8h ah, al, bh, bl;
+        fragments_of(ra + k, ra + k + 4, ah, al);
+        fragments_of(rb + k, rb + k + 4, bh, bl);
+        all = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah, bl, all, 0, 0, 0);
+        all = __builtin_amdgcn_mfma_f32_16x16x32_f16(al, bh, all, 0, 0, 0);
+        all = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah, bh, all, 0, 0, 0);
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint32_t word = of_p[(tr * 16 + r_in + k) * kSquare + tc * 16 + i];
+        const float gram = ((float)__builtin_bit_cast(f16_t, (uint16_t)word) + (float)__builtin_bit_cast(f16_t, (uint16_t)(word >> 16))) * (1.f / kOfGram);
+        made[n][k] = pair_of((times * gram + square * (all[k] * (1.f / (kOfGram * kOfGram))) + (tr == tc && r_in + k == i ? plus : 0.f)) * kOfPoly);
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < kMine; ++n) {
+      const uint32_t t = wave + n * kSmallWaves;
+      if (t >= kTiles) continue;
+      uint32_t tr, tc;
+      place(t, &tr, &tc);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) of_p[(tr * 16 + r_in + k) * kSquare + tc * 16 + i] = made[n][k];
+      if (tr != tc) *reinterpret_cast<four*>(of_p + (tc * 16 + i) * kSquare + tr * 16 + r_in) = made[n];
+    }
+    __syncthreads();
+    // P X
+    const bool last = step + 1 == p.steps;
+    const float unit = last ? p.scale * (1.f / (kOfPoly * kOfX)) : kOfX / (kOfPoly * kOfX);
+#pragma unroll
+    for (int a = 0; a < NT; ++a) {
+      v4f all[CT] = {};
+      const uint32_t* row = of_p + (a * 16 + i) * kSquare + g * 4;
+#pragma unroll
+      for (int s = 0; s < NT / 2; ++s) {
+        v8h ph, pl;
+        fragments_of(row + s * 32, row + s * 32 + 16, ph, pl);
+#pragma unroll
+        for (int b = 0; b < CT; ++b) all[b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ph, low[s][b], all[b], 0, 0, 0);
+#pragma unroll
+        for (int b = 0; b < CT; ++b) all[b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(pl, high[s][b], all[b], 0, 0, 0);
+#pragma unroll
+        for (int b = 0; b < CT; ++b) all[b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ph, high[s][b], all[b], 0, 0, 0);
+      }
+#pragma unroll
+      for (int b = 0; b < CT; ++b)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[a][b][k] = all[b][k] * unit;
+    }
+  }
+  auto store = [&](auto of) {
+    using T = decltype(of);
+    T* to = static_cast<T*>(p.y.p) + m * p.y.pitch;
+    const uint64_t to_r = p.tall ? 1 : p.y.ld, to_c = p.tall ? p.y.ld : 1;
+#pragma unroll
+    for (int a = 0; a < NT; ++a)
+#pragma unroll
+      for (int b = 0; b < CT; ++b)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const uint32_t r = r_in + a * 16 + k, c = c_in + b * 16;
+          if (r < p.n && c < p.m) to[r * to_r + c * to_c] = (T)x[a][b][k];
+          if (k == 3) __builtin_amdgcn_sched_barrier(0);  // (so many addresses at once leave no registers)
+        }
+  };
+  switch (p.of_y) {
+    case TNG_TYPE_F32: store(float{}); break;
+    case TNG_TYPE_BF16: store(bf16_t{}); break;
+    default: store(f16_t{}); break;
+  }
+}
+
+// As many columns as LDS holds beside 64 or 32 rows.
+inline bool is_small(uint64_t n, uint64_t m) { return n <= 32 ? m <= 1024 : n <= 64 && m <= 512; }
+
+hipError_t launch_small(const SmallTask& p, uint32_t workers, hipStream_t s) {
+  auto launch = [&](auto rows, auto cols) { small_kernel<rows, cols><<<dim3(workers), kSmallWaves * kWave, 0, s>>>(p); };
+  constexpr std::integral_constant<int, 1> one;
+  constexpr std::integral_constant<int, 2> two;
+  constexpr std::integral_constant<int, 4> four;
+  constexpr std::integral_constant<int, 8> eight;
+  auto of_rows = [&](auto rows) {
+    if (p.m <= 128)
+      launch(rows, one);
+    else if (p.m <= 256)
+      launch(rows, two);
+    else
+      launch(rows, four);
+  };
+  if (p.n > 32)
+    of_rows(four);
+  else if (p.m <= 512)
+    of_rows(two);
+  else
+    launch(two, eight);
+  return hipGetLastError();
+}
+
 struct Layout {
   uint64_t n, m;
   bool tall;
@@ -701,10 +952,17 @@ bool orthogonal_in_range(const float* coefficients, uint32_t steps) {
   return true;
 }
 
-size_t orthogonal_bytes(const Extent& e) { return layout_of(e, nullptr).bytes; }
+size_t orthogonal_bytes(const Extent& e) {
+  return is_small(std::min(e.rows, e.cols), std::max(e.rows, e.cols)) ? 0 : layout_of(e, nullptr).bytes;
+}
 
 hipError_t launch_orthogonalize(tng_type of_x, tng_type of_y, const Extent& e, const View& x, const float* coefficients, uint32_t steps, float eps, float scale,
                                 const View& y, char* scratch, hipStream_t s) {
+  if (is_small(std::min(e.rows, e.cols), std::max(e.rows, e.cols))) {
+    SmallTask small{(uint32_t)std::min(e.rows, e.cols), (uint32_t)std::max(e.rows, e.cols), steps, e.rows > e.cols, x, y, of_x, of_y, eps, scale, {}};
+    std::copy(coefficients, coefficients + 3 * steps, small.abc);
+    return launch_small(small, e.workers, s);
+  }
   const Layout l = layout_of(e, scratch);
   const StartTask first{e.rows, e.cols, x, l.part, l.parts, eps, l.tall, l.x_by_n, l.x_by_m[0]};
   switch (of_x) {
