@@ -282,7 +282,7 @@ tng_status tng_rms_norm_codes(void* hip_stream, const tng_matrix* x, const tng_m
 
 size_t tng_rms_norm_grad_bytes(const tng_matrix* dy) {
   if (dy == nullptr || !is_float(dy->type) || dy->workers == 0 || dy->workers > 65535u || !sides_ok(dy)) return 0;
-  return 256 + tng::rms_norm_grad_floats((tng_type)dy->type, extent(dy)) * sizeof(float);
+  return 256 + tng::rms_norm_grad_floats(extent(dy)) * sizeof(float);
 }
 
 tng_status tng_rms_norm_grad(void* hip_stream, const tng_matrix* dy, const tng_matrix* h, const tng_matrix* dresidual, const tng_rms* norm,

@@ -78,7 +78,7 @@ struct NormArgs {
 hipError_t launch_rms_norm(tng_type type, const Extent& n, const View& x, const View& residual, const NormArgs& norm, const View& h, const View& y,
                            float* scale, hipStream_t s);
 // residual.p and dw may be null.  Scratch: rms_norm_grad_floats() floats.
-size_t rms_norm_grad_floats(tng_type type, const Extent& n);
+size_t rms_norm_grad_floats(const Extent& n);
 hipError_t launch_rms_norm_grad(tng_type type, const Extent& n, const View& dy, const View& h, const View& residual, const NormArgs& norm,
                                 const View& dx, float* dw, float* scratch, hipStream_t s);
 

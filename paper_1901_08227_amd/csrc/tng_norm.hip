@@ -135,6 +135,7 @@ __device__ __forceinline__ float inverse_root(float sum, float eps, uint64_t col
   return 1.0f / sqrtf(sum / (float)cols + eps);
 }
 
+constexpr int kLongThreads = 1024;
 constexpr int threads_of(int lanes) { return lanes > kBlock ? lanes : kBlock; }
 
 struct NormTask {
@@ -148,7 +149,7 @@ struct NormTask {
 // LANES take one row and hold it, HELD times 8 columns each: x and the residual are read once, and what becomes of them written once.  The memory
 // bounds it.  CODED: y is codes of the rows, with a scale for each.
 template <typename T, bool CODED, int LANES, int HELD, bool NARROW>
-__global__ void __launch_bounds__(threads_of(LANES)) rms_norm_kernel(NormTask p) {
+__global__ void __launch_bounds__(threads_of(LANES), sizeof(T) == 2 && LANES == kLongThreads && HELD <= 3 ? 8 : 1) rms_norm_kernel(NormTask p) {
   constexpr int kThreads = threads_of(LANES);
   __shared__ float of_sum[kThreads / kWave][2];
   __shared__ uint32_t of_max[kThreads / kWave];
@@ -166,7 +167,6 @@ __global__ void __launch_bounds__(threads_of(LANES)) rms_norm_kernel(NormTask p)
     e[k] = eight_of<NARROW>((k * LANES + lane) * 8, p.cols);
     x[k] = load_eight<T, NARROW>(row, e[k], p.cols);
   }
-  float v[HELD][8];
   if (p.r.p != nullptr) {
     const T* other = static_cast<const T*>(p.r.p) + m * p.r.pitch + r * p.r.ld;
     Vec8<T> o[HELD];
@@ -177,41 +177,39 @@ __global__ void __launch_bounds__(threads_of(LANES)) rms_norm_kernel(NormTask p)
 #pragma unroll
       for (int i = 0; i < 8; ++i) x[k][i] = (T)pinned((float)x[k][i] + (float)o[k][i]);  // (h: what it is stored as is what is normalised)
   }
-  float sum = 0.f;
+  // (the row is held as it was loaded, and widened where it is used: what 16-bit numbers save is a second workgroup on the CU)
+  auto sum_of = [&](float f) {
+    float sum = 0.f;
 #pragma unroll
-  for (int k = 0; k < HELD; ++k) {
-    widen<T>(x[k], v[k]);
+    for (int k = 0; k < HELD; ++k) {
 #pragma unroll
-    for (uint32_t i = 0; i < 8; ++i) {
-      if (!NARROW && i < e[k].shift) v[k][i] = 0.f;
-      sum += v[k][i] * v[k][i];
+      for (uint32_t i = 0; i < 8; ++i) {
+        const float v = NARROW || i >= e[k].shift ? (float)x[k][i] * f : 0.f;
+        sum += v * v;
+      }
+      asm volatile("" : "+v"(x[k]));
     }
-  }
-  sum = joint.sum(sum);
-  const float s = inverse_root(sum, p.eps, p.cols, [&](float f) {
-    float less = 0.f;
-#pragma unroll
-    for (int k = 0; k < HELD; ++k)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) less += v[k][i] * f * (v[k][i] * f);
-    return joint.sum(less);
-  });
+    return joint.sum(sum);
+  };
+  const float s = inverse_root(sum_of(1.f), p.eps, p.cols, sum_of);
   if (p.h.p != nullptr) {
     T* h = static_cast<T*>(p.h.p) + m * p.h.pitch + r * p.h.ld;
 #pragma unroll
     for (int k = 0; k < HELD; ++k) store_eight<T, NARROW>(h, e[k], p.cols, x[k]);
   }
+  float v[CODED ? HELD : 1][8];
   uint32_t top = 0u;
 #pragma unroll
   for (int k = 0; k < HELD; ++k) {
     float w[8];
     load_weight<NARROW>(p.weight, e[k], p.cols, w);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      v[k][i] = v[k][i] * s * w[i];
-      if (CODED) top = max(top, magnitude_bits(v[k][i]));
+    for (uint32_t i = 0; i < 8; ++i) {
+      float& y = v[CODED ? k : 0][i];
+      y = (float)x[k][i] * s * w[i];
+      if (CODED && (NARROW || i >= e[k].shift)) top = max(top, magnitude_bits(y));
     }
-    if (!CODED) store_eight<T, NARROW>(static_cast<T*>(p.y.p) + m * p.y.pitch + r * p.y.ld, e[k], p.cols, narrowed<T>(v[k]));
+    if (!CODED) store_eight<T, NARROW>(static_cast<T*>(p.y.p) + m * p.y.pitch + r * p.y.ld, e[k], p.cols, narrowed<T>(v[0]));
   }
   if (!CODED) return;
   top = joint.max_bits(top);
@@ -222,7 +220,7 @@ __global__ void __launch_bounds__(threads_of(LANES)) rms_norm_kernel(NormTask p)
   for (int k = 0; k < HELD; ++k) {
     uint32_t q[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) q[i] = code_nearest(v[k][i], inv);
+    for (int i = 0; i < 8; ++i) q[i] = code_nearest(v[CODED ? k : 0][i], inv);
     Vec8<int8_t> codes;
     const uint32_t low = pack4(q[0], q[1], q[2], q[3]), high = pack4(q[4], q[5], q[6], q[7]);
     __builtin_memcpy(&codes, &low, 4);
@@ -232,7 +230,6 @@ __global__ void __launch_bounds__(threads_of(LANES)) rms_norm_kernel(NormTask p)
 }
 
 // Longer rows, a workgroup each: h is made (and read) again for y, and for codes once more, mostly from a cache.
-constexpr int kLongThreads = 1024;
 
 template <typename T, bool CODED>
 __global__ void __launch_bounds__(kLongThreads) rms_norm_long_kernel(NormTask p) {
@@ -314,8 +311,8 @@ __global__ void __launch_bounds__(kLongThreads) rms_norm_long_kernel(NormTask p)
 
 constexpr std::integral_constant<int, 1> kOne;
 constexpr std::integral_constant<int, 2> kTwo;
+constexpr std::integral_constant<int, 3> kThree;
 constexpr std::integral_constant<int, 4> kFour;
-constexpr std::integral_constant<int, 6> kSix;
 constexpr std::integral_constant<int, kWave> kOfWave;
 constexpr std::integral_constant<int, kBlock> kOfBlock;
 constexpr std::integral_constant<int, 512> kOfSome;
@@ -340,10 +337,14 @@ void norm_typed(const NormTask& p, hipStream_t s) {
     launch(kOfBlock, kOne, std::false_type{});
   else if (p.cols <= 4096)
     launch(kOfBlock, kTwo, std::false_type{});
+  else if (p.cols <= 6144)
+    launch(kOfBlock, kThree, std::false_type{});
   else if (p.cols <= 8192)
     launch(kOfBlock, kFour, std::false_type{});
   else if (p.cols <= 16384)
     launch(kOfMany, kTwo, std::false_type{});
+  else if (p.cols <= 24576)
+    launch(kOfMany, kThree, std::false_type{});
   else if (p.cols <= 32768)
     launch(kOfMany, kFour, std::false_type{});
   else
@@ -376,23 +377,14 @@ __global__ void __launch_bounds__(threads_of(LANES)) rms_norm_grad_kernel(NormGr
   const uint32_t lane = threadIdx.x % LANES, group = __builtin_amdgcn_readfirstlane(threadIdx.x / LANES), wave = threadIdx.x / kWave, m = blockIdx.y;
   const Joint<LANES> joint{of_sum, nullptr, group * (LANES / kWave), wave};
   Eight e[HELD];
-  constexpr bool kWeights = HELD <= 4;  // they stay in registers; otherwise they are read (from a cache) for each row
-  float held[kWeights ? HELD : 1][8], dw[HELD][8];
+  float w[HELD][8], dw[HELD][8];
 #pragma unroll
   for (int k = 0; k < HELD; ++k) {
     e[k] = eight_of<NARROW>((k * LANES + lane) * 8, p.cols);
-    if (kWeights) load_weight<NARROW>(p.weight, e[k], p.cols, held[k]);
+    load_weight<NARROW>(p.weight, e[k], p.cols, w[k]);
 #pragma unroll
     for (int i = 0; i < 8; ++i) dw[k][i] = 0.f;
   }
-  auto weights = [&](int k, float(&w)[8]) {
-    if (kWeights) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) w[i] = held[kWeights ? k : 0][i];
-    } else {
-      load_weight<NARROW>(p.weight, e[k], p.cols, w);
-    }
-  };
   struct Row {
     Vec8<T> dy[HELD], h[HELD], r[HELD];
   };
@@ -431,14 +423,12 @@ __global__ void __launch_bounds__(threads_of(LANES)) rms_norm_grad_kernel(NormGr
     float squares = 0.f, dot = 0.f;
 #pragma unroll
     for (int k = 0; k < HELD; ++k) {
-      float w[8];
-      weights(k, w);
 #pragma unroll
       for (uint32_t i = 0; i < 8; ++i) {
         const bool mine = NARROW || i >= e[k].shift;
         const float h = mine ? (float)now.h[k][i] : 0.f, dy = mine ? (float)now.dy[k][i] : 0.f;
         squares += h * h;
-        dot += dy * w[i] * h;
+        dot += dy * w[k][i] * h;
       }
     }
     keep();
@@ -448,14 +438,12 @@ __global__ void __launch_bounds__(threads_of(LANES)) rms_norm_grad_kernel(NormGr
       float less = 0.f, small = 0.f;
 #pragma unroll
       for (int k = 0; k < HELD; ++k) {
-        float w[8];
-        weights(k, w);
 #pragma unroll
         for (uint32_t i = 0; i < 8; ++i) {
           const bool mine = NARROW || i >= e[k].shift;
           const float h = mine ? (float)now.h[k][i] * f : 0.f;
           less += h * h;
-          small += (mine ? (float)now.dy[k][i] : 0.f) * w[i] * h;
+          small += (mine ? (float)now.dy[k][i] : 0.f) * w[k][i] * h;
         }
       }
       joint.sum(less, small);
@@ -471,13 +459,12 @@ __global__ void __launch_bounds__(threads_of(LANES)) rms_norm_grad_kernel(NormGr
       T* dx = static_cast<T*>(p.dx.p) + m * p.dx.pitch + row * p.dx.ld;
 #pragma unroll
       for (int k = 0; k < HELD; ++k) {
-        float v[8], w[8];
-        weights(k, w);
+        float v[8];
 #pragma unroll
         for (uint32_t i = 0; i < 8; ++i) {
           const float unit = (float)now.h[k][i] * s, dy = (float)now.dy[k][i];
           dw[k][i] += dy * unit;
-          v[i] = s * (dy * w[i] - unit * along);
+          v[i] = s * (dy * w[k][i] - unit * along);
           if (rs != nullptr) v[i] += (float)now.r[k][i];
         }
         store_eight<T, NARROW>(dx, e[k], p.cols, narrowed<T>(v));
@@ -604,23 +591,26 @@ __global__ void __launch_bounds__(kBlock) rms_norm_grad_join_kernel(const float*
   dw[m * cols + c] = sum;
 }
 
-// How long a row the workgroups hold: sixteen registers of 32 bits for a lane's eights of both operands, and as many for dw and the weights.
-inline uint64_t held_cols(tng_type type) { return type == TNG_TYPE_F32 ? 16384 : 24576; }
+// How long a row the workgroups hold: for longer ones they would have no registers but for one on a CU.  (1537 x 20011 bfloat16, 184 MB, 73 us, where two passes
+// take 71; 8 x 100 x 18000 40 and 32; 2048 x 16384 52 and 64.)
+constexpr uint64_t kHeldCols = 16384;
 
 // Workgroups of a worker: as many as run at a time, but no more than there are rows for.
-uint32_t grad_parts(tng_type type, const Extent& n) {
+uint32_t grad_parts(const Extent& n) {
   const uint64_t groups = n.cols <= 1024 ? kBlock / kWave : 1;  // rows that a workgroup has at a time
-  const uint64_t most = n.cols <= 8192 ? 768 : 256, tiles = n.cols > held_cols(type) ? (n.cols + kBlock * 8 - 1) / (kBlock * 8) : 1;
+  // (268 MB of bfloat16, us, with 256 / 512 / 768 / 1024 workgroups: 65536 x 256 (half of that) 79 / 53 / 48 / 48, 8192 x 4096 75 / 54 / 53 / 55, 4096 x 8192
+  // 59 / 56 / 69 / 68, 2048 x 16384 64 / 71 / 81 / 87)
+  const uint64_t most = n.cols <= 512 ? 1024 : n.cols <= 1024 ? 512 : n.cols <= 4096 ? 768 : n.cols <= 8192 ? 512 : n.cols <= kHeldCols ? 256 : 512, tiles = n.cols > kHeldCols ? (n.cols + kBlock * 8 - 1) / (kBlock * 8) : 1;
   const uint64_t each = std::max<uint64_t>(1, most / (n.workers * tiles)), rows = (n.rows + groups - 1) / groups;
   return (uint32_t)std::min(each, std::max<uint64_t>(1, rows));
 }
 
 template <typename T>
-void norm_grad_typed(tng_type type, uint32_t workers, const NormGradTask& p, hipStream_t s) {
+void norm_grad_typed(uint32_t workers, const NormGradTask& p, hipStream_t s) {
   auto launch = [&](auto lanes, auto held, auto narrow) {
     rms_norm_grad_kernel<T, lanes, held, narrow><<<dim3(p.parts, workers), threads_of(lanes), 0, s>>>(p);
   };
-  if (p.cols > held_cols(type)) {
+  if (p.cols > kHeldCols) {
     rms_norm_grad_sums_kernel<T><<<dim3((uint32_t)(workers * p.rows)), kLongThreads, 0, s>>>(p);
     rms_norm_grad_columns_kernel<T><<<dim3((uint32_t)((p.cols + kBlock * 8 - 1) / (kBlock * 8)), p.parts, workers), kBlock, 0, s>>>(p);
   } else if (p.cols < 8) {
@@ -633,12 +623,12 @@ void norm_grad_typed(tng_type type, uint32_t workers, const NormGradTask& p, hip
     launch(kOfBlock, kOne, std::false_type{});
   } else if (p.cols <= 4096) {
     launch(kOfBlock, kTwo, std::false_type{});
+  } else if (p.cols <= 6144) {
+    launch(kOfBlock, kThree, std::false_type{});
   } else if (p.cols <= 8192) {
     launch(kOfBlock, kFour, std::false_type{});
-  } else if (p.cols <= 16384) {
+  } else {
     launch(kOfSome, kFour, std::false_type{});
-  } else if constexpr (sizeof(T) == 2) {
-    launch(kOfSome, kSix, std::false_type{});
   }
 }
 
@@ -656,20 +646,20 @@ hipError_t launch_rms_norm(tng_type type, const Extent& n, const View& x, const 
   return hipGetLastError();
 }
 
-size_t rms_norm_grad_floats(tng_type type, const Extent& n) {
-  return n.workers * ((uint64_t)grad_parts(type, n) * n.cols + (n.cols > held_cols(type) ? 2 * n.rows : 0));
+size_t rms_norm_grad_floats(const Extent& n) {
+  return n.workers * ((uint64_t)grad_parts(n) * n.cols + (n.cols > kHeldCols ? 2 * n.rows : 0));
 }
 
 hipError_t launch_rms_norm_grad(tng_type type, const Extent& n, const View& dy, const View& h, const View& residual, const NormArgs& norm,
                                 const View& dx, float* dw, float* scratch, hipStream_t s) {
-  const uint32_t parts = grad_parts(type, n);
+  const uint32_t parts = grad_parts(n);
   NormGradTask p{n.rows, n.cols, dy, h, residual, dx, norm.weight, norm.eps, dw == nullptr ? nullptr : scratch, parts, nullptr};
   p.row_part = scratch + (uint64_t)n.workers * parts * n.cols;
   if (n.rows > 0) {
     switch (type) {
-      case TNG_TYPE_F32: norm_grad_typed<float>(type, n.workers, p, s); break;
-      case TNG_TYPE_BF16: norm_grad_typed<bf16_t>(type, n.workers, p, s); break;
-      default: norm_grad_typed<f16_t>(type, n.workers, p, s); break;
+      case TNG_TYPE_F32: norm_grad_typed<float>(n.workers, p, s); break;
+      case TNG_TYPE_BF16: norm_grad_typed<bf16_t>(n.workers, p, s); break;
+      default: norm_grad_typed<f16_t>(n.workers, p, s); break;
     }
   }
   if (dw != nullptr)
