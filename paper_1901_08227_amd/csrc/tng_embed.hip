@@ -336,13 +336,19 @@ __device__ __forceinline__ void add_all(F row, uint32_t count, const Columns<Q>&
   while (k < count) add_many<2, T, Q, NARROW>(row, k, count, c, cols, sum);
 }
 
-// The rows of dy of tokens first .. end - 1.  A wavefront reads 32 tokens at a time, a lane one.
+// The rows of dy of the tokens that lanes first .. first + count - 1 hold.
+template <typename T, int Q, bool NARROW>
+__device__ __forceinline__ void add_tokens(const T* dy, uint64_t ld, uint32_t token, uint32_t first, uint32_t count, const Columns<Q>& c, uint64_t cols,
+                                           float (&sum)[Q][4]) {
+  add_all<T, Q, NARROW>([&](uint32_t k) { return dy + (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)token, (int)(first + k)) * ld; }, count, c, cols, sum);
+}
+// Those of places first .. end - 1: a wavefront reads 32 tokens at a time, a lane one.
 template <typename T, int Q, bool NARROW>
 __device__ __forceinline__ void add_rows(const T* dy, uint64_t ld, const uint32_t* token, uint32_t first, uint32_t end, const Columns<Q>& c, uint64_t cols,
                                          float (&sum)[Q][4]) {
   for (; first < end; first += kPiece) {
-    const uint32_t count = min(end - first, kPiece), mine = token[first + min(threadIdx.x % kPiece, count - 1)];
-    add_all<T, Q, NARROW>([&](uint32_t k) { return dy + (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)mine, (int)k) * ld; }, count, c, cols, sum);
+    const uint32_t count = min(end - first, kPiece);
+    add_tokens<T, Q, NARROW>(dy, ld, token[first + min(threadIdx.x % kPiece, count - 1)], 0, count, c, cols, sum);
   }
 }
 
@@ -386,6 +392,7 @@ __global__ void __launch_bounds__(kBlock) embed_pieces_kernel(EmbedGradTask p) {
   const uint32_t* row = p.row + all;
   // (a row that is none is nobody's run)
   const uint32_t before = first > 0u ? row[first - 1] : ~0u, after = first + kPlaces < p.places ? row[first + kPlaces] : ~0u;
+  const uint32_t token = WHOLE ? 0u : p.token[all + first + threadIdx.x % kPiece];
   uint32_t starts, ends;  // of a piece's places; of a piece of pieces, each piece's first place and its last
   if (WHOLE) {
     starts = row[first + threadIdx.x % kPiece * kPiece];
@@ -400,13 +407,12 @@ __global__ void __launch_bounds__(kBlock) embed_pieces_kernel(EmbedGradTask p) {
   float* to = (WHOLE ? p.whole : p.piece) + ((uint64_t)m * p.blocks * each + number) * stride;
   const float* piece = WHOLE ? p.piece + (((uint64_t)m * p.blocks + block) * (p.places / kPiece) + in * kPiece) * stride : nullptr;
   const T* dy = static_cast<const T*>(p.dy.p) + m * p.dy.pitch;
-  const uint32_t* token = p.token + all + first;
   if (coming > 0u) {
     float sum[Q][4] = {};
     if (WHOLE)
       add_parts<Q, NARROW>(piece, stride, coming, c, p.cols, sum);
     else
-      add_rows<T, Q, NARROW>(dy, p.dy.ld, token, 0, coming, c, p.cols, sum);
+      add_tokens<T, Q, NARROW>(dy, p.dy.ld, token, 0, coming, c, p.cols, sum);
     store_sum<Q, NARROW>(to, c, p.cols, sum, 1.f, false);
   }
   if (going > 0u) {
@@ -416,7 +422,7 @@ __global__ void __launch_bounds__(kBlock) embed_pieces_kernel(EmbedGradTask p) {
       add_parts<Q, NARROW>(from + p.cols, stride, 1, c, p.cols, sum);
       add_parts<Q, NARROW>(from + stride, stride, going - 1, c, p.cols, sum);
     } else {
-      add_rows<T, Q, NARROW>(dy, p.dy.ld, token, kPiece - going, kPiece, c, p.cols, sum);
+      add_tokens<T, Q, NARROW>(dy, p.dy.ld, token, kPiece - going, going, c, p.cols, sum);
     }
     store_sum<Q, NARROW>(to + p.cols, c, p.cols, sum, 1.f, false);
   }
@@ -460,7 +466,7 @@ __global__ void __launch_bounds__(kBlock) embed_grad_kernel(EmbedGradTask p) {
         continue;
       }
       // the run goes out of its first piece (or piece of pieces), and comes into the others
-      const bool whole = whole_a != whole_b;
+      const bool whole = p.whole != nullptr && whole_a != whole_b;
       const uint32_t from = whole ? whole_a : piece_a, to = whole ? whole_b : piece_b, each = p.places / (whole ? kWhole : kPiece);
       const float* part = (whole ? p.whole : p.piece) + (((uint64_t)m * p.blocks + block) * each + from) * stride;
       add_parts<Q, NARROW>(part + p.cols, stride, 1, c, p.cols, sum);
@@ -484,7 +490,7 @@ uint32_t places_of(uint64_t rows) {
     if (rows <= n) return n;
   return kSorted;
 }
-constexpr uint64_t kPiecesFrom = 4 * kPiece;
+constexpr uint64_t kPiecesFrom = 4 * kPiece, kWholesFrom = 4096;
 
 // What the gradient keeps, in words of 32 bits.
 uint64_t embed_grad_layout(EmbedGradTask& p, uint32_t workers, uint32_t* scratch) {
@@ -506,10 +512,8 @@ uint64_t embed_grad_layout(EmbedGradTask& p, uint32_t workers, uint32_t* scratch
   p.token = take(blocks * kSorted);
   p.begin = take(blocks * (p.groups + 1));
   p.piece = p.whole = nullptr;
-  if (p.rows >= kPiecesFrom) {
-    p.piece = reinterpret_cast<float*>(take(blocks * (p.places / kPiece) * 2 * p.cols));
-    p.whole = reinterpret_cast<float*>(take(blocks * (p.places / kWhole) * 2 * p.cols));
-  }
+  if (p.rows >= kPiecesFrom) p.piece = reinterpret_cast<float*>(take(blocks * (p.places / kPiece) * 2 * p.cols));
+  if (p.places >= kWholesFrom) p.whole = reinterpret_cast<float*>(take(blocks * (p.places / kWhole) * 2 * p.cols));
   return at;
 }
 
@@ -533,11 +537,10 @@ void embed_grad_typed(uint32_t workers, const EmbedGradTask& p, hipStream_t s) {
   auto launch = [&](auto lanes, auto fours) {
     const uint32_t across = (uint32_t)((p.cols + lanes * fours * 4 - 1) / (lanes * fours * 4)), at_a_time = kBlock / lanes;
     const uint32_t pieces = p.blocks * (p.places / kPiece), wholes = p.blocks * (p.places / kWhole);
-    if (p.piece != nullptr) {
+    if (p.piece != nullptr)
       embed_pieces_kernel<T, false, lanes, fours, NARROW><<<dim3((pieces + at_a_time - 1) / at_a_time, across, workers), kBlock, 0, s>>>(p);
-      if (p.places > kWhole)
-        embed_pieces_kernel<T, true, lanes, fours, NARROW><<<dim3((wholes + at_a_time - 1) / at_a_time, across, workers), kBlock, 0, s>>>(p);
-    }
+    if (p.whole != nullptr)
+      embed_pieces_kernel<T, true, lanes, fours, NARROW><<<dim3((wholes + at_a_time - 1) / at_a_time, across, workers), kBlock, 0, s>>>(p);
     embed_grad_kernel<T, lanes, fours, NARROW><<<dim3(p.groups, across, workers), kBlock, lds, s>>>(p);
   };
   constexpr std::integral_constant<int, 1> one;
