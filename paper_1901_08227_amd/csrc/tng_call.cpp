@@ -12,10 +12,11 @@
 //   layer(address, address of the call that sizes its scratch, stream, kinds, argument, ...) -> status, or None
 //
 // the same for the calls on layers: kinds has a letter per argument, m a matrix of numbers ([rows, cols] or [M, rows, cols]), i one of codes,
-// d the five fields of tng_drop in a tuple, and float32 vectors by the last matrix before them: r workers * rows, n rows, c cols long.  A w
-// (W) at the end takes no argument: scratch, as large as is said of the first matrix (of the first two and the last), from torch.  Nor
-// does an o (p): a matrix like the first (with a column for each row of the last before it), from torch; that tensor is what is returned
-// where the call succeeds.
+// t tokens ([T] or [M, T]), d the five fields of tng_drop in a tuple, g a norm's weights and eps in one, f a float, and float32 vectors by the
+// last matrix before them: r workers * rows, n rows, c cols, e workers * cols long.  A w (W) at the end takes no argument: scratch, as large as is
+// said of the first matrix (of the first two and the last), from torch.  Nor do those that stand for a result, a tensor from torch: o (p) a matrix like the
+// first (with a column for each row of the last before it), q (u) codes of the first matrix (turned), s (x) a float32 for each of its rows (columns) and
+// workers; the result, or a tuple of them, is what is returned where the call succeeds.
 //
 //   linear(addresses, stream, x, drop, codes, scales, bias) -> (y, scales, turned codes)
 //   linear_grad(addresses, stream, dy, scales, turned codes, weights' scales, weights' turned codes, drop, x, (seed, iter, site), out)
@@ -114,6 +115,23 @@ at::Tensor numbers(const at::Tensor& x, int64_t rows, int64_t cols, at::ScalarTy
   *m = tng_matrix{t.data_ptr(), type == at::kFloat ? TNG_TYPE_F32 : type == at::kHalf ? TNG_TYPE_F16 : TNG_TYPE_BF16,
                   x.dim() == 3 ? (uint32_t)x.size(0) : 1u, (uint64_t)rows, (uint64_t)cols, (uint64_t)cols, (uint64_t)(rows * cols)};
   return t;
+}
+
+// Codes whose rows begin 16 bytes apart, and their matrix.
+at::Tensor codes(const at::Tensor& x, int64_t rows, int64_t cols, tng_matrix* m) {
+  const int64_t ld = (cols + 15) / 16 * 16;
+  const at::Tensor t = at::empty(shape_like(x, rows, ld), x.options().dtype(at::kChar));
+  *m = tng_matrix{t.data_ptr(), TNG_TYPE_I8, x.dim() == 3 ? (uint32_t)x.size(0) : 1u, (uint64_t)rows, (uint64_t)cols, (uint64_t)ld,
+                  (uint64_t)(rows * ld)};
+  return ld == cols ? t : t.narrow(-1, 0, cols);
+}
+
+// A float32 vector: a row of each worker's.
+at::Tensor floats(const at::Tensor& x, int64_t n) {
+  Shape s;
+  if (x.dim() == 3) s.push_back(x.size(0));
+  s.push_back(n);
+  return at::empty(s, x.options().dtype(at::kFloat));
 }
 
 constexpr int kLayerFixed = 4, kLayerMost = 16;
@@ -247,7 +265,7 @@ PyObject* layer(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   const Py_ssize_t letters = PyUnicode_GET_LENGTH(args[3]);
   const bool scratch = letters > 0 && (kinds[letters - 1] == 'w' || kinds[letters - 1] == 'W');
   Py_ssize_t made = 0;  // without an argument
-  for (Py_ssize_t i = 0; i < letters; ++i) made += strchr("wWop", kinds[i]) != nullptr;
+  for (Py_ssize_t i = 0; i < letters; ++i) made += strchr("wWopqusx", kinds[i]) != nullptr;
   if (nargs != kLayerFixed + letters - made || letters > kLayerMost - 3) {
     PyErr_SetString(PyExc_TypeError, "layer: an argument per letter");
     return nullptr;
@@ -258,16 +276,28 @@ PyObject* layer(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   LayerCall c;
   int n = 1, status = -1;
   try {
-    at::Tensor out;
+    c10::SmallVector<at::Tensor, 4> results;
     PyObject* const* next = args + kLayerFixed;
     for (Py_ssize_t i = 0; i < letters - scratch; ++i, ++n) {
-      if (kinds[i] == 'o' || kinds[i] == 'p') {
+      if (strchr("opqusx", kinds[i]) != nullptr) {
         if (c.matrices == 0 || c.matrices == 8 || c.first == nullptr) Py_RETURN_NONE;
         const tng_matrix& m = c.matrix[0];
         const at::Tensor& like = THPVariable_Unpack(c.first);
-        out = numbers(like, (int64_t)m.rows, (int64_t)(kinds[i] == 'o' ? m.cols : c.matrix[c.matrices - 1].rows), like.scalar_type(),
-                      &c.matrix[c.matrices]);
-        a[n] = reinterpret_cast<uintptr_t>(&c.matrix[c.matrices++]);
+        const int64_t rows = (int64_t)m.rows, cols = (int64_t)m.cols;
+        if (kinds[i] == 's' || kinds[i] == 'x') {
+          results.push_back(floats(like, kinds[i] == 's' ? rows : cols));
+          a[n] = reinterpret_cast<uintptr_t>(results.back().data_ptr());
+          continue;
+        }
+        tng_matrix* made_m = &c.matrix[c.matrices];
+        switch (kinds[i]) {
+          case 'q': results.push_back(codes(like, rows, cols, made_m)); break;
+          case 'u': results.push_back(codes(like, cols, rows, made_m)); break;
+          case 'o': results.push_back(numbers(like, rows, cols, like.scalar_type(), made_m)); break;
+          default: results.push_back(numbers(like, rows, (int64_t)c.matrix[c.matrices - 1].rows, like.scalar_type(), made_m));
+        }
+        a[n] = reinterpret_cast<uintptr_t>(made_m);
+        ++c.matrices;
         continue;
       }
       PyObject* obj = *next++;
@@ -308,7 +338,12 @@ PyObject* layer(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
       default: break;
     }
     Py_END_ALLOW_THREADS
-    if (status == 0 && out.defined()) return THPVariable_Wrap(out);
+    if (status == 0 && results.size() == 1) return THPVariable_Wrap(results[0]);
+    if (status == 0 && !results.empty()) {
+      PyObject* all = PyTuple_New((Py_ssize_t)results.size());
+      for (size_t k = 0; all != nullptr && k < results.size(); ++k) PyTuple_SET_ITEM(all, (Py_ssize_t)k, THPVariable_Wrap(results[k]));
+      return all;
+    }
   } catch (const std::exception&) {
     Py_RETURN_NONE;
   }
@@ -344,23 +379,6 @@ bool entries_of(PyObject* obj, Entries* e) {
   e->product = reinterpret_cast<Product>(a[3]);
   e->product_bytes = reinterpret_cast<ProductBytes>(a[4]);
   return !PyErr_Occurred();
-}
-
-// Codes whose rows begin 16 bytes apart, and their matrix.
-at::Tensor codes(const at::Tensor& x, int64_t rows, int64_t cols, tng_matrix* m) {
-  const int64_t ld = (cols + 15) / 16 * 16;
-  const at::Tensor t = at::empty(shape_like(x, rows, ld), x.options().dtype(at::kChar));
-  *m = tng_matrix{t.data_ptr(), TNG_TYPE_I8, x.dim() == 3 ? (uint32_t)x.size(0) : 1u, (uint64_t)rows, (uint64_t)cols, (uint64_t)ld,
-                  (uint64_t)(rows * ld)};
-  return ld == cols ? t : t.narrow(-1, 0, cols);
-}
-
-// A float32 vector: a row of each worker's.
-at::Tensor floats(const at::Tensor& x, int64_t n) {
-  Shape s;
-  if (x.dim() == 3) s.push_back(x.size(0));
-  s.push_back(n);
-  return at::empty(s, x.options().dtype(at::kFloat));
 }
 
 at::Tensor bytes_of(const at::Tensor& x, size_t n) { return at::empty({(int64_t)n}, x.options().dtype(at::kByte)); }

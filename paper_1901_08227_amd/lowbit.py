@@ -212,6 +212,16 @@ def _run(name, device, *args, made=None):
     return args[-1]
 
 
+def _make(name, device, kinds, *args):
+    """A layer call by the native function, which makes all its results (letters of csrc/tng_call.cpp); None where an argument is not plain."""
+    if not _plain(device):
+        return None
+    got = B._layer(B._address[name], B._address.get(name + "_bytes", 0), _stream(device), kinds, *args)
+    if isinstance(got, int):
+        B._check(got, name)
+    return got
+
+
 def _codes(shape, device):
     """int8 codes whose rows begin 16 bytes apart, which the products' fast kernels ask for."""
     cols = shape[-1]
@@ -288,6 +298,10 @@ def rms_norm(x, weight=None, residual=None, eps=1e-6, out=None):
         if out is None:
             return _run("tng_rms_norm", x.device, x, None, (weight, float(eps)), None, made=x.shape)
         return _run("tng_rms_norm", x.device, x, None, (weight, float(eps)), None, _out(out, x.shape, x.dtype, x.device))
+    if out is None:
+        got = _make("tng_rms_norm", x.device, "mmgoo", x, residual, (weight, float(eps)))
+        if got is not None:
+            return got[1], got[0]
     h = torch.empty(x.shape, dtype=x.dtype, device=x.device)
     out = _out(out, x.shape, x.dtype, x.device)
     return _run("tng_rms_norm", x.device, x, residual, (weight, float(eps)), h, out), h
@@ -295,6 +309,13 @@ def rms_norm(x, weight=None, residual=None, eps=1e-6, out=None):
 
 def rms_norm_codes(x, weight=None, residual=None, eps=1e-6, turned=False):
     """The codes of rms_norm's result, which is itself written nowhere: NormCodes(q, scale, h, qt).  h is x where there is no residual."""
+    if residual is not None:
+        if turned:
+            got = _make("tng_rms_norm_codes", x.device, "mmgoqsu", x, residual, (weight, float(eps)))
+        else:
+            got = _make("tng_rms_norm_codes", x.device, "mmgoqsi", x, residual, (weight, float(eps)), None)
+        if got is not None:
+            return NormCodes(got[1], got[2], got[0], got[3] if turned else None)
     shape, device = _dims(x, "x"), x.device
     q, scale = _codes(shape, device), _floats(shape[:-1], device)
     qt = _codes((*shape[:-2], shape[-1], shape[-2]), device) if turned else None
@@ -307,6 +328,10 @@ def rms_norm_grad(dy, h, weight=None, dresidual=None, eps=1e-6, out=None):
     """(dx, dw) from the gradient dy of rms_norm's result (or of what its codes stand for) and h, what was normalised.  dresidual: the gradient that
     reaches h past the norm.  dx is the gradient of x, and of the residual; dw [M, cols] float32 (without the M where dy has none), None without
     weights."""
+    if out is None and weight is not None:
+        got = _make("tng_rms_norm_grad", dy.device, "mmmgoxw", dy, h, dresidual, (weight, float(eps)))
+        if got is not None:
+            return got
     dx = _out(out, dy.shape, dy.dtype, dy.device)
     (*lead, _, cols), dw = _dims(dy, "dy"), None
     if weight is not None:
