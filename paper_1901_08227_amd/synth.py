@@ -124,3 +124,15 @@ def class_mixture(M: int, rows: int, width: int, classes: int, seed: int, it: in
     g = _gen(seed * 1000003 + it + 1, device)
     labels = torch.randint(0, classes, (M, rows), generator=g, device=device)
     return centres[labels] + torch.randn((M, rows, width), generator=g, device=device), labels
+
+
+def token_classes(M: int, rows: int, vocabulary: int, classes: int, seed: int, it: int, device="cpu"):
+    """Minibatches of tokens that each belong to a class: iteration `it` of worker m.
+
+    Returns (tokens[M][rows], the chance of the k-th most frequent falling as 1 / k; labels[M][rows], a class drawn once for each token).
+    """
+    of_token = torch.randint(0, classes, (vocabulary,), generator=_gen(seed, device), device=device)
+    g = _gen(seed * 1000003 + it + 1, device)
+    u = torch.rand((M, rows), generator=g, device=device, dtype=torch.float64)
+    tokens = (torch.exp(u * math.log(vocabulary + 1.0)) - 1).long().clamp(0, vocabulary - 1)
+    return tokens, of_token[tokens]
