@@ -849,8 +849,8 @@ __global__ void __launch_bounds__(kSmallWaves* kWave) small_kernel(SmallTask p) 
   }
 }
 
-// As many columns as LDS holds beside 64 or 32 rows.
-inline bool is_small(uint64_t n, uint64_t m) { return n <= 32 ? m <= 1024 : n <= 64 && m <= 512; }
+// As many columns as LDS holds beside the rows, in turns of 128.
+inline bool is_small(uint64_t n, uint64_t m) { return m <= (n <= 32 ? 1024u : n <= 64 ? 512u : n <= 96 ? 256u : n <= 128 ? 128u : 0u); }
 
 hipError_t launch_small(const SmallTask& p, uint32_t workers, hipStream_t s) {
   auto launch = [&](auto rows, auto cols) { small_kernel<rows, cols><<<dim3(workers), kSmallWaves * kWave, 0, s>>>(p); };
@@ -858,20 +858,17 @@ hipError_t launch_small(const SmallTask& p, uint32_t workers, hipStream_t s) {
   constexpr std::integral_constant<int, 2> two;
   constexpr std::integral_constant<int, 4> four;
   constexpr std::integral_constant<int, 8> eight;
-  auto of_rows = [&](auto rows) {
-    if (p.m <= 128)
-      launch(rows, one);
-    else if (p.m <= 256)
-      launch(rows, two);
-    else
-      launch(rows, four);
-  };
-  if (p.n > 32)
-    of_rows(four);
-  else if (p.m <= 512)
-    of_rows(two);
+  constexpr std::integral_constant<int, 6> six;
+  auto up_to_256 = [&](auto rows) { p.m <= 128 ? launch(rows, one) : launch(rows, two); };
+  auto up_to_512 = [&](auto rows) { p.m <= 256 ? up_to_256(rows) : launch(rows, four); };
+  if (p.n <= 32)
+    p.m <= 512 ? up_to_512(two) : launch(two, eight);
+  else if (p.n <= 64)
+    up_to_512(four);
+  else if (p.n <= 96)
+    up_to_256(six);
   else
-    launch(two, eight);
+    launch(eight, one);
   return hipGetLastError();
 }
 

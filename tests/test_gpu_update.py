@@ -18,7 +18,8 @@ pytestmark = pytest.mark.gpu
 QUINTIC = (update.QUINTIC,) * 5
 CUBIC = ((1.5, -0.5, 0.0),) * 3
 ONE = (update.QUINTIC,)
-SHAPES = [(1, 1, 1), (1, 1, 7), (2, 9, 1), (3, 5, 8), (2, 31, 33), (1, 64, 64), (2, 65, 32), (1, 100, 257), (5, 130, 96), (1, 300, 200), (40, 64, 130), (2, 33, 512), (1, 63, 257), (3, 32, 1024), (2, 20, 600), (2, 64, 513), (1, 32, 1025)]
+SHAPES = [(1, 1, 1), (1, 1, 7), (2, 9, 1), (3, 5, 8), (2, 31, 33), (1, 64, 64), (2, 65, 32), (1, 100, 257), (5, 130, 96), (1, 300, 200), (40, 64, 130), (2, 33, 512), (1, 63, 257), (3, 32, 1024), (2, 20, 600), (2, 64, 513), (1, 32, 1025), (2, 96, 256), (1, 65, 129), (2, 96, 257), (3, 128, 128), (1, 97, 100),
+          (1, 128, 129)]
 
 
 def roundings():
