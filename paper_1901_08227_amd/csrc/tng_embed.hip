@@ -125,7 +125,7 @@ void embed_from(tng_type table, tng_type type, uint32_t workers, EmbedTask& p, h
 // together then, a run, in the order that they came in, whatever ran first.  Sums are taken in that order.  Runs that cross the ends of pieces of kPiece sorted
 // places are summed by pieces first, and those that cross the ends of kPiece pieces by such wholes: whatever tokens come, no sum is a long chain, and
 // each row of dy is read once.  Every row of the table is written, those of no token with zeros.
-constexpr uint32_t kSorted = 8192, kSortThreads = 1024, kSortWaves = kSortThreads / kWave;
+constexpr uint32_t kSorted = 4096, kSortThreads = 1024, kSortWaves = kSortThreads / kWave;
 constexpr uint32_t kFewSorted = 256;                        // so many are sorted by counting for each those before it
 constexpr uint32_t kPiece = 32, kWhole = kPiece * kPiece;  // places of a piece, and of a piece of pieces
 constexpr uint32_t kMostBins = 256;
@@ -486,9 +486,7 @@ __global__ void __launch_bounds__(kBlock) embed_grad_nothing_kernel(uint64_t row
 // How many of a block's places are written, and whether sums of pieces are taken (of few tokens no chain is long).
 uint32_t places_of(uint64_t rows) {
   if (rows <= kFewSorted) return kFewSorted;
-  for (const uint32_t n : {1024u, 2048u, 4096u})
-    if (rows <= n) return n;
-  return kSorted;
+  return rows <= 1024 ? 1024u : rows <= 2048 ? 2048u : kSorted;
 }
 constexpr uint64_t kPiecesFrom = 4 * kPiece, kWholesFrom = 4096;
 
@@ -526,8 +524,7 @@ void sort_typed(uint32_t workers, const EmbedGradTask& p, hipStream_t s) {
     case kFewSorted: embed_sort_few_kernel<I><<<grid, kFewSorted, 0, s>>>(p); break;
     case 1024: launch(std::integral_constant<int, 1>{}); break;
     case 2048: launch(std::integral_constant<int, 2>{}); break;
-    case 4096: launch(std::integral_constant<int, 4>{}); break;
-    default: launch(std::integral_constant<int, 8>{});
+    default: launch(std::integral_constant<int, kSorted / kSortThreads>{});
   }
 }
 
