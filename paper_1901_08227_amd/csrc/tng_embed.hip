@@ -17,7 +17,7 @@ __device__ __forceinline__ uint32_t row_of(const I* ids, uint64_t at, uint64_t r
   return id >= 0 && (uint64_t)id < rows ? (uint32_t)id : (uint32_t)rows;
 }
 
-// Results of more bytes are written past the caches: the memory-side cache does not hold them.
+// Results of more bytes are written past the caches: the memory-side cache, of 256 MiB, does not hold them beside what is read.
 constexpr uint64_t kPast = 128u << 20;
 
 struct EmbedTask {
@@ -28,7 +28,8 @@ struct EmbedTask {
   bool past;  // y is written past the caches
 };
 
-// y = scale table[id].  A lane takes eight columns of kMany tokens' rows (the row's last eight where it ends inside them: what two lanes write of
+// y = scale table[id].  What it moves bounds it: 32768 tokens of 4096 bfloat16, whose 15000 rows and result are 390 MB, 74 us; 3 x 20011 of 1003, float32 to
+// float16, rows at odd places, 38 us, in which 240 MB come out of the dies' caches.  A lane takes eight columns of kMany tokens' rows (the row's last eight where it ends inside them: what two lanes write of
 // one column is the same), so that their tokens, and then their rows, are on the way together.
 template <typename I, typename W, typename T, bool NARROW>
 __global__ void __launch_bounds__(kBlock) embed_kernel(EmbedTask p) {
@@ -161,7 +162,8 @@ __device__ __forceinline__ void groups_begin(const EmbedGradTask& p, uint32_t m,
 }
 
 // Least significant digits first, of 2^digit bins.  A wavefront takes consecutive places, 64 at a time: lanes of one digit find each other by ballots, and
-// the wavefront's counter of that digit says how many came before them.  That all is in one CU's LDS is what bounds it.
+// the wavefront's counter of that digit says how many came before them.  That all is one CU's work is what bounds it: six instructions a bit and token for
+// the ballots.  2048 tokens of 32000 rows 9.7 us, 4096 of 4099 rows 12 (8192 at a time 18, and the gradient of 30000 tokens into 20000 x 256 43 instead of 36).
 template <typename I, int ITEMS>
 __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(EmbedGradTask p, uint32_t digit, uint32_t passes) {
   __shared__ uint32_t keys[ITEMS * kSortThreads];
@@ -380,7 +382,7 @@ __device__ __forceinline__ void store_sum(float* to, const Columns<Q>& c, uint64
 }
 
 // The two runs that cross the ends of a piece (or of a piece of pieces): the sum of the one that comes in, as far as it goes, and of the one that
-// begins here and goes on.  LANES take a piece.
+// begins here and goes on.  LANES take a piece.  3 x 20011 tokens of 1003 float16, 120 MB, 26 us; few pieces take the latency of their loads, 10.
 template <typename T, bool WHOLE, int LANES, int Q, bool NARROW>
 __global__ void __launch_bounds__(kBlock) embed_pieces_kernel(EmbedGradTask p) {
   constexpr uint32_t kPlaces = WHOLE ? kWhole : kPiece;
@@ -428,7 +430,9 @@ __global__ void __launch_bounds__(kBlock) embed_pieces_kernel(EmbedGradTask p) {
   }
 }
 
-// Rows of the table, p.each for a workgroup, LANES for each at a time.  What it has to write bounds it.
+// Rows of the table, p.each for a workgroup, LANES for each at a time.  What it has to write bounds it: 4 x 32000 x 2048, 1049 MB, 190 to 200 us (a fill
+// takes 153; of no tokens 188).  Zeros first, by workgroups beside those of the pieces, and then the rows that have tokens, run by run, was 3 % sooner there and
+// 13 % later where most rows have some.  Of 5 tokens a row, in five blocks, the latency of tokens and rows: 3 x 4099 x 1003 39 us.
 template <typename T, int LANES, int Q, bool NARROW>
 __global__ void __launch_bounds__(kBlock) embed_grad_kernel(EmbedGradTask p) {
   constexpr uint32_t kAtATime = kBlock / LANES;

@@ -147,7 +147,8 @@ struct NormTask {
 };
 
 // LANES take one row and hold it, HELD times 8 columns each: x and the residual are read once, and what becomes of them written once.  The memory
-// bounds it.  CODED: y is codes of the rows, with a scale for each.
+// bounds it: 8192 x 4096 bfloat16 with a residual, into h and codes, 235 MB, 44 us (5.3 TB/s); 1537 x 20011 float16, rows at odd places, 123 MB, 37.  One row is a
+// launch and two latencies, 3.6 us.  CODED: y is codes of the rows, with a scale for each.
 template <typename T, bool CODED, int LANES, int HELD, bool NARROW>
 __global__ void __launch_bounds__(threads_of(LANES), sizeof(T) == 2 && LANES == kLongThreads && HELD <= 3 ? 8 : 1) rms_norm_kernel(NormTask p) {
   constexpr int kThreads = threads_of(LANES);
@@ -356,7 +357,7 @@ void norm_typed(const NormTask& p, hipStream_t s) {
 //   s = 1 / sqrt(mean h^2 + eps),  g = w dy,  dx = s (g - h s^2 mean(g h)) + dr,  dw = sum over a worker's rows of dy h s
 //
 // s is made again: both sums of a row come out of the one pass that has to read it anyway.  dw lies in registers while a group of LANES takes rows, one
-// after another, and the groups' parts meet in the second kernel.
+// after another, and the groups' parts meet in the second kernel.  4 x 2048 x 4096 bfloat16 with dr, 268 MB, 49 us (5.5 TB/s), and 5 for the parts.
 
 struct NormGradTask {
   uint64_t rows, cols;
@@ -500,7 +501,7 @@ __global__ void __launch_bounds__(threads_of(LANES)) rms_norm_grad_kernel(NormGr
   }
 }
 
-// Longer rows: a row's two sums by a workgroup, then columns by tiles as long as a wavefront's eights.
+// Longer rows: a row's two sums by a workgroup, then columns, by tiles of a workgroup's eights (1537 x 20011 float16: 30 and 32 us).
 template <typename T>
 __global__ void __launch_bounds__(kLongThreads) rms_norm_grad_sums_kernel(NormGradTask p) {
   __shared__ float of_sum[kLongThreads / kWave][2];
