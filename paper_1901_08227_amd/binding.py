@@ -164,7 +164,8 @@ def lib() -> ctypes.CDLL:
                                  "tng_step", "tng_dropout", "tng_dropout_grad", "tng_quantize_rows", "tng_quantize_grad",
                                  "tng_quantize_grad_bytes", "tng_matmul_i8", "tng_matmul_i8_bytes", "tng_linear_i8",
                                  "tng_linear_i8_bytes", "tng_rms_norm", "tng_rms_norm_codes", "tng_rms_norm_grad",
-                                 "tng_rms_norm_grad_bytes", "tng_embed", "tng_embed_grad", "tng_embed_grad_bytes")}
+                                 "tng_rms_norm_grad_bytes", "tng_embed", "tng_embed_grad", "tng_embed_grad_bytes", "tng_orthogonalize",
+                                 "tng_orthogonalize_bytes")}
         _lib = L
     return _lib
 

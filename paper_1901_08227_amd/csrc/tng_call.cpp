@@ -12,11 +12,12 @@
 //   layer(address, address of the call that sizes its scratch, stream, kinds, argument, ...) -> status, or None
 //
 // the same for the calls on layers: kinds has a letter per argument, m a matrix of numbers ([rows, cols] or [M, rows, cols]), i one of codes,
-// t tokens ([T] or [M, T]), d the five fields of tng_drop in a tuple, g a norm's weights and eps in one, f a float, and float32 vectors by the
-// last matrix before them: r workers * rows, n rows, c cols, e workers * cols long.  A w (W) at the end takes no argument: scratch, as large as is
+// t tokens ([T] or [M, T]), d the five fields of tng_drop in a tuple, g a norm's weights and eps in one, j the coefficients of an orthogonalisation,
+// one behind the other, its eps and scale in one, f a float, and float32 vectors by the last matrix before them: r workers * rows, n rows, c cols, e workers * cols long.  A w (W) at the end takes no argument: scratch, as large as is
 // said of the first matrix (of the first two and the last), from torch.  Nor do those that stand for a result, a tensor from torch: o (p) a matrix like the
 // first (with a column for each row of the last before it), q (u) codes of the first matrix (turned), s (x) a float32 for each of its rows (columns) and
-// workers; the result, or a tuple of them, is what is returned where the call succeeds.
+// workers.  A k takes a dtype, a v a number of rows: a row of that type for each token, of the last matrix's columns; so many rows of float32, of the last
+// matrix's workers and columns.  The result, or a tuple of them, is what is returned where the call succeeds.
 //
 //   linear(addresses, stream, x, drop, codes, scales, bias) -> (y, scales, turned codes)
 //   linear_grad(addresses, stream, dy, scales, turned codes, weights' scales, weights' turned codes, drop, x, (seed, iter, site), out)
@@ -31,6 +32,7 @@
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
 #include <c10/util/SmallVector.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "../../include/tng.h"
@@ -142,10 +144,12 @@ struct LayerCall {
   int matrices = 0;
   tng_drop drop;
   tng_rms norm;
+  tng_orthogonal plan;
+  float coefficients[3 * 64];
   float number;
   c10::Device device{c10::kCPU};
   bool have_device = false;
-  PyObject* first = nullptr;  // the first matrix
+  PyObject *first = nullptr, *last = nullptr;  // the first matrix, and the last one that is an argument
 
   bool same_device(const at::Tensor& t) {
     if (!have_device) {
@@ -186,6 +190,7 @@ struct LayerCall {
     m.ld = (uint64_t)strides[dim - 2];
     m.pitch = dim == 3 ? (uint64_t)strides[0] : 0u;
     if (matrices++ == 0) first = obj;
+    last = obj;
     *out = reinterpret_cast<uintptr_t>(&m);
     return true;
   }
@@ -212,6 +217,7 @@ struct LayerCall {
     m = tng_matrix{t.data_ptr(), t.scalar_type() == at::kInt ? TNG_TYPE_I32 : TNG_TYPE_I64, dim == 2 ? (uint32_t)sizes[0] : 1u,
                    (uint64_t)sizes[dim - 1], 1u, (uint64_t)strides[dim - 1], dim == 2 ? (uint64_t)strides[0] : 0u};
     if (matrices++ == 0) first = obj;
+    last = obj;
     *out = reinterpret_cast<uintptr_t>(&m);
     return true;
   }
@@ -222,6 +228,19 @@ struct LayerCall {
     if (PyTuple_GET_ITEM(obj, 0) != Py_None && !as_vector(PyTuple_GET_ITEM(obj, 0), 'c', &weight)) return false;
     norm = tng_rms{reinterpret_cast<const float*>(weight), (float)PyFloat_AS_DOUBLE(PyTuple_GET_ITEM(obj, 1))};
     *out = reinterpret_cast<uintptr_t>(&norm);
+    return true;
+  }
+
+  bool as_plan(PyObject* obj, uintptr_t* out) {
+    if (!PyTuple_Check(obj)) return false;
+    const Py_ssize_t n = PyTuple_GET_SIZE(obj) - 2;
+    if (n < 3 || n > 3 * 64 || n % 3 != 0) return false;
+    for (Py_ssize_t i = 0; i < n + 2; ++i)
+      if (!PyFloat_CheckExact(PyTuple_GET_ITEM(obj, i))) return false;
+    for (Py_ssize_t i = 0; i < n; ++i) coefficients[i] = (float)PyFloat_AS_DOUBLE(PyTuple_GET_ITEM(obj, i));
+    plan = tng_orthogonal{coefficients, (uint32_t)(n / 3), (float)PyFloat_AS_DOUBLE(PyTuple_GET_ITEM(obj, n)),
+                          (float)PyFloat_AS_DOUBLE(PyTuple_GET_ITEM(obj, n + 1))};
+    *out = reinterpret_cast<uintptr_t>(&plan);
     return true;
   }
 
@@ -301,6 +320,34 @@ PyObject* layer(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
         continue;
       }
       PyObject* obj = *next++;
+      if (kinds[i] == 'k' || kinds[i] == 'v') {
+        if (c.matrices == 0 || c.matrices == 8 || c.last == nullptr) Py_RETURN_NONE;
+        const at::Tensor &tokens = THPVariable_Unpack(c.first), &like = THPVariable_Unpack(c.last);
+        const int64_t cols = (int64_t)c.matrix[c.matrices - 1].cols;
+        tng_matrix* made_m = &c.matrix[c.matrices];
+        if (kinds[i] == 'k') {
+          if (!THPDtype_Check(obj)) Py_RETURN_NONE;
+          const at::ScalarType type = reinterpret_cast<THPDtype*>(obj)->scalar_type;
+          if (type != at::kFloat && type != at::kBFloat16 && type != at::kHalf) Py_RETURN_NONE;
+          Shape s(tokens.sizes().begin(), tokens.sizes().end());
+          s.push_back(cols);
+          results.push_back(at::empty(s, like.options().dtype(type)));
+          *made_m = c.matrix[0];
+          made_m->data = results.back().data_ptr();
+          made_m->type = type == at::kFloat ? TNG_TYPE_F32 : type == at::kHalf ? TNG_TYPE_F16 : TNG_TYPE_BF16;
+          made_m->cols = made_m->ld = (uint64_t)cols;
+          made_m->pitch = made_m->rows * made_m->ld;
+        } else {
+          if (!PyLong_CheckExact(obj)) Py_RETURN_NONE;
+          int overflow = 0;
+          const long long rows = PyLong_AsLongLongAndOverflow(obj, &overflow);
+          if (overflow != 0 || rows < 0 || rows > (1ll << 22)) Py_RETURN_NONE;  // (more: the library says so, without memory for them)
+          results.push_back(numbers(like, rows, cols, at::kFloat, made_m));
+        }
+        a[n] = reinterpret_cast<uintptr_t>(made_m);
+        ++c.matrices;
+        continue;
+      }
       if (obj == Py_None) {
         a[n] = 0;
         continue;
@@ -310,6 +357,7 @@ PyObject* layer(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
                          : k == 'm' || k == 'i' ? c.as_matrix(obj, k == 'i', &a[n])
                          : k == 't'             ? c.as_tokens(obj, &a[n])
                          : k == 'g'             ? c.as_norm(obj, &a[n])
+                         : k == 'j'             ? c.as_plan(obj, &a[n])
                          : k == 'f'             ? c.as_number(obj, &a[n])
                                                 : c.as_vector(obj, k, &a[n]);
       if (!plain) Py_RETURN_NONE;

@@ -343,6 +343,10 @@ def rms_norm_grad(dy, h, weight=None, dresidual=None, eps=1e-6, out=None):
 def embed(ids, table, scale=1.0, dtype=None, out=None):
     """scale table[ids] of the table's type, or of dtype: tokens [T] or [M, T], int32 or int64, a table [vocabulary, cols] for all workers or [M,
     vocabulary, cols].  A token outside the table (-1, say) gets a row of zeros."""
+    if out is None:
+        got = _make("tng_embed", ids.device, "tmfk", ids, table, float(scale), table.dtype if dtype is None else dtype)
+        if got is not None:
+            return got
     return _run("tng_embed", ids.device, ids, table, float(scale),
                 _out(out, (*ids.shape, table.shape[-1]), (table if out is None else out).dtype if dtype is None else dtype, ids.device))
 
@@ -350,6 +354,10 @@ def embed(ids, table, scale=1.0, dtype=None, out=None):
 def embed_grad(ids, dy, vocabulary, scale=1.0, out=None):
     """The gradient of each worker's table [M, vocabulary, cols] (without the M where ids have none), float32, from that of embed's result.  Every
     row is written, those of no token with zeros.  out: where it is written, any pitch."""
+    if out is None:
+        got = _make("tng_embed_grad", dy.device, "tmfvW", ids, dy, float(scale), vocabulary)
+        if got is not None:
+            return got
     out = _out(out, (*_dims(dy, "dy")[:-2], vocabulary, dy.shape[-1]), torch.float32, dy.device)
     return _run("tng_embed_grad", dy.device, ids, dy, float(scale), out)
 

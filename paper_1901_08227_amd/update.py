@@ -24,13 +24,16 @@ def orthogonalize(x, coefficients=(QUINTIC,) * 5, eps=1e-7, scale=1.0, out=None)
     device = x.device
     if device.type != "cuda":
         raise TypeError("x: expected a CUDA tensor")
-    if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=device)
-    else:
-        out = lowbit._out(out, x.shape, out.dtype, device)
     flat = [float(v) for step in coefficients for v in step]
     if len(flat) != 3 * len(coefficients):
         raise ValueError("coefficients: expected (a, b, c) for each step")
+    if out is None:
+        got = lowbit._make("tng_orthogonalize", device, "mjow", x, (*flat, float(eps), float(scale)))
+        if got is not None:
+            return got
+        out = torch.empty(x.shape, dtype=x.dtype, device=device)
+    else:
+        out = lowbit._out(out, x.shape, out.dtype, device)
     plan = B.TngOrthogonal((ctypes.c_float * len(flat))(*flat), len(coefficients), float(eps), float(scale))
     a, y = lowbit._matrix(x, lowbit._TYPES, "x"), lowbit._matrix(out, lowbit._TYPES, "out")
     L = B.lib()

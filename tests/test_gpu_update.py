@@ -138,3 +138,10 @@ def test_graph_and_another_stream():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(got, update.orthogonalize(x))
+
+
+def test_ctypes_way_is_the_same(monkeypatch):
+    x = normal((2, 70, 90), torch.bfloat16, 40)
+    want = update.orthogonalize(x, scale=2)
+    monkeypatch.setattr(B, "_layer", B._through_ctypes)
+    assert torch.equal(update.orthogonalize(x, scale=2), want)
