@@ -364,11 +364,11 @@ tng_status tng_linear_i8(void* hip_stream, const tng_drop* drop, const tng_matri
  * a NaN gives NaN; squares beyond binary32 are none of those (they are taken of h 2^-70 then).  Sums of a row: binary32, in a fixed order. */
 typedef struct {
   const float* weight; /* device float[cols], one for all workers; NULL: 1     */
-  float eps;           /* at least FLT_MIN, finite: rows of zeros give zeros   */
+  float eps;           /* FLT_MIN .. 2^64: rows of zeros give zeros            */
 } tng_rms;
 
-/* Matrices of one type (F32, BF16, F16) and size, limits as for tng_quantize_rows; residual and h may be NULL (h: not wanted).  h and y may each be x or
- * residual. */
+/* Matrices of one type (F32, BF16, F16) and size, limits as for tng_quantize_rows; residual and h may be NULL (h: not wanted).  h and y may be x or
+ * residual, but not both the same. */
 tng_status tng_rms_norm(void* hip_stream, const tng_matrix* x, const tng_matrix* residual, const tng_rms* norm, const tng_matrix* h,
                         const tng_matrix* y);
 /* The rows of y, before a rounding to x's type, as tng_quantize_rows codes them: q, scale[workers][rows], and with qt (NULL: not wanted) the same
@@ -377,7 +377,8 @@ tng_status tng_rms_norm_codes(void* hip_stream, const tng_matrix* x, const tng_m
                               const tng_matrix* q, float* scale, const tng_matrix* qt);
 /* With g = weight dy:  dx = s (g - h s^2 mean(g h)) + dresidual,  dw[m] = sum over worker m's rows of dy h s.
  * dy: the gradient of y; h: as above; dresidual: what reaches h on the way past the norm (NULL: nothing); dx: the gradient of x, which is the residual's
- * too, and may be dy, h or dresidual; dw: device float[workers][cols], binary32 in a fixed order, NULL: not wanted. */
+ * too, and may be dy, h or dresidual; dw: device float[workers][cols], binary32 in an order that sizes and the number of workers decide, NULL: not
+ * wanted. */
 size_t tng_rms_norm_grad_bytes(const tng_matrix* dy);
 tng_status tng_rms_norm_grad(void* hip_stream, const tng_matrix* dy, const tng_matrix* h, const tng_matrix* dresidual, const tng_rms* norm,
                              const tng_matrix* dx, float* dw, void* workspace, size_t workspace_bytes);
@@ -397,8 +398,8 @@ tng_status tng_embed_grad(void* hip_stream, const tng_matrix* ids, const tng_mat
  * A decoded average (or what a momentum makes of it) whose singular values are brought near 1 before the step:
  *   X = x / (||x|| + eps);  for each of the steps, with its a, b, c:  G = X X^T,  X = (a + b G + c G G) X;  y = scale X
  * ||x||: the root of the sum of squares, in binary64.  Products are of pairs of binary16 that hold 22 bits of a number and more, but nothing
- * below 2^-39, summed in binary32.  A
- * matrix that holds an infinity or a NaN gives NaN; one of zeros gives zeros.  The coefficients have to keep the singular values, which begin at 1 or
+ * below 2^-39, summed in binary32, in an order that sizes and the number of matrices decide (a call repeats bit for bit; a matrix alone and the same
+ * among others may differ in their last bits).  A matrix that holds an infinity or a NaN gives NaN; one of zeros gives zeros.  The coefficients have to keep the singular values, which begin at 1 or
  * below, under 2, and a + b s^2 + c s^4 of them within 8 (TNG_ERR_UNSUPPORTED otherwise); the optimiser Muon's (3.4445, -4.775, 2.0315), and
  * (1.5, -0.5, 0) and (1.875, -1.25, 0.375), whose values approach 1, do. */
 typedef struct {

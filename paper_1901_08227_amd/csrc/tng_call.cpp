@@ -12,12 +12,14 @@
 //   layer(address, address of the call that sizes its scratch, stream, kinds, argument, ...) -> status, or None
 //
 // the same for the calls on layers: kinds has a letter per argument, m a matrix of numbers ([rows, cols] or [M, rows, cols]), i one of codes,
-// t tokens ([T] or [M, T]), d the five fields of tng_drop in a tuple, g a norm's weights and eps in one, j the coefficients of an orthogonalisation,
-// one behind the other, its eps and scale in one, f a float, and float32 vectors by the last matrix before them: r workers * rows, n rows, c cols, e workers * cols long.  A w (W) at the end takes no argument: scratch, as large as is
-// said of the first matrix (of the first two and the last), from torch.  Nor do those that stand for a result, a tensor from torch: o (p) a matrix like the
-// first (with a column for each row of the last before it), q (u) codes of the first matrix (turned), s (x) a float32 for each of its rows (columns) and
-// workers.  A k takes a dtype, a v a number of rows: a row of that type for each token, of the last matrix's columns; so many rows of float32, of the last
-// matrix's workers and columns.  The result, or a tuple of them, is what is returned where the call succeeds.
+// t tokens ([T] or [M, T]), d the five fields of tng_drop in a tuple, g a norm's weights and eps in one, j the coefficients of an
+// orthogonalisation, one behind the other, its eps and scale in one, f a float, and float32 vectors by the last matrix before them: r
+// workers * rows, n rows, c cols, e workers * cols long.  A w (W) at the end takes no argument: scratch, as large as is said of the first
+// matrix (of the first two and the last), from torch.  Nor do those that stand for a result, a tensor from torch: o (p) a matrix like the
+// first (with a column for each row of the last before it), q (u) codes of the first matrix (turned), s (x) a float32 for each of its rows
+// (columns) and workers.  A k takes a dtype, a v a number of rows: a row of that type for each token, of the last matrix's columns; so
+// many rows of float32, of the last matrix's workers and columns.  The result, or a tuple of them, is what is returned where the call
+// succeeds.
 //
 //   linear(addresses, stream, x, drop, codes, scales, bias) -> (y, scales, turned codes)
 //   linear_grad(addresses, stream, dy, scales, turned codes, weights' scales, weights' turned codes, drop, x, (seed, iter, site), out)

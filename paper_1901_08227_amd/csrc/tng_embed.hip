@@ -44,7 +44,7 @@ __global__ void __launch_bounds__(kBlock) embed_kernel(EmbedTask p) {
 #pragma unroll
   for (int k = 0; k < kMany; ++k) {
     const uint64_t at = min(first + k * kBlock, n - 1);
-    t[k] = n >> 32 == 0 ? (uint32_t)at / (uint32_t)p.eights : at / p.eights;  // (64 bits take four times the instructions)
+    t[k] = (uint32_t)at / (uint32_t)p.eights;  // (no matrix has 2^32 eights, and 64 bits take four times the instructions)
     c[k] = (at - t[k] * p.eights) * 8;
     if (!NARROW) c[k] = min(c[k], p.cols - 8);
     row[k] = row_of<I>(ids, t[k] * p.ids.ld, p.vocabulary);
@@ -82,16 +82,16 @@ __global__ void __launch_bounds__(kBlock) embed_kernel(EmbedTask p) {
 // No row to read: all tokens are outside.
 template <typename T>
 __global__ void __launch_bounds__(kBlock) embed_nothing_kernel(uint64_t rows, uint64_t cols, View y) {
-  const uint64_t e = (uint64_t)blockIdx.x * kBlock + threadIdx.x;
+  const uint64_t e = block_number() * kBlock + threadIdx.x;
   if (e >= rows * cols) return;
   const uint64_t r = e / cols;
-  static_cast<T*>(y.p)[blockIdx.y * y.pitch + r * y.ld + (e - r * cols)] = (T)0.f;
+  static_cast<T*>(y.p)[blockIdx.z * y.pitch + r * y.ld + (e - r * cols)] = (T)0.f;
 }
 
 template <typename I, typename W, typename T>
 void embed_typed(uint32_t workers, EmbedTask& p, hipStream_t s) {
   if (p.vocabulary == 0) {
-    embed_nothing_kernel<T><<<dim3((uint32_t)((p.rows * p.cols + kBlock - 1) / kBlock), workers), kBlock, 0, s>>>(p.rows, p.cols, p.y);
+    embed_nothing_kernel<T><<<grid_of((p.rows * p.cols + kBlock - 1) / kBlock, workers), kBlock, 0, s>>>(p.rows, p.cols, p.y);
     return;
   }
   p.eights = (p.cols + 7) / 8;
@@ -481,10 +481,10 @@ __global__ void __launch_bounds__(kBlock) embed_grad_kernel(EmbedGradTask p) {
 }
 
 __global__ void __launch_bounds__(kBlock) embed_grad_nothing_kernel(uint64_t rows, uint64_t cols, View y) {
-  const uint64_t e = (uint64_t)blockIdx.x * kBlock + threadIdx.x;
+  const uint64_t e = block_number() * kBlock + threadIdx.x;
   if (e >= rows * cols) return;
   const uint64_t r = e / cols;
-  static_cast<float*>(y.p)[blockIdx.y * y.pitch + r * y.ld + (e - r * cols)] = 0.f;
+  static_cast<float*>(y.p)[blockIdx.z * y.pitch + r * y.ld + (e - r * cols)] = 0.f;
 }
 
 // How many of a block's places are written, and whether sums of pieces are taken (of few tokens no chain is long).
@@ -580,7 +580,7 @@ size_t embed_grad_words(uint32_t workers, uint64_t rows, uint64_t cols, uint64_t
 hipError_t launch_embed_grad(tng_type of_ids, tng_type type, uint32_t workers, uint64_t rows, uint64_t cols, uint64_t vocabulary, const View& ids,
                              const View& dy, float scale, const View& dtable, uint32_t* scratch, hipStream_t s) {
   if (rows == 0) {
-    embed_grad_nothing_kernel<<<dim3((uint32_t)((vocabulary * cols + kBlock - 1) / kBlock), workers), kBlock, 0, s>>>(vocabulary, cols, dtable);
+    embed_grad_nothing_kernel<<<grid_of((vocabulary * cols + kBlock - 1) / kBlock, workers), kBlock, 0, s>>>(vocabulary, cols, dtable);
     return hipGetLastError();
   }
   EmbedGradTask p{};

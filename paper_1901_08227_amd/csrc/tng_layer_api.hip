@@ -110,7 +110,7 @@ bool linear_scratch(const tng_matrix* x, const tng_matrix* b, const tng_matrix* 
 }
 
 bool norm_ok(const tng_rms* n) {
-  return n != nullptr && n->eps >= FLT_MIN && n->eps <= FLT_MAX && aligned(n->weight, 4);
+  return n != nullptr && n->eps >= FLT_MIN && n->eps <= 0x1p64f && aligned(n->weight, 4);
 }
 
 tng::NormArgs norm_args(const tng_rms& n) { return tng::NormArgs{n.weight, n.eps}; }
@@ -121,6 +121,9 @@ bool normed_ok(const tng_matrix* x, const tng_matrix* residual, const tng_rms* n
   if (residual != nullptr && (!sound(residual, false) || residual->type != x->type || !same_size(x, residual))) return false;
   return h == nullptr || (sound(h, true) && h->type == x->type && same_size(x, h));
 }
+
+// Whether two results begin at one place.
+bool same_place(const tng_matrix* a, const tng_matrix* b) { return a != nullptr && b != nullptr && !empty(*a) && !empty(*b) && a->data == b->data; }
 
 // Tokens and the matrix with a row for each of them.
 bool tokens_ok(const tng_matrix* ids, const tng_matrix* rows, bool output) {
@@ -259,7 +262,8 @@ tng_status tng_linear_i8(void* hip_stream, const tng_drop* drop, const tng_matri
 
 tng_status tng_rms_norm(void* hip_stream, const tng_matrix* x, const tng_matrix* residual, const tng_rms* norm, const tng_matrix* h,
                         const tng_matrix* y) {
-  if (!normed_ok(x, residual, norm, h) || !sound(y, true) || y->type != x->type || !same_size(x, y)) return TNG_ERR_INVALID_ARG;
+  if (!normed_ok(x, residual, norm, h) || !sound(y, true) || y->type != x->type || !same_size(x, y) || same_place(h, y))
+    return TNG_ERR_INVALID_ARG;
   if (empty(*x)) return TNG_OK;
   return hip_status(tng::launch_rms_norm((tng_type)x->type, extent(x), view(x), view(residual), norm_args(*norm), view(h), view(y), nullptr,
                                          static_cast<hipStream_t>(hip_stream)));

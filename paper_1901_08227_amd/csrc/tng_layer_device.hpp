@@ -16,6 +16,13 @@ __device__ __forceinline__ float pinned(float x) {
   return x;
 }
 
+// Workgroups by one number, of up to 1024 threads each: a grid's side holds 2^32 threads less one, which rows of the longest matrices pass.
+inline dim3 grid_of(uint64_t blocks, uint32_t workers = 1) {
+  const uint64_t side = 1u << 20;
+  return dim3((uint32_t)(blocks < side ? blocks : side), (uint32_t)((blocks + side - 1) / side), workers);
+}
+__device__ __forceinline__ uint64_t block_number() { return (uint64_t)blockIdx.y * gridDim.x + blockIdx.x; }
+
 // Eight (or N) consecutive elements at an address of the element's own alignment, as 32-bit numbers.  Rows of odd length start
 // anywhere; loads of 16 bytes are legal there on this target.
 template <typename T, int N>

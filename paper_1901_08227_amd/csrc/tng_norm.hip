@@ -155,8 +155,9 @@ __global__ void __launch_bounds__(threads_of(LANES), sizeof(T) == 2 && LANES == 
   __shared__ float of_sum[kThreads / kWave][2];
   __shared__ uint32_t of_max[kThreads / kWave];
   const uint32_t lane = threadIdx.x % LANES, wave = threadIdx.x / kWave;
-  const uint64_t index = (uint64_t)blockIdx.x * (kThreads / LANES) + __builtin_amdgcn_readfirstlane(threadIdx.x / LANES);
-  if (LANES == kWave && index >= p.all) return;  // (LANES == kThreads otherwise: no row is left over)
+  static_assert(LANES == kWave || LANES == kThreads, "who meets has a row, or returns, together");
+  const uint64_t index = block_number() * (kThreads / LANES) + __builtin_amdgcn_readfirstlane(threadIdx.x / LANES);
+  if (index >= p.all) return;
   const Joint<LANES> joint{of_sum, of_max, threadIdx.x / LANES * (LANES / kWave), wave};
   const uint32_t m = (uint32_t)index / (uint32_t)p.rows;
   const uint64_t r = index - m * p.rows;
@@ -237,7 +238,8 @@ __global__ void __launch_bounds__(kLongThreads) rms_norm_long_kernel(NormTask p)
   __shared__ float of_sum[kLongThreads / kWave][2];
   __shared__ uint32_t of_max[kLongThreads / kWave];
   const Joint<kLongThreads> joint{of_sum, of_max, 0, threadIdx.x / kWave};
-  const uint64_t index = blockIdx.x;
+  const uint64_t index = block_number();
+  if (index >= p.all) return;
   const uint32_t m = (uint32_t)index / (uint32_t)p.rows;
   const uint64_t r = index - m * p.rows;
   const T* row = static_cast<const T*>(p.x.p) + m * p.x.pitch + r * p.x.ld;
@@ -323,7 +325,7 @@ template <typename T, bool CODED>
 void norm_typed(const NormTask& p, hipStream_t s) {
   auto launch = [&](auto lanes, auto held, auto narrow) {
     constexpr int threads = threads_of(lanes), each = threads / lanes;
-    rms_norm_kernel<T, CODED, lanes, held, narrow><<<dim3((uint32_t)((p.all + each - 1) / each)), threads, 0, s>>>(p);
+    rms_norm_kernel<T, CODED, lanes, held, narrow><<<grid_of((p.all + each - 1) / each), threads, 0, s>>>(p);
   };
   const bool many = p.all >= 1024;  // (few rows get a workgroup each, for their latency)
   if (p.cols < 8)
@@ -349,7 +351,7 @@ void norm_typed(const NormTask& p, hipStream_t s) {
   else if (p.cols <= 32768)
     launch(kOfMany, kFour, std::false_type{});
   else
-    rms_norm_long_kernel<T, CODED><<<dim3((uint32_t)p.all), kLongThreads, 0, s>>>(p);
+    rms_norm_long_kernel<T, CODED><<<grid_of(p.all), kLongThreads, 0, s>>>(p);
 }
 
 // ---- the gradient
@@ -503,10 +505,11 @@ __global__ void __launch_bounds__(threads_of(LANES)) rms_norm_grad_kernel(NormGr
 
 // Longer rows: a row's two sums by a workgroup, then columns, by tiles of a workgroup's eights (1537 x 20011 float16: 30 and 32 us).
 template <typename T>
-__global__ void __launch_bounds__(kLongThreads) rms_norm_grad_sums_kernel(NormGradTask p) {
+__global__ void __launch_bounds__(kLongThreads) rms_norm_grad_sums_kernel(NormGradTask p, uint64_t rows) {
   __shared__ float of_sum[kLongThreads / kWave][2];
   const Joint<kLongThreads> joint{of_sum, nullptr, 0, threadIdx.x / kWave};
-  const uint64_t index = blockIdx.x;
+  const uint64_t index = block_number();
+  if (index >= rows) return;
   const uint32_t m = (uint32_t)index / (uint32_t)p.rows;
   const uint64_t r = index - m * p.rows;
   const T* dys = static_cast<const T*>(p.dy.p) + m * p.dy.pitch + r * p.dy.ld;
@@ -612,7 +615,7 @@ void norm_grad_typed(uint32_t workers, const NormGradTask& p, hipStream_t s) {
     rms_norm_grad_kernel<T, lanes, held, narrow><<<dim3(p.parts, workers), threads_of(lanes), 0, s>>>(p);
   };
   if (p.cols > kHeldCols) {
-    rms_norm_grad_sums_kernel<T><<<dim3((uint32_t)(workers * p.rows)), kLongThreads, 0, s>>>(p);
+    rms_norm_grad_sums_kernel<T><<<grid_of(workers * p.rows), kLongThreads, 0, s>>>(p, workers * p.rows);
     rms_norm_grad_columns_kernel<T><<<dim3((uint32_t)((p.cols + kBlock * 8 - 1) / (kBlock * 8)), p.parts, workers), kBlock, 0, s>>>(p);
   } else if (p.cols < 8) {
     launch(kOfWave, kOne, std::true_type{});

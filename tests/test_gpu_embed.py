@@ -80,6 +80,12 @@ def test_gradient(M, T, V, C, dtype):
         assert torch.equal(lowbit.embed_grad(ids, dy, V, 3.25), got)
 
 
+# the most blocks of sorted tokens that 2^19 make, and the largest tables, whose rows' numbers take 22 and 23 bits
+@pytest.mark.parametrize("M,T,V,C", [(1, 1 << 19, 7, 9), (2, 300001, 70000, 5), (1, 5000, (1 << 22) - 1, 3), (2, 200, 1 << 22, 8), (1, 9, 1 << 22, 5)])
+def test_gradient_of_many(M, T, V, C):
+    test_gradient(M, T, V, C, torch.float32)
+
+
 def test_gradients_are_written_nowhere_else():
     big = torch.full((3, 20, 50), 7.0, device=DEV)
     ids, dy = tokens(3, 100, 16, 7, "skewed"), normal((3, 100, 33), torch.float32, 8)
@@ -170,3 +176,12 @@ def test_ctypes_way_is_the_same(monkeypatch):
     want = calls()
     monkeypatch.setattr(B, "_layer", B._through_ctypes)
     assert all(torch.equal(a, b) for a, b in zip(calls(), want))
+
+
+def test_results_beyond_32_bits_of_no_row_and_of_no_token():
+    T, C = 1 << 22, 1100
+    out = torch.ones((T, C), dtype=torch.bfloat16, device=DEV)
+    table = torch.empty((0, C), dtype=torch.bfloat16, device=DEV)
+    assert not lowbit.embed(torch.zeros(T, dtype=torch.int32, device=DEV), table, out=out).any()
+    out = torch.ones((T, C), device=DEV)
+    assert not lowbit.embed_grad(torch.empty(0, dtype=torch.int64, device=DEV), torch.empty((0, C), device=DEV), T, out=out).any()

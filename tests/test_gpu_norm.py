@@ -220,3 +220,13 @@ def test_ctypes_way_is_the_same(monkeypatch):
     want = calls()
     monkeypatch.setattr(B, "_layer", B._through_ctypes)
     assert all(torch.equal(a, b) for a, b in zip(calls(), want))
+
+
+@pytest.mark.parametrize("rows,cols", [((1 << 19) + 1, 8200), (3, 40000)])
+def test_more_rows_than_a_side_of_a_grid(rows, cols):
+    # eight workers of more than 2^19 rows: beyond 2^32 threads; one row stands for all
+    x, w = normal((1, 1, cols), torch.bfloat16, 60), weights(cols)
+    n, one = lowbit.rms_norm_codes(x.expand(8, rows, cols), w), lowbit.rms_norm_codes(x, w)
+    assert n.scale.eq(one.scale).all()
+    for m in range(8):
+        assert n.q[m].eq(one.q[0]).all()

@@ -145,3 +145,13 @@ def test_ctypes_way_is_the_same(monkeypatch):
     want = update.orthogonalize(x, scale=2)
     monkeypatch.setattr(B, "_layer", B._through_ctypes)
     assert torch.equal(update.orthogonalize(x, scale=2), want)
+
+
+# few rows of matrices that are too long for one workgroup; alone, a matrix's sums may be taken in other pieces: near as well
+@pytest.mark.parametrize("shape", [(2, 1, 2000), (3, 2, 65536), (2, 3, 4097), (70, 33, 1030)])
+def test_few_long_rows(shape):
+    x = normal(shape, torch.float32, 1, 1e-3)
+    y = update.orthogonalize(x, scale=1.25)
+    assert near(y, host(x), QUINTIC, 1e-7, 1.25) and torch.equal(update.orthogonalize(x, scale=1.25), y)
+    assert near(update.orthogonalize(x[:1], scale=1.25), host(x[:1]), QUINTIC, 1e-7, 1.25)
+    assert near(update.orthogonalize(x.transpose(1, 2).contiguous(), scale=1.25).transpose(1, 2), host(x), QUINTIC, 1e-7, 1.25)

@@ -136,3 +136,12 @@ def test_host_tensors_and_wrong_shapes_are_refused():
         lowbit.rms_norm(x, residual=x, out=torch.zeros(3, 3))
     with pytest.raises(ValueError):
         lowbit.embed_grad(i, x, 5, out=torch.zeros(4, 3))
+
+
+def test_two_results_in_one_place_and_an_eps_beside_which_no_square_counts():
+    L = B.lib()
+    ok, other = mat(), B.TngMatrix(P + 4096, *[getattr(mat(), f) for f, _ in B.TngMatrix._fields_[1:]])
+    assert L.tng_rms_norm(None, ok, None, rms(), other, other) == B.TNG_ERR_INVALID_ARG
+    assert L.tng_rms_norm(None, ok, None, rms(2.0 ** 65), None, other) == B.TNG_ERR_INVALID_ARG
+    none = mat(rows=0)
+    assert L.tng_rms_norm(None, none, None, rms(2.0 ** 64), none, none) == B.TNG_OK
