@@ -52,7 +52,9 @@ __global__ void __launch_bounds__(kBlock) embed_kernel(EmbedTask p) {
   Vec8<W> w[kMany];
 #pragma unroll
   for (int k = 0; k < kMany; ++k) {
-    const W* from = table + (uint64_t)(row[k] < p.vocabulary ? row[k] : 0u) * p.table.ld + c[k];
+    w[k] = Vec8<W>{};
+    if (row[k] >= p.vocabulary) continue;
+    const W* from = table + (uint64_t)row[k] * p.table.ld + c[k];
     if (NARROW) {
 #pragma unroll
       for (uint32_t i = 0; i < 8; ++i) w[k][i] = i < p.cols ? from[i] : (W)0.f;
@@ -127,9 +129,9 @@ void embed_from(tng_type table, tng_type type, uint32_t workers, EmbedTask& p, h
 // places are summed by pieces first, and those that cross the ends of kPiece pieces by such wholes: whatever tokens come, no sum is a long chain, and
 // each row of dy is read once.  Every row of the table is written, those of no token with zeros.
 constexpr uint32_t kSorted = 4096, kSortThreads = 1024, kSortWaves = kSortThreads / kWave;
-constexpr uint32_t kFewSorted = 256;                        // so many are sorted by counting for each those before it
+constexpr uint32_t kFew = kBlock;                           // so many a workgroup picks its rows' from, without an order made before
 constexpr uint32_t kPiece = 32, kWhole = kPiece * kPiece;  // places of a piece, and of a piece of pieces
-constexpr uint32_t kMostBins = 256;
+constexpr uint32_t kMostBins = 256, kMostEach = 16;
 
 struct EmbedGradTask {
   uint64_t rows, cols, vocabulary;
@@ -138,10 +140,10 @@ struct EmbedGradTask {
   uint32_t bits;          // of a row's number; the largest number they hold stands for no row
   uint32_t blocks;        // of kSorted tokens, of a worker
   uint32_t places;        // of a block that are written: those behind the last token hold no row
-  uint32_t each, groups;  // rows of the table that a workgroup writes, and how many such groups there are
+  uint32_t each, groups;  // rows of the table that a workgroup writes (kMostEach at most), and how many such groups there are
   uint32_t *row, *token;  // [worker][block][kSorted]: sorted rows, and the token's number
   uint32_t* begin;        // [worker][block][groups + 1]: where a group's rows begin in a block
-  float *piece, *whole;   // [worker][block][places / kPiece][2][cols], and / kWhole: of the run that comes in, and of the one that goes out; or null
+  float *piece, *whole;   // [worker][block][places / kPiece][2][cols], and / kWhole (or null): of the run that comes in, and of the one that goes out
   bool past;              // dtable is written past the caches
 };
 
@@ -249,34 +251,6 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(EmbedGradTask 
   }
   groups_begin(p, m, keys, ITEMS * kSortThreads);
 }
-
-// The same of few tokens: each counts those that come before it.
-template <typename I>
-__global__ void __launch_bounds__(kFewSorted) embed_sort_few_kernel(EmbedGradTask p) {
-  typedef uint32_t four __attribute__((ext_vector_type(4)));
-  __shared__ __align__(16) uint32_t keys[kFewSorted];  // a row, and below it the token's place: no two are the same
-  __shared__ uint32_t sorted[kFewSorted];
-  const uint32_t m = blockIdx.y, t = threadIdx.x, none = (1u << p.bits) - 1u;
-  const I* ids = static_cast<const I*>(p.ids.p) + m * p.ids.pitch;
-  const uint32_t r = row_of<I>(ids, min((uint64_t)t, p.rows - 1) * p.ids.ld, p.vocabulary), row = t < p.rows && r < p.vocabulary ? r : none;
-  const uint32_t key = row * kFewSorted + t;
-  keys[t] = key;
-  __syncthreads();
-  uint32_t to = 0u;
-#pragma unroll 8
-  for (uint32_t j = 0; j < kFewSorted; j += 4) {
-    const four k = *reinterpret_cast<const four*>(keys + j);
-#pragma unroll
-    for (uint32_t n = 0; n < 4; ++n) to += k[n] < key ? 1u : 0u;
-  }
-  sorted[to] = row;
-  const uint64_t at = (uint64_t)m * kSorted + to;
-  p.row[at] = row;
-  p.token[at] = t;
-  __syncthreads();
-  groups_begin(p, m, sorted, kFewSorted);
-}
-static_assert(kFewSorted <= 256, "a row of 23 bits and a place of 8 are a key");
 
 // What a lane has of a row: Q times four columns, LANES fours apart, so that a wavefront's accesses have no gaps.  Where a row ends inside a four, the row's
 // last four are taken (what two lanes have of one column is the same).  NARROW: rows of less than four columns.
@@ -465,7 +439,7 @@ __global__ void __launch_bounds__(kBlock) embed_grad_kernel(EmbedGradTask p) {
       const uint32_t a = __builtin_amdgcn_readfirstlane(bound[block * bounds + r]), b = __builtin_amdgcn_readfirstlane(bound[block * bounds + r + 1]);
       if (a == b) continue;
       const uint32_t piece_a = a / kPiece, piece_b = (b - 1) / kPiece, whole_a = a / kWhole, whole_b = (b - 1) / kWhole;
-      if (p.piece == nullptr || piece_a == piece_b) {
+      if (piece_a == piece_b) {
         add_rows<T, Q, NARROW>(dy, p.dy.ld, p.token + all + (uint64_t)block * kSorted, a, b, c, p.cols, sum);
         continue;
       }
@@ -480,6 +454,51 @@ __global__ void __launch_bounds__(kBlock) embed_grad_kernel(EmbedGradTask p) {
   }
 }
 
+// Of few tokens: a workgroup looks at all of them for those of its rows.  4 x 33 tokens into 1000 x 256 4.3 us, 200 into 32000 x 2048 37, 262 MB; a launch that
+// sorted them first, by counting for each token those before it, made 8.8 and 48 of that.  256 tokens of one row are the longest chain, 13.
+template <typename T, int LANES, int Q, bool NARROW>
+__global__ void __launch_bounds__(kBlock) embed_grad_few_kernel(EmbedGradTask p, bool longs) {
+  constexpr uint32_t kAtATime = kBlock / LANES, kWaves = kBlock / kWave;
+  __shared__ uint64_t has[kMostEach][kWaves];  // which lanes of a wavefront have a token of a row
+  __shared__ uint32_t token[kFew];             // row by row, in the order that they came in
+  const uint32_t m = blockIdx.z, t = threadIdx.x, lane = t % kWave, wave = t / kWave, sub = __builtin_amdgcn_readfirstlane(t / LANES);
+  const uint64_t v0 = (uint64_t)blockIdx.x * p.each, at = m * p.ids.pitch + min((uint64_t)t, p.rows - 1) * p.ids.ld;
+  const uint32_t rows = (uint32_t)min(p.vocabulary - v0, (uint64_t)p.each);
+  const uint64_t id = (uint64_t)(longs ? static_cast<const int64_t*>(p.ids.p)[at] : (int64_t)static_cast<const int32_t*>(p.ids.p)[at]);
+  const uint32_t row = t < p.rows && id - v0 < rows ? (uint32_t)(id - v0) : ~0u;
+  for (uint32_t r = 0; r < rows; ++r) {
+    const uint64_t mine = __ballot(row == r);
+    if (lane == 0) has[r][wave] = mine;
+  }
+  __syncthreads();
+  // a lane counts a row's tokens; upto: those of all rows up to it
+  uint32_t upto = 0u;
+  if (lane < rows) {
+#pragma unroll
+    for (uint32_t w = 0; w < kWaves; ++w) upto += __popcll(has[lane][w]);
+  }
+#pragma unroll
+  for (uint32_t off = 1; off < kMostEach; off *= 2) {
+    const uint32_t other = __shfl_up(upto, off, kWave);
+    if (lane >= off) upto += other;
+  }
+  const uint32_t before = __shfl(upto, (int)min(row, kMostEach) - 1, kWave);
+  if (row != ~0u) {
+    uint32_t to = (row > 0u ? before : 0u) + __popcll(has[row][wave] & ((1ull << lane) - 1ull));
+    for (uint32_t w = 0; w < wave; ++w) to += __popcll(has[row][w]);
+    token[to] = t;
+  }
+  __syncthreads();
+  const Columns<Q> c = columns_of<LANES, Q, NARROW>(blockIdx.y, t % LANES, p.cols);
+  const T* dy = static_cast<const T*>(p.dy.p) + m * p.dy.pitch;
+  for (uint32_t r = sub; r < rows; r += kAtATime) {
+    float sum[Q][4] = {};
+    const uint32_t a = r > 0u ? (uint32_t)__builtin_amdgcn_readlane((int)upto, (int)r - 1) : 0u, b = (uint32_t)__builtin_amdgcn_readlane((int)upto, (int)r);
+    add_rows<T, Q, NARROW>(dy, p.dy.ld, token, a, b, c, p.cols, sum);
+    store_sum<Q, NARROW>(static_cast<float*>(p.dtable.p) + m * p.dtable.pitch + (v0 + r) * p.dtable.ld, c, p.cols, sum, p.scale, p.past);
+  }
+}
+
 __global__ void __launch_bounds__(kBlock) embed_grad_nothing_kernel(uint64_t rows, uint64_t cols, View y) {
   const uint64_t e = block_number() * kBlock + threadIdx.x;
   if (e >= rows * cols) return;
@@ -487,22 +506,19 @@ __global__ void __launch_bounds__(kBlock) embed_grad_nothing_kernel(uint64_t row
   static_cast<float*>(y.p)[blockIdx.z * y.pitch + r * y.ld + (e - r * cols)] = 0.f;
 }
 
-// How many of a block's places are written, and whether sums of pieces are taken (of few tokens no chain is long).
-uint32_t places_of(uint64_t rows) {
-  if (rows <= kFewSorted) return kFewSorted;
-  return rows <= 1024 ? 1024u : rows <= 2048 ? 2048u : kSorted;
-}
-constexpr uint64_t kPiecesFrom = 4 * kPiece, kWholesFrom = 4096;
+// How many of a block's places are written.
+uint32_t places_of(uint64_t rows) { return rows <= 1024 ? 1024u : rows <= 2048 ? 2048u : kSorted; }
 
 // What the gradient keeps, in words of 32 bits.
 uint64_t embed_grad_layout(EmbedGradTask& p, uint32_t workers, uint32_t* scratch) {
   p.blocks = (uint32_t)((p.rows + kSorted - 1) / kSorted);
   p.places = places_of(p.rows);
   // Where rows have tokens they take time one after another; where most have none, what a workgroup does before its first one counts.
-  p.each = p.rows * 4 >= p.vocabulary ? 4 : 16;
+  p.each = p.rows * 4 >= p.vocabulary ? 4 : kMostEach;
   p.groups = (uint32_t)((p.vocabulary + p.each - 1) / p.each);
   p.bits = 1;
   while (p.vocabulary >> p.bits != 0) ++p.bits;
+  if (p.rows <= kFew) return 0;
   const uint64_t blocks = (uint64_t)workers * p.blocks;
   uint64_t at = 0;
   auto take = [&](uint64_t words) {
@@ -513,9 +529,8 @@ uint64_t embed_grad_layout(EmbedGradTask& p, uint32_t workers, uint32_t* scratch
   p.row = take(blocks * kSorted);
   p.token = take(blocks * kSorted);
   p.begin = take(blocks * (p.groups + 1));
-  p.piece = p.whole = nullptr;
-  if (p.rows >= kPiecesFrom) p.piece = reinterpret_cast<float*>(take(blocks * (p.places / kPiece) * 2 * p.cols));
-  if (p.places >= kWholesFrom) p.whole = reinterpret_cast<float*>(take(blocks * (p.places / kWhole) * 2 * p.cols));
+  p.piece = reinterpret_cast<float*>(take(blocks * (p.places / kPiece) * 2 * p.cols));
+  p.whole = p.places < kSorted ? nullptr : reinterpret_cast<float*>(take(blocks * (p.places / kWhole) * 2 * p.cols));
   return at;
 }
 
@@ -525,7 +540,6 @@ void sort_typed(uint32_t workers, const EmbedGradTask& p, hipStream_t s) {
   const dim3 grid(p.blocks, workers);
   auto launch = [&](auto items) { embed_sort_kernel<I, items><<<grid, kSortThreads, 0, s>>>(p, digit, passes); };
   switch (p.places) {
-    case kFewSorted: embed_sort_few_kernel<I><<<grid, kFewSorted, 0, s>>>(p); break;
     case 1024: launch(std::integral_constant<int, 1>{}); break;
     case 2048: launch(std::integral_constant<int, 2>{}); break;
     default: launch(std::integral_constant<int, kSorted / kSortThreads>{});
@@ -533,13 +547,16 @@ void sort_typed(uint32_t workers, const EmbedGradTask& p, hipStream_t s) {
 }
 
 template <typename T, bool NARROW>
-void embed_grad_typed(uint32_t workers, const EmbedGradTask& p, hipStream_t s) {
+void embed_grad_typed(uint32_t workers, const EmbedGradTask& p, bool longs, hipStream_t s) {
   const size_t lds = p.blocks * (p.each + 1) * sizeof(uint32_t);
   auto launch = [&](auto lanes, auto fours) {
     const uint32_t across = (uint32_t)((p.cols + lanes * fours * 4 - 1) / (lanes * fours * 4)), at_a_time = kBlock / lanes;
+    if (p.rows <= kFew) {
+      embed_grad_few_kernel<T, lanes, fours, NARROW><<<dim3(p.groups, across, workers), kBlock, 0, s>>>(p, longs);
+      return;
+    }
     const uint32_t pieces = p.blocks * (p.places / kPiece), wholes = p.blocks * (p.places / kWhole);
-    if (p.piece != nullptr)
-      embed_pieces_kernel<T, false, lanes, fours, NARROW><<<dim3((pieces + at_a_time - 1) / at_a_time, across, workers), kBlock, 0, s>>>(p);
+    embed_pieces_kernel<T, false, lanes, fours, NARROW><<<dim3((pieces + at_a_time - 1) / at_a_time, across, workers), kBlock, 0, s>>>(p);
     if (p.whole != nullptr)
       embed_pieces_kernel<T, true, lanes, fours, NARROW><<<dim3((wholes + at_a_time - 1) / at_a_time, across, workers), kBlock, 0, s>>>(p);
     embed_grad_kernel<T, lanes, fours, NARROW><<<dim3(p.groups, across, workers), kBlock, lds, s>>>(p);
@@ -593,15 +610,13 @@ hipError_t launch_embed_grad(tng_type of_ids, tng_type type, uint32_t workers, u
   p.scale = scale;
   p.past = (uint64_t)workers * vocabulary * cols * sizeof(float) > kPast;
   embed_grad_layout(p, workers, scratch);
-  if (of_ids == TNG_TYPE_I32)
-    sort_typed<int32_t>(workers, p, s);
-  else
-    sort_typed<int64_t>(workers, p, s);
+  const bool longs = of_ids == TNG_TYPE_I64;
+  if (p.rows > kFew) longs ? sort_typed<int64_t>(workers, p, s) : sort_typed<int32_t>(workers, p, s);
   auto grad = [&](auto narrow) {
     switch (type) {
-      case TNG_TYPE_F32: embed_grad_typed<float, narrow>(workers, p, s); break;
-      case TNG_TYPE_BF16: embed_grad_typed<bf16_t, narrow>(workers, p, s); break;
-      default: embed_grad_typed<f16_t, narrow>(workers, p, s); break;
+      case TNG_TYPE_F32: embed_grad_typed<float, narrow>(workers, p, longs, s); break;
+      case TNG_TYPE_BF16: embed_grad_typed<bf16_t, narrow>(workers, p, longs, s); break;
+      default: embed_grad_typed<f16_t, narrow>(workers, p, longs, s); break;
     }
   };
   if (cols < 4)
