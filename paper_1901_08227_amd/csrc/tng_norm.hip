@@ -599,6 +599,10 @@ __global__ void __launch_bounds__(kBlock) rms_norm_grad_join_kernel(const float*
 // take 71; 8 x 100 x 18000 40 and 32; 2048 x 16384 52 and 64.)
 constexpr uint64_t kHeldCols = 16384;
 
+// So many rows one after another take less than parts that have to be joined, by a launch more: 8 rows of 1000 bfloat16, two for each wavefront, 4.8 us and 5.6, 2
+// of 4096 4.7 and 5.4 (four after another 7.6 and 5.4).
+constexpr uint64_t kTurns = 2;
+
 // Workgroups of a worker: as many as run at a time, but no more than there are rows for.
 uint32_t grad_parts(const Extent& n) {
   const uint64_t groups = n.cols <= 1024 ? kBlock / kWave : 1;  // rows that a workgroup has at a time
@@ -606,7 +610,8 @@ uint32_t grad_parts(const Extent& n) {
   // 59 / 56 / 69 / 68, 2048 x 16384 64 / 71 / 81 / 87)
   const uint64_t most = n.cols <= 512 ? 1024 : n.cols <= 1024 ? 512 : n.cols <= 4096 ? 768 : n.cols <= 8192 ? 512 : n.cols <= kHeldCols ? 256 : 512, tiles = n.cols > kHeldCols ? (n.cols + kBlock * 8 - 1) / (kBlock * 8) : 1;
   const uint64_t each = std::max<uint64_t>(1, most / (n.workers * tiles)), rows = (n.rows + groups - 1) / groups;
-  return (uint32_t)std::min(each, std::max<uint64_t>(1, rows));
+  if (rows <= kTurns) return 1;
+  return (uint32_t)std::min(each, rows);
 }
 
 template <typename T>
@@ -659,6 +664,8 @@ hipError_t launch_rms_norm_grad(tng_type type, const Extent& n, const View& dy, 
   const uint32_t parts = grad_parts(n);
   NormGradTask p{n.rows, n.cols, dy, h, residual, dx, norm.weight, norm.eps, dw == nullptr ? nullptr : scratch, parts, nullptr};
   p.row_part = scratch + (uint64_t)n.workers * parts * n.cols;
+  const bool joined = dw != nullptr && (parts > 1 || n.rows == 0);  // (one part is dw itself)
+  if (!joined) p.part = dw;
   if (n.rows > 0) {
     switch (type) {
       case TNG_TYPE_F32: norm_grad_typed<float>(n.workers, p, s); break;
@@ -666,7 +673,7 @@ hipError_t launch_rms_norm_grad(tng_type type, const Extent& n, const View& dy, 
       default: norm_grad_typed<f16_t>(n.workers, p, s); break;
     }
   }
-  if (dw != nullptr)
+  if (joined)
     rms_norm_grad_join_kernel<<<dim3((uint32_t)((n.cols + kWave - 1) / kWave), n.workers), kBlock, 0, s>>>(scratch, n.rows > 0 ? parts : 0u, n.cols,
                                                                                                      dw);
   return hipGetLastError();
