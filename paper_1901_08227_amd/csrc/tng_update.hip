@@ -197,7 +197,9 @@ constexpr uint32_t turn_pitch(int tiles) { return tiles * 16 + 4; }
 // A wavefront makes RN x CN tiles of 16 x 16 results, WR x WC of them a workgroup's tile.  A stage is 32 columns of the operands' rows, 128 bytes each; SLOTS of them lie
 // in LDS.  While the products of a stage run, the next one's fragments are read into registers, and the loads of the stage that follows the last one in LDS
 // are asked for, in the place of the one that has been read: one wait and one barrier a stage.  Tiles of 128 take 0.55 us a stage, those of 64, two
-// on a CU, 0.34: the loads, of 32 and 16 KB a tile and stage out of the die's cache.
+// on a CU, 0.34: the loads, of 32 and 16 KB a tile and stage out of the die's cache.  Tiles of 128 by four wavefronts, two on a CU, take 1.1, as long, but one
+// tile's beginning and end pass while the other is multiplied: 4 x 2053 x 1003 748 -> 703 us, 100 x 256 x 256 357 -> 317.  (A meeting every other stage, with five in
+// LDS: no sooner.)
 template <int RN, int CN, int WR, int WC, int SLOTS>
 struct PairKernel {
   static constexpr int kRows = RN * WR * 16, kCols = CN * WC * 16, kWaves = WR * WC, kThreads = kWaves * kWave;
@@ -571,7 +573,7 @@ struct Shape {
   double stage, alone, rest;
 };
 constexpr uint32_t kCus = 256;
-constexpr Shape kShapes[] = {{256, 256, 2.0, 2.0, 10.}, {192, 256, 1.25, 1.25, 9.}, {128, 256, 0.55, 0.55, 8.}, {64, 512, 0.34, 0.25, 4.}};
+constexpr Shape kShapes[] = {{256, 256, 2.0, 2.0, 10.}, {192, 256, 1.25, 1.25, 9.}, {128, 256, 0.55, 0.55, 8.}, {64, 512, 0.34, 0.25, 4.}, {128, 512, 1.1, 0.8, 8.}};
 
 // How a product is made: whatever tiles, and pieces of the tiles that would have the chip to themselves at the end, an estimate of the time says.  (Four
 // steps' products of one size with one kind of tile, us: 4096 x 4096 with 256, 192, 128 and 64: 3890, 3500, 4290, 4790, and 3270 by the estimate; 256 x 4096: 1330,
@@ -623,7 +625,8 @@ void product(PairTask p, hipStream_t s) {
     case 0: launch(pair_large_kernel<T, END, 8, 4, 2, 4, 2, 2>, pair_join_kernel<T, END, 8, 4, 2, 4>, 512, 4); break;
     case 1: launch(pair_large_kernel<T, END, 6, 3, 2, 4, 3, 1>, pair_join_kernel<T, END, 6, 3, 2, 4>, 512, 3); break;
     case 2: launch(pair_kernel<T, END, 4, 2, 2, 4, 4>, pair_join_kernel<T, END, 4, 2, 2, 4>, 512, 2); break;
-    default: launch(pair_kernel<T, END, 2, 2, 2, 2, 4>, pair_join_kernel<T, END, 2, 2, 2, 2>, 256, 1); break;
+    case 3: launch(pair_kernel<T, END, 2, 2, 2, 2, 4>, pair_join_kernel<T, END, 2, 2, 2, 2>, 256, 1); break;
+    default: launch(pair_kernel<T, END, 4, 4, 2, 2, 2>, pair_join_kernel<T, END, 4, 4, 2, 2>, 256, 2); break;
   }
 }
 

@@ -155,3 +155,9 @@ def test_few_long_rows(shape):
     assert near(y, host(x), QUINTIC, 1e-7, 1.25) and torch.equal(update.orthogonalize(x, scale=1.25), y)
     assert near(update.orthogonalize(x[:1], scale=1.25), host(x[:1]), QUINTIC, 1e-7, 1.25)
     assert near(update.orthogonalize(x.transpose(1, 2).contiguous(), scale=1.25).transpose(1, 2), host(x), QUINTIC, 1e-7, 1.25)
+
+
+# with those above: each product by every kind of tiles that the estimate takes for it, whole ones and such as several workgroups share
+@pytest.mark.parametrize("shape", [(1, 2900, 2891), (15, 915, 949), (3, 1162, 1109), (1, 2544, 1603), (15, 873, 595), (2, 1795, 2372)])
+def test_all_kinds_of_tiles(shape):
+    test_large(shape, 2)
