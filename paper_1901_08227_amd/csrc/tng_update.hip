@@ -80,6 +80,17 @@ __global__ void __launch_bounds__(kBlock) squares_kernel(StartTask p) {
   p.part[(uint64_t)m * p.parts + blockIdx.x] = sum;
 }
 
+__device__ __forceinline__ double sum_of_parts(const double* part, uint32_t parts, uint32_t lane) {
+  double sum = 0.;
+  for (uint32_t k = lane; k < parts; k += kWave) sum += part[k];
+  for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, kWave);
+  return sum;
+}
+// What x is multiplied by, from its squares.  (A matrix that holds what is not finite is NaN as a whole.)
+__device__ __forceinline__ double inverse_of(double squares, float eps) {
+  return (squares < __builtin_inf() ? 1. / (sqrt(squares) + (double)eps) : __builtin_nan("")) * (double)kOfX;
+}
+
 // 64 x 64 elements of x for a workgroup: as pairs along the columns, and turned, along the rows.
 constexpr uint32_t kTurn = 64;
 
@@ -89,14 +100,11 @@ __global__ void __launch_bounds__(kBlock) start_kernel(StartTask p) {
   __shared__ double inverse;
   const uint32_t m = blockIdx.z;
   if (threadIdx.x < kWave) {
-    double sum = 0.;
-    for (uint32_t k = threadIdx.x; k < p.parts; k += kWave) sum += p.part[(uint64_t)m * p.parts + k];
-    for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, kWave);
-    // (a matrix that holds what is not finite is NaN as a whole)
-    if (threadIdx.x == 0) inverse = sum < __builtin_inf() ? 1. / (sqrt(sum) + (double)p.eps) : __builtin_nan("");
+    const double sum = sum_of_parts(p.part + (uint64_t)m * p.parts, p.parts, threadIdx.x);
+    if (threadIdx.x == 0) inverse = inverse_of(sum, p.eps);
   }
   __syncthreads();
-  const double inv = inverse * (double)kOfX;
+  const double inv = inverse;
   const T* x = static_cast<const T*>(p.x.p) + m * p.x.pitch;
   const uint64_t r0 = (uint64_t)blockIdx.y * kTurn, c0 = (uint64_t)blockIdx.x * kTurn;
   const Pairs along = p.tall ? p.x_by_m : p.x_by_n, turned = p.tall ? p.x_by_n : p.x_by_m;
@@ -630,22 +638,12 @@ void product(PairTask p, hipStream_t s) {
   }
 }
 
-// ---- Small matrices: a workgroup each, everything in one launch.
+// ---- Small matrices: a workgroup each, everything in one launch; and few rows of longer ones, a strip of columns for each workgroup and a launch a step.
 //
 // A wavefront holds CT tiles of 16 columns of X, all NT of their tiles of rows, as its matrix instructions leave them: four consecutive rows of a column a
 // lane.  P X takes them from there: which of P's columns meets which of X's rows in a lane's eight is free as long as both sides agree, so a lane's
-// two fours of rows are its eight, and P's are read from LDS in that order.  Only X X^T wants rows of X, through LDS, where a word is a pair.  16 x 64 x 256 in
-// five steps: 28 us, by the latencies of four meetings a step; three launches a step were 80.
+// two fours of rows are its eight, and P's are read from LDS in that order.  Only X X^T wants rows of X, through LDS, where a word is a pair.
 constexpr int kSmallWaves = 8, kSmallSteps = 64;
-
-struct SmallTask {
-  uint32_t n, m, steps;
-  bool tall;
-  View x, y;
-  tng_type of_x, of_y;
-  float eps, scale;
-  float abc[3 * kSmallSteps];
-};
 
 // Eight pairs, or four and four, as fragments.
 __device__ __forceinline__ void fragments_of(const uint32_t* first, const uint32_t* second, v8h& high, v8h& low) {
@@ -668,72 +666,92 @@ __device__ __forceinline__ uint32_t pair_of(float v) {
   return (uint32_t)__builtin_bit_cast(uint16_t, h) | (uint32_t)__builtin_bit_cast(uint16_t, l) << 16;
 }
 
+// What both kernels do; all of a workgroup come to each of these as often as the others.
 template <int NT, int CT>
-__global__ void __launch_bounds__(kSmallWaves* kWave) small_kernel(SmallTask p) {
+struct Small {
   static_assert(NT % 2 == 0, "a lane's eight are two tiles' fours");
-  constexpr int kRows = NT * 16, kCols = CT * 16 * kSmallWaves, kPitch = kCols + 4, kSquare = kRows + 4, kTiles = NT * (NT + 1) / 2;
-  constexpr int kMine = (kTiles + kSmallWaves - 1) / kSmallWaves;
+  static constexpr int kRows = NT * 16, kCols = CT * 16 * kSmallWaves, kPitch = kCols + 4, kSquare = kRows + 4, kTiles = NT * (NT + 1) / 2;
+  static constexpr int kMine = (kTiles + kSmallWaves - 1) / kSmallWaves;
   typedef uint32_t four __attribute__((ext_vector_type(4)));
-  __shared__ __align__(16) uint32_t of_x[kRows * kPitch];
-  __shared__ __align__(16) uint32_t of_p[kRows * kSquare];  // G, then P
-  __shared__ double of_wave[kSmallWaves];
-  const uint32_t lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), i = lane % 16, g = lane / 16, m = blockIdx.x;
-  const uint32_t c_in = wave * CT * 16 + i, r_in = g * 4;
-  const uint64_t by_r = p.tall ? 1 : p.x.ld, by_c = p.tall ? p.x.ld : 1;
+  typedef v4f Strip[NT][CT];
+  typedef v8h Fragments[NT / 2][CT];
+  uint32_t *of_x, *of_p;  // LDS: [kRows][kPitch]; [kRows][kSquare], G, then P
+  uint32_t lane, wave, i, g, r_in;
 
-  v4f x[NT][CT];
-  auto load = [&](auto of) {
-    using T = decltype(of);
-    const T* from = static_cast<const T*>(p.x.p) + m * p.x.pitch;
+  __device__ __forceinline__ Small(uint32_t* x, uint32_t* p) : of_x(x), of_p(p) {
+    lane = threadIdx.x % kWave;
+    wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    i = lane % 16;
+    g = lane / 16;
+    r_in = g * 4;
+  }
+  __device__ __forceinline__ uint32_t column(int b) const { return wave * CT * 16 + i + b * 16; }
+
+  // n rows and m columns of X, which is what lies there, or, where that is tall, what lies there turned: then a lane's four are side by side.
+  template <typename T>
+  __device__ __forceinline__ void load(const T* from, bool tall, uint64_t ld, uint32_t n, uint32_t m, Strip& x) const {
+    if (tall) {
+#pragma unroll
+      for (int a = 0; a < NT; ++a)
+#pragma unroll
+        for (int b = 0; b < CT; ++b) {
+          const uint32_t r = r_in + a * 16, c = min(column(b), m - 1);  // (past the end: the last one, which is not used)
+          float v[4] = {0.f, 0.f, 0.f, 0.f};
+          if (r < n) load_n_within<T, 4>(from + c * ld + r, n - r, 0.f, v);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) x[a][b][k] = v[k];
+          if (b == CT - 1) __builtin_amdgcn_sched_barrier(0);
+        }
+      return;
+    }
 #pragma unroll
     for (int a = 0; a < NT; ++a)
 #pragma unroll
       for (int b = 0; b < CT; ++b)
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          const uint32_t r = r_in + a * 16 + k, c = c_in + b * 16;  // (past the end: the last one, which is not used)
-          x[a][b][k] = (float)from[min(r, p.n - 1) * by_r + min(c, p.m - 1) * by_c];
+          x[a][b][k] = (float)from[min(r_in + a * 16 + k, n - 1) * ld + min(column(b), m - 1)];
           if (b == CT - 1 && k == 3) __builtin_amdgcn_sched_barrier(0);
         }
-  };
-  switch (p.of_x) {
-    case TNG_TYPE_F32: load(float{}); break;
-    case TNG_TYPE_BF16: load(bf16_t{}); break;
-    default: load(f16_t{}); break;
   }
-  double sum = 0.;
+  template <typename T>
+  __device__ __forceinline__ void store(T* to, bool tall, uint64_t ld, uint32_t n, uint32_t m, const Strip& x) const {
+    // (a barrier behind each tile: so many addresses at once leave no registers)
+    if (tall) {
 #pragma unroll
-  for (int a = 0; a < NT; ++a)
+      for (int a = 0; a < NT; ++a)
 #pragma unroll
-    for (int b = 0; b < CT; ++b)
+        for (int b = 0; b < CT; ++b) {
+          const uint32_t r = r_in + a * 16, c = column(b);
+          const float v[4] = {x[a][b][0], x[a][b][1], x[a][b][2], x[a][b][3]};
+          if (r < n && c < m) store_n_within<T, 4>(to + c * ld + r, n - r, v);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      return;
+    }
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (r_in + a * 16 + k < p.n && c_in + b * 16 < p.m) sum += (double)x[a][b][k] * (double)x[a][b][k];
-  for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, kWave);
-  if (lane == 0) of_wave[wave] = sum;
-  __syncthreads();
-  sum = 0.;
-  for (int k = 0; k < kSmallWaves; ++k) sum += of_wave[k];
-  const double inv = (sum < __builtin_inf() ? 1. / (sqrt(sum) + (double)p.eps) : __builtin_nan("")) * (double)kOfX;
+    for (int a = 0; a < NT; ++a)
 #pragma unroll
-  for (int a = 0; a < NT; ++a)
+      for (int b = 0; b < CT; ++b)
 #pragma unroll
-    for (int b = 0; b < CT; ++b)
+        for (int k = 0; k < 4; ++k) {
+          const uint32_t r = r_in + a * 16 + k, c = column(b);
+          if (r < n && c < m) to[r * ld + c] = (T)x[a][b][k];
+          if (k == 3) __builtin_amdgcn_sched_barrier(0);
+        }
+  }
+  __device__ __forceinline__ void scale(double inv, uint32_t n, uint32_t m, Strip& x) const {
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-        x[a][b][k] = r_in + a * 16 + k < p.n && c_in + b * 16 < p.m ? (float)((double)x[a][b][k] * inv) : 0.f;
+    for (int a = 0; a < NT; ++a)
+#pragma unroll
+      for (int b = 0; b < CT; ++b)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[a][b][k] = r_in + a * 16 + k < n && column(b) < m ? (float)((double)x[a][b][k] * inv) : 0.f;
+  }
 
-  // The tile of a number: rows first, c <= r.
-  auto place = [](uint32_t number, uint32_t* r, uint32_t* c) {
-    uint32_t row = 0;
-    while (number > row) number -= ++row;
-    *r = row;
-    *c = number;
-  };
-  v8h high[NT / 2][CT], low[NT / 2][CT];
-  for (uint32_t step = 0; step < p.steps; ++step) {
-    const float plus = p.abc[3 * step], times = p.abc[3 * step + 1], square = p.abc[3 * step + 2];
-    // X as fragments here, and as pairs in LDS
+  // X as fragments, and as pairs in LDS.
+  template <bool FRAGMENTS, bool LDS>
+  __device__ __forceinline__ void divide(const Strip& x, Fragments& high, Fragments& low) const {
 #pragma unroll
     for (int a = 0; a < NT; ++a)
 #pragma unroll
@@ -742,46 +760,57 @@ __global__ void __launch_bounds__(kSmallWaves* kWave) small_kernel(SmallTask p) 
         for (int k = 0; k < 4; ++k) {
           f16_t h, l;
           split(x[a][b][k], h, l);
-          high[a / 2][b][a % 2 * 4 + k] = h;
-          low[a / 2][b][a % 2 * 4 + k] = l;
-          of_x[(a * 16 + r_in + k) * kPitch + c_in + b * 16] = (uint32_t)__builtin_bit_cast(uint16_t, h) | (uint32_t)__builtin_bit_cast(uint16_t, l) << 16;
+          if (FRAGMENTS) {
+            high[a / 2][b][a % 2 * 4 + k] = h;
+            low[a / 2][b][a % 2 * 4 + k] = l;
+          }
+          if (LDS) of_x[(a * 16 + r_in + k) * kPitch + column(b)] = (uint32_t)__builtin_bit_cast(uint16_t, h) | (uint32_t)__builtin_bit_cast(uint16_t, l) << 16;
         }
-    __syncthreads();
-    // G: of each wavefront's tiles
-#pragma unroll 1
-    for (uint32_t t = wave; t < kTiles; t += kSmallWaves) {
-      uint32_t tr, tc;
-      place(t, &tr, &tc);
-      v4f main = {0.f, 0.f, 0.f, 0.f}, cross = {0.f, 0.f, 0.f, 0.f};
-      const uint32_t *ra = of_x + (tr * 16 + i) * kPitch + g * 8, *rb = of_x + (tc * 16 + i) * kPitch + g * 8;
-#pragma unroll 2
-      for (uint32_t k = 0; k < kCols; k += 32) {
-        v8h ah, al, bh, bl;
-        fragments_of(ra + k, ra + k + 4, ah, al);
-        fragments_of(rb + k, rb + k + 4, bh, bl);
-        cross = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah, bl, cross, 0, 0, 0);
-        main = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah, bh, main, 0, 0, 0);
-        cross = __builtin_amdgcn_mfma_f32_16x16x32_f16(al, bh, cross, 0, 0, 0);
-      }
-      four pair;
+  }
+
+  // The tile of a number: rows first, c <= r.
+  static __device__ __forceinline__ Place place(uint32_t number) {
+    uint32_t row = 0;
+    while (number > row) number -= ++row;
+    return Place{row, number};
+  }
+  __device__ __forceinline__ void put(const Place& at, const four& pair) const {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        pair[k] = pair_of((main[k] + cross[k]) * (kOfGram / (kOfX * kOfX)));
-        of_p[(tr * 16 + r_in + k) * kSquare + tc * 16 + i] = pair[k];
-      }
-      if (tr != tc) *reinterpret_cast<four*>(of_p + (tc * 16 + i) * kSquare + tr * 16 + r_in) = pair;
+    for (int k = 0; k < 4; ++k) of_p[(at.r * 16 + r_in + k) * kSquare + at.c * 16 + i] = pair[k];
+    if (at.r != at.c) *reinterpret_cast<four*>(of_p + (at.c * 16 + i) * kSquare + at.r * 16 + r_in) = pair;
+  }
+  // A tile of X X^T times kOfX^2, of what is in LDS.
+  __device__ __forceinline__ v4f gram(const Place& at) const {
+    v4f main = {0.f, 0.f, 0.f, 0.f}, cross = {0.f, 0.f, 0.f, 0.f};
+    const uint32_t *ra = of_x + (at.r * 16 + i) * kPitch + g * 8, *rb = of_x + (at.c * 16 + i) * kPitch + g * 8;
+#pragma unroll 2
+    for (uint32_t k = 0; k < kCols; k += 32) {
+      v8h ah, al, bh, bl;
+      fragments_of(ra + k, ra + k + 4, ah, al);
+      fragments_of(rb + k, rb + k + 4, bh, bl);
+      cross = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah, bl, cross, 0, 0, 0);
+      main = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah, bh, main, 0, 0, 0);
+      cross = __builtin_amdgcn_mfma_f32_16x16x32_f16(al, bh, cross, 0, 0, 0);
     }
-    __syncthreads();
-    // P, in the place of G
+    return main + cross;
+  }
+  static __device__ __forceinline__ four pairs_of_gram(const v4f& sum) {
+    four pair;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) pair[k] = pair_of(sum[k] * (kOfGram / (kOfX * kOfX)));
+    return pair;
+  }
+
+  // P, in the place of G.
+  __device__ __forceinline__ void polynomial(float plus, float times, float square) const {
     four made[kMine];
 #pragma unroll
     for (int n = 0; n < kMine; ++n) {
       const uint32_t t = wave + n * kSmallWaves;
       if (t >= kTiles) continue;
-      uint32_t tr, tc;
-      place(t, &tr, &tc);
+      const Place at = place(t);
       v4f all = {0.f, 0.f, 0.f, 0.f};
-      const uint32_t *ra = of_p + (tr * 16 + i) * kSquare + g * 8, *rb = of_p + (tc * 16 + i) * kSquare + g * 8;
+      const uint32_t *ra = of_p + (at.r * 16 + i) * kSquare + g * 8, *rb = of_p + (at.c * 16 + i) * kSquare + g * 8;
 #pragma unroll
       for (uint32_t k = 0; k < kRows; k += 32) {
         v8h ah, al, bh, bl;
@@ -793,26 +822,22 @@ __global__ void __launch_bounds__(kSmallWaves* kWave) small_kernel(SmallTask p) 
       }
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const uint32_t word = of_p[(tr * 16 + r_in + k) * kSquare + tc * 16 + i];
+        const uint32_t word = of_p[(at.r * 16 + r_in + k) * kSquare + at.c * 16 + i];
         const float gram = ((float)__builtin_bit_cast(f16_t, (uint16_t)word) + (float)__builtin_bit_cast(f16_t, (uint16_t)(word >> 16))) * (1.f / kOfGram);
-        made[n][k] = pair_of((times * gram + square * (all[k] * (1.f / (kOfGram * kOfGram))) + (tr == tc && r_in + k == i ? plus : 0.f)) * kOfPoly);
+        made[n][k] = pair_of((times * gram + square * (all[k] * (1.f / (kOfGram * kOfGram))) + (at.r == at.c && r_in + k == i ? plus : 0.f)) * kOfPoly);
       }
     }
     __syncthreads();
 #pragma unroll
     for (int n = 0; n < kMine; ++n) {
       const uint32_t t = wave + n * kSmallWaves;
-      if (t >= kTiles) continue;
-      uint32_t tr, tc;
-      place(t, &tr, &tc);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) of_p[(tr * 16 + r_in + k) * kSquare + tc * 16 + i] = made[n][k];
-      if (tr != tc) *reinterpret_cast<four*>(of_p + (tc * 16 + i) * kSquare + tr * 16 + r_in) = made[n];
+      if (t < kTiles) put(place(t), made[n]);
     }
     __syncthreads();
-    // P X
-    const bool last = step + 1 == p.steps;
-    const float unit = last ? p.scale * (1.f / (kOfPoly * kOfX)) : kOfX / (kOfPoly * kOfX);
+  }
+
+  // P X times unit, in the place of X.
+  __device__ __forceinline__ void apply(const Fragments& high, const Fragments& low, float unit, Strip& x) const {
 #pragma unroll
     for (int a = 0; a < NT; ++a) {
       v4f all[CT] = {};
@@ -834,26 +859,139 @@ __global__ void __launch_bounds__(kSmallWaves* kWave) small_kernel(SmallTask p) 
         for (int k = 0; k < 4; ++k) x[a][b][k] = all[b][k] * unit;
     }
   }
-  auto store = [&](auto of) {
-    using T = decltype(of);
-    T* to = static_cast<T*>(p.y.p) + m * p.y.pitch;
-    const uint64_t to_r = p.tall ? 1 : p.y.ld, to_c = p.tall ? p.y.ld : 1;
-#pragma unroll
-    for (int a = 0; a < NT; ++a)
-#pragma unroll
-      for (int b = 0; b < CT; ++b)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const uint32_t r = r_in + a * 16 + k, c = c_in + b * 16;
-          if (r < p.n && c < p.m) to[r * to_r + c * to_c] = (T)x[a][b][k];
-          if (k == 3) __builtin_amdgcn_sched_barrier(0);  // (so many addresses at once leave no registers)
-        }
-  };
-  switch (p.of_y) {
-    case TNG_TYPE_F32: store(float{}); break;
-    case TNG_TYPE_BF16: store(bf16_t{}); break;
-    default: store(f16_t{}); break;
+};
+
+template <typename F>
+__device__ __forceinline__ void with_type(tng_type type, F f) {
+  switch (type) {
+    case TNG_TYPE_F32: f(float{}); break;
+    case TNG_TYPE_BF16: f(bf16_t{}); break;
+    default: f(f16_t{}); break;
   }
+}
+
+struct SmallTask {
+  uint32_t n, m, steps;
+  bool tall;
+  View x, y;
+  tng_type of_x, of_y;
+  float eps, scale;
+  float abc[3 * kSmallSteps];
+};
+
+// 16 x 64 x 256 in five steps: 28 us, by the latencies of four meetings a step; three launches a step were 80.
+template <int NT, int CT>
+__global__ void __launch_bounds__(kSmallWaves* kWave) small_kernel(SmallTask p) {
+  using K = Small<NT, CT>;
+  __shared__ __align__(16) uint32_t of_x[K::kRows * K::kPitch];
+  __shared__ __align__(16) uint32_t of_p[K::kRows * K::kSquare];
+  __shared__ double of_wave[kSmallWaves];
+  const K all(of_x, of_p);
+  const uint32_t m = blockIdx.x;
+  typename K::Strip x;
+  with_type(p.of_x, [&](auto of) {
+    using T = decltype(of);
+    all.load(static_cast<const T*>(p.x.p) + m * p.x.pitch, p.tall, p.x.ld, p.n, p.m, x);
+  });
+  double sum = 0.;
+#pragma unroll
+  for (int a = 0; a < NT; ++a)
+#pragma unroll
+    for (int b = 0; b < CT; ++b)
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (all.r_in + a * 16 + k < p.n && all.column(b) < p.m) sum += (double)x[a][b][k] * (double)x[a][b][k];
+  for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, kWave);
+  if (all.lane == 0) of_wave[all.wave] = sum;
+  __syncthreads();
+  sum = 0.;
+  for (int k = 0; k < kSmallWaves; ++k) sum += of_wave[k];
+  all.scale(inverse_of(sum, p.eps), p.n, p.m, x);
+  typename K::Fragments high, low;
+  for (uint32_t step = 0; step < p.steps; ++step) {
+    all.template divide<true, true>(x, high, low);
+    __syncthreads();
+#pragma unroll 1
+    for (uint32_t t = all.wave; t < K::kTiles; t += kSmallWaves) {
+      const Place at = K::place(t);
+      all.put(at, K::pairs_of_gram(all.gram(at)));
+    }
+    __syncthreads();
+    all.polynomial(p.abc[3 * step], p.abc[3 * step + 1], p.abc[3 * step + 2]);
+    all.apply(high, low, step + 1 == p.steps ? p.scale * (1.f / (kOfPoly * kOfX)) : kOfX / (kOfPoly * kOfX), x);
+  }
+  with_type(p.of_y, [&](auto of) {
+    using T = decltype(of);
+    all.store(static_cast<T*>(p.y.p) + m * p.y.pitch, p.tall, p.y.ld, p.n, p.m, x);
+  });
+}
+
+struct StripTask {
+  uint32_t n, m, step, steps;  // launches 0 .. steps
+  bool tall;
+  View x, y;
+  tng_type of_x, of_y;
+  float eps, scale;
+  float plus, times, square;  // of step - 1
+  const double* part;         // squares: [matrix][parts]
+  uint32_t parts;
+  float* state;               // [matrix][strip][tile of rows][tile of columns][thread][4]: X, from step 1 on
+  const float* sums;          // [matrix][strip][tile of X X^T][lane][4], from the launch before
+  float* next;                // the same for the next one
+};
+
+// A strip of columns in one step: X X^T from what all strips found of it, P, by every workgroup for itself, P X, and this strip's part of the next X X^T.  Latencies
+// bound it: 64 x 1024 in five steps is seven launches of 5 to 7 us, where tiles take three a step and more.
+template <int NT, int CT>
+__global__ void __launch_bounds__(kSmallWaves* kWave) strip_kernel(StripTask p) {
+  using K = Small<NT, CT>;
+  __shared__ __align__(16) uint32_t of_x[K::kRows * K::kPitch];
+  __shared__ __align__(16) uint32_t of_p[K::kRows * K::kSquare];
+  const K all(of_x, of_p);
+  const uint32_t m = blockIdx.y, strip = blockIdx.x, strips = gridDim.x;
+  const uint32_t c0 = strip * K::kCols, left = p.m - c0;
+  typename K::Strip x;
+  float* state = p.state + ((uint64_t)m * strips + strip) * (K::kRows * K::kCols) + threadIdx.x * 4;
+  if (p.step <= 1) {
+    with_type(p.of_x, [&](auto of) {
+      using T = decltype(of);
+      all.load(static_cast<const T*>(p.x.p) + m * p.x.pitch + c0 * (p.tall ? p.x.ld : 1), p.tall, p.x.ld, p.n, left, x);
+    });
+    all.scale(inverse_of(sum_of_parts(p.part + (uint64_t)m * p.parts, p.parts, all.lane), p.eps), p.n, left, x);
+  } else {
+#pragma unroll
+    for (int k = 0; k < NT * CT; ++k) x[k / CT][k % CT] = *reinterpret_cast<const v4f*>(state + k * (kSmallWaves * kWave * 4));
+  }
+  typename K::Fragments high, low;
+  if (p.step > 0) {
+    const float* sums = p.sums + (uint64_t)m * strips * (K::kTiles * 256) + all.lane * 4;
+#pragma unroll 1
+    for (uint32_t t = all.wave; t < K::kTiles; t += kSmallWaves) {
+      v4f sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+      for (uint32_t k = 0; k < strips; ++k) sum += *reinterpret_cast<const v4f*>(sums + ((uint64_t)k * K::kTiles + t) * 256);
+      all.put(K::place(t), K::pairs_of_gram(sum));
+    }
+    all.template divide<true, false>(x, high, low);
+    __syncthreads();
+    all.polynomial(p.plus, p.times, p.square);
+    const bool last = p.step == p.steps;
+    all.apply(high, low, last ? p.scale * (1.f / (kOfPoly * kOfX)) : kOfX / (kOfPoly * kOfX), x);
+    if (last) {
+      with_type(p.of_y, [&](auto of) {
+        using T = decltype(of);
+        all.store(static_cast<T*>(p.y.p) + m * p.y.pitch + c0 * (p.tall ? p.y.ld : 1), p.tall, p.y.ld, p.n, left, x);
+      });
+      return;
+    }
+#pragma unroll
+    for (int k = 0; k < NT * CT; ++k) *reinterpret_cast<v4f*>(state + k * (kSmallWaves * kWave * 4)) = x[k / CT][k % CT];
+  }
+  all.template divide<false, true>(x, high, low);
+  __syncthreads();
+  float* next = p.next + ((uint64_t)m * strips + strip) * (K::kTiles * 256) + all.lane * 4;
+#pragma unroll 1
+  for (uint32_t t = all.wave; t < K::kTiles; t += kSmallWaves) *reinterpret_cast<v4f*>(next + t * 256) = all.gram(K::place(t));
 }
 
 // As many columns as LDS holds beside the rows, in turns of 128.
@@ -879,6 +1017,64 @@ hipError_t launch_small(const SmallTask& p, uint32_t workers, hipStream_t s) {
   return hipGetLastError();
 }
 
+// Strips of this many columns, or 0: not by strips.  Every strip reads what all of them found of X X^T, so there are no more than sixteen.  (Five
+// steps, us, and by tiles: 64 x 1024 46 and 104, 32 x 4096 37 and 108, 64 x 8192 85 and 127, 100 x 64 x 1024 144 and 190, 100 x 64 x 8000 740 and 1055, with up to
+// 32 strips 77 and 1128 of the last 85 and 740; 96 x 1000 69 and 100, 64 x 96 x 1000 204 and 188, so not where the chip is full anyway.)
+constexpr uint32_t kMostStrips = 16;
+uint32_t strip_of(const Extent& e) {
+  const uint64_t n = std::min(e.rows, e.cols), m = std::max(e.rows, e.cols);
+  const uint32_t most = n <= 64 ? 512 : n <= 96 ? 256 : 0;  // (LDS has room for no more)
+  for (uint32_t cols = 128; cols <= most; cols *= 2) {
+    const uint64_t strips = (m + cols - 1) / cols;
+    if (strips <= kMostStrips) return n <= 64 || e.workers * strips <= kCus ? cols : 0;
+  }
+  return 0;
+}
+
+struct Strips {
+  uint64_t n, m;
+  uint32_t cols, count, parts;
+  double* part;
+  float *state, *sums[2];
+  uint64_t bytes;
+};
+uint32_t squares_parts(const Extent& e) {  // (four pieces of a row for each wavefront)
+  const uint64_t pieces = e.rows * ((e.cols + kWave * 8 - 1) / (kWave * 8));
+  return (uint32_t)std::min<uint64_t>(std::max<uint64_t>(1, 1024 / e.workers), (pieces + 15) / 16);
+}
+Strips strips_of(const Extent& e, char* scratch) {
+  Strips l{};
+  l.n = std::min(e.rows, e.cols);
+  l.m = std::max(e.rows, e.cols);
+  l.cols = strip_of(e);
+  l.count = (uint32_t)((l.m + l.cols - 1) / l.cols);
+  l.parts = squares_parts(e);
+  auto take = [&](uint64_t bytes) {
+    char* here = scratch + l.bytes;
+    l.bytes += (bytes + 255) / 256 * 256;
+    return here;
+  };
+  const uint64_t tiles = (l.n + 31) / 32 * 2, all = e.workers * (uint64_t)l.count;
+  l.part = reinterpret_cast<double*>(take(e.workers * (uint64_t)l.parts * sizeof(double)));
+  l.state = reinterpret_cast<float*>(take(all * tiles * 16 * l.cols * sizeof(float)));
+  for (float*& sums : l.sums) sums = reinterpret_cast<float*>(take(all * (tiles * (tiles + 1) / 2 * 256) * sizeof(float)));
+  return l;
+}
+void launch_strip(const StripTask& p, const Strips& l, uint32_t workers, hipStream_t s) {
+  auto launch = [&](auto rows, auto cols) { strip_kernel<rows, cols><<<dim3(l.count, workers), kSmallWaves * kWave, 0, s>>>(p); };
+  constexpr std::integral_constant<int, 1> one;
+  constexpr std::integral_constant<int, 2> two;
+  constexpr std::integral_constant<int, 4> four;
+  constexpr std::integral_constant<int, 6> six;
+  auto of_rows = [&](auto rows) { l.cols == 128 ? launch(rows, one) : l.cols == 256 ? launch(rows, two) : launch(rows, four); };
+  if (l.n <= 32)
+    of_rows(two);
+  else if (l.n <= 64)
+    of_rows(four);
+  else
+    l.cols == 128 ? launch(six, one) : launch(six, two);
+}
+
 struct Layout {
   uint64_t n, m;
   bool tall;
@@ -894,8 +1090,7 @@ Layout layout_of(const Extent& e, char* scratch) {
   l.tall = e.rows > e.cols;
   l.n = std::min(e.rows, e.cols);
   l.m = std::max(e.rows, e.cols);
-  const uint64_t elements = e.rows * e.cols;
-  l.parts = (uint32_t)std::min<uint64_t>(std::max<uint64_t>(1, 1024 / e.workers), (elements + 8191) / 8192);
+  l.parts = squares_parts(e);
   auto take = [&](uint64_t bytes) {
     char* here = scratch + l.bytes;
     l.bytes += (bytes + 255) / 256 * 256;
@@ -919,6 +1114,7 @@ Layout layout_of(const Extent& e, char* scratch) {
 template <typename T>
 void start(const StartTask& p, uint32_t workers, hipStream_t s) {
   squares_kernel<T><<<dim3(p.parts, workers), kBlock, 0, s>>>(p);
+  if (p.x_by_n.p == nullptr) return;
   start_kernel<T><<<dim3((uint32_t)((p.cols + kTurn - 1) / kTurn), (uint32_t)((p.rows + kTurn - 1) / kTurn), workers), kBlock, 0, s>>>(p);
 }
 
@@ -957,7 +1153,8 @@ bool orthogonal_in_range(const float* coefficients, uint32_t steps) {
 }
 
 size_t orthogonal_bytes(const Extent& e) {
-  return is_small(std::min(e.rows, e.cols), std::max(e.rows, e.cols)) ? 0 : layout_of(e, nullptr).bytes;
+  const uint64_t n = std::min(e.rows, e.cols), m = std::max(e.rows, e.cols);
+  return is_small(n, m) ? 0 : strip_of(e) != 0 ? strips_of(e, nullptr).bytes : layout_of(e, nullptr).bytes;
 }
 
 hipError_t launch_orthogonalize(tng_type of_x, tng_type of_y, const Extent& e, const View& x, const float* coefficients, uint32_t steps, float eps, float scale,
@@ -967,13 +1164,31 @@ hipError_t launch_orthogonalize(tng_type of_x, tng_type of_y, const Extent& e, c
     std::copy(coefficients, coefficients + 3 * steps, small.abc);
     return launch_small(small, e.workers, s);
   }
-  const Layout l = layout_of(e, scratch);
-  const StartTask first{e.rows, e.cols, x, l.part, l.parts, eps, l.tall, l.x_by_n, l.x_by_m[0]};
-  switch (of_x) {
-    case TNG_TYPE_F32: start<float>(first, e.workers, s); break;
-    case TNG_TYPE_BF16: start<bf16_t>(first, e.workers, s); break;
-    default: start<f16_t>(first, e.workers, s); break;
+  auto begin = [&](const StartTask& first) {
+    switch (of_x) {
+      case TNG_TYPE_F32: start<float>(first, e.workers, s); break;
+      case TNG_TYPE_BF16: start<bf16_t>(first, e.workers, s); break;
+      default: start<f16_t>(first, e.workers, s); break;
+    }
+  };
+  if (strip_of(e) != 0) {
+    const Strips l = strips_of(e, scratch);
+    begin(StartTask{e.rows, e.cols, x, l.part, l.parts, eps, false, {}, {}});
+    StripTask p{(uint32_t)l.n, (uint32_t)l.m, 0, steps, e.rows > e.cols, x, y, of_x, of_y, eps, scale, 0.f, 0.f, 0.f, l.part, l.parts, l.state, nullptr, nullptr};
+    for (; p.step <= steps; ++p.step) {
+      if (p.step > 0) {
+        p.plus = coefficients[3 * p.step - 3];
+        p.times = coefficients[3 * p.step - 2];
+        p.square = coefficients[3 * p.step - 1];
+      }
+      p.sums = l.sums[(p.step + 1) % 2];
+      p.next = l.sums[p.step % 2];
+      launch_strip(p, l, e.workers, s);
+    }
+    return hipGetLastError();
   }
+  const Layout l = layout_of(e, scratch);
+  begin(StartTask{e.rows, e.cols, x, l.part, l.parts, eps, l.tall, l.x_by_n, l.x_by_m[0]});
   const uint32_t n = (uint32_t)l.n, m = (uint32_t)l.m, n_stages = (n + kBlockCols - 1) / kBlockCols, m_stages = (m + kBlockCols - 1) / kBlockCols;
   for (uint32_t k = 0; k < steps; ++k) {
     const Pairs &now = l.x_by_m[k % 2], &then = l.x_by_m[1 - k % 2];

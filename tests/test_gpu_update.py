@@ -161,3 +161,39 @@ def test_few_long_rows(shape):
 @pytest.mark.parametrize("shape", [(1, 2900, 2891), (15, 915, 949), (3, 1162, 1109), (1, 2544, 1603), (15, 873, 595), (2, 1795, 2372)])
 def test_all_kinds_of_tiles(shape):
     test_large(shape, 2)
+
+
+# strips of 128, 256 and 512 columns, the last one whole or not, for 32, 64 and 96 rows; more matrices than strips are for
+@pytest.mark.parametrize("shape", [(3, 5, 1100), (2, 20, 3000), (1, 32, 8192), (1, 40, 2500), (2, 64, 8000), (1, 33, 8193), (1, 70, 1000), (2, 96, 2100), (40, 66, 900)])
+@pytest.mark.parametrize("steps", [1, 2, 5])
+def test_strips(shape, steps):
+    coefficients = QUINTIC[:steps]
+    for x in (normal(shape, torch.float32, 1, 1e-3), normal(shape, torch.float32, 2, 1e-3).transpose(1, 2).contiguous()):
+        y = update.orthogonalize(x, coefficients, scale=1.25)
+        wide = x.shape[1] < x.shape[2]
+        assert near(y if wide else y.transpose(1, 2), host(x) if wide else host(x.transpose(1, 2).contiguous()), coefficients, 1e-7, 1.25)
+        a = x.clone()
+        assert update.orthogonalize(a, coefficients, scale=1.25, out=a) is a and torch.equal(a, y)
+        out = spread(torch.zeros_like(x), 0)
+        assert update.orthogonalize(spread(x, 0), coefficients, scale=1.25, out=out) is out and torch.equal(out, y)
+        b = x.bfloat16()
+        assert same(update.orthogonalize(b, coefficients), update.orthogonalize(b.float(), coefficients).bfloat16().cpu())
+
+
+# a strip's launches, those of tiles, and of tiles that several workgroups share
+@pytest.mark.parametrize("shape", [(3, 50, 1300), (3, 300, 500), (3, 120, 3000)])
+def test_every_way_captured_and_with_what_is_not_finite(shape):
+    x = normal(shape, torch.float32, 50)
+    bad = x.clone()
+    bad[0, 3, 7], bad[1] = float("nan"), 0
+    got, want = update.orthogonalize(bad), update.orthogonalize(x)
+    assert got[0].isnan().all() and got[1].eq(0).all() and torch.equal(got[2], want[2])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        first, second = update.orthogonalize(x), update.orthogonalize(bad)
+    for k in range(3):
+        x.copy_(normal(shape, torch.float32, 60 + k))
+        bad.copy_(normal(shape, torch.float32, 70 + k))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(first, update.orthogonalize(x)) and torch.equal(second, update.orthogonalize(bad))
