@@ -399,9 +399,9 @@ tng_status tng_embed_grad(void* hip_stream, const tng_matrix* ids, const tng_mat
  *   X = x / (||x|| + eps);  for each of the steps, with its a, b, c:  G = X X^T,  X = (a + b G + c G G) X;  y = scale X
  * ||x||: the root of the sum of squares, in binary64.  Products are of pairs of binary16 that hold 22 bits of a number and more, but nothing
  * below 2^-39, summed in binary32, in an order that sizes and the number of matrices decide (a call repeats bit for bit; a matrix alone and the same
- * among others may differ in their last bits).  A matrix that holds an infinity or a NaN gives NaN; one of zeros gives zeros.  The coefficients have to keep the singular values, which begin at 1 or
- * below, under 2, and a + b s^2 + c s^4 of them within 8 (TNG_ERR_UNSUPPORTED otherwise); the optimiser Muon's (3.4445, -4.775, 2.0315), and
- * (1.5, -0.5, 0) and (1.875, -1.25, 0.375), whose values approach 1, do. */
+ * among others may differ in their last bits).  A matrix that holds an infinity or a NaN gives NaN; one of zeros gives zeros.
+ * The coefficients have to keep the singular values, which begin at 1 or below, under 2, and a + b s^2 + c s^4 of them within 8 (TNG_ERR_UNSUPPORTED
+ * otherwise); the optimiser Muon's (3.4445, -4.775, 2.0315), and (1.5, -0.5, 0) and (1.875, -1.25, 0.375), whose values approach 1, do. */
 typedef struct {
   const float* coefficients; /* host float[steps][3], finite */
   uint32_t steps;            /* 1 .. 64                      */

@@ -608,7 +608,8 @@ uint32_t grad_parts(const Extent& n) {
   const uint64_t groups = n.cols <= 1024 ? kBlock / kWave : 1;  // rows that a workgroup has at a time
   // (268 MB of bfloat16, us, with 256 / 512 / 768 / 1024 workgroups: 65536 x 256 (half of that) 79 / 53 / 48 / 48, 8192 x 4096 75 / 54 / 53 / 55, 4096 x 8192
   // 59 / 56 / 69 / 68, 2048 x 16384 64 / 71 / 81 / 87)
-  const uint64_t most = n.cols <= 512 ? 1024 : n.cols <= 1024 ? 512 : n.cols <= 4096 ? 768 : n.cols <= 8192 ? 512 : n.cols <= kHeldCols ? 256 : 512, tiles = n.cols > kHeldCols ? (n.cols + kBlock * 8 - 1) / (kBlock * 8) : 1;
+  const uint64_t most = n.cols <= 512 ? 1024 : n.cols <= 1024 ? 512 : n.cols <= 4096 ? 768 : n.cols <= 8192 ? 512 : n.cols <= kHeldCols ? 256 : 512;
+  const uint64_t tiles = n.cols > kHeldCols ? (n.cols + kBlock * 8 - 1) / (kBlock * 8) : 1;
   const uint64_t each = std::max<uint64_t>(1, most / (n.workers * tiles)), rows = (n.rows + groups - 1) / groups;
   if (rows <= kTurns) return 1;
   return (uint32_t)std::min(each, rows);
