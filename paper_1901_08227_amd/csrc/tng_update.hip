@@ -9,6 +9,7 @@
 // in binary32.  That is as exact as binary32 within a factor of two, and three times the work at sixteen times the rate.  Bits of 16 alone would not do: what rounding
 // takes from a direction of small singular value grows with it, by 3.4 a step.
 #include "tng_layer_device.hpp"
+#include "tng_pair_loads.hpp"
 
 #include <algorithm>
 #include <cmath>
@@ -370,50 +371,28 @@ __global__ void __launch_bounds__(WR* WC* kWave) pair_join_kernel(PairTask p) {
                           reinterpret_cast<uint32_t*>(lds + wave * K::kTurnBytes), lane);
 }
 
-// 16 bytes for each lane to LDS, as load_to_lds; from: bytes more, the same for all lanes.
-__device__ __forceinline__ void load_rows_to_lds(uint64_t base, uint32_t bytes, uint32_t offset, uint32_t from, uint32_t lds) {
-  const v4u rsrc = {(uint32_t)base, (uint32_t)(base >> 32) & 0xFFFFu, bytes, 0x00020000u};
-  asm volatile(
-      "s_mov_b32 m0, %0\n\t"
-      "s_nop 3\n\t"
-      "buffer_load_dwordx4 %1, %2, %3 offen lds"
-      :
-      : "s"(lds), "v"(offset), "s"(rsrc), "s"(from)
-      : "memory");
-}
-
 // A workgroup's operands: number j of a wavefront's loads takes 8 rows, a row eight lanes.  Rows behind the last one, and stages behind the last one, are out
 // of bounds: nothing is read, and what the loads clear belongs to no result.
 template <typename K>
 struct Operands {
-  uint64_t a, b;
-  uint32_t bytes_a, bytes_b, offset_a, offset_b, step_a, step_b, lds;
-  int left;  // stages not asked for
-  __device__ __forceinline__ Operands(const PairTask& p, const Work& w, uint32_t lane, uint32_t wave, const char* at) {
-    const uint32_t r0 = w.place.r * K::kRows, c0 = w.place.c * K::kCols;
-    a = reinterpret_cast<uint64_t>(p.a.p) + w.plane * p.a.pitch + r0 * p.a.ld + w.first * 128ull;
-    b = reinterpret_cast<uint64_t>(p.b.p) + w.plane * p.b.pitch + c0 * p.b.ld + w.first * 128ull;
-    bytes_a = (min(p.rows - r0, (uint32_t)K::kRows) - 1) * (uint32_t)p.a.ld + w.stages * 128u;
-    bytes_b = (min(p.cols - c0, (uint32_t)K::kCols) - 1) * (uint32_t)p.b.ld + w.stages * 128u;
-    const uint32_t r = wave * 8 + lane / 8, in_row = (lane % 8 ^ (r >> 1 & 7u)) * 16;  // (rows that loads are apart do not change what pieces are moved by)
-    offset_a = r * (uint32_t)p.a.ld + in_row;
-    offset_b = r * (uint32_t)p.b.ld + in_row;
-    step_a = K::kWaves * 8 * (uint32_t)p.a.ld;
-    step_b = K::kWaves * 8 * (uint32_t)p.b.ld;
-    left = (int)w.stages;
-    lds = (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const char*)at) + wave * 1024;
-  }
+  PairRows a, b;
+  uint32_t offset_a, offset_b, lds;
+  __device__ __forceinline__ Operands(const PairTask& p, const Work& w, uint32_t lane, uint32_t wave, const char* at)
+      : a(PairRows::of(reinterpret_cast<uint64_t>(p.a.p) + w.plane * p.a.pitch, p.a.ld, p.rows, w.place.r * K::kRows, K::kRows, w.first, w.stages)),
+        b(PairRows::of(reinterpret_cast<uint64_t>(p.b.p) + w.plane * p.b.pitch, p.b.ld, p.cols, w.place.c * K::kCols, K::kCols, w.first, w.stages)),
+        offset_a(a.offset(lane, wave)),
+        offset_b(b.offset(lane, wave)),
+        lds((uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const char*)at) + wave * 1024) {}
   __device__ __forceinline__ void load(int j, uint32_t slot) const {
     const bool of_a = j < K::kLoadsOfA;
-    load_rows_to_lds(of_a ? a : b, left > 0 ? (of_a ? bytes_a : bytes_b) : 0u, of_a ? offset_a : offset_b, of_a ? j * step_a : (j - K::kLoadsOfA) * step_b,
-                     lds + slot + j * K::kWaves * 1024);
+    const PairRows::Descriptor d = of_a ? a.from(j * K::kWaves * 8) : b.from((j - K::kLoadsOfA) * K::kWaves * 8);
+    load_to_lds(d.base, d.bytes, of_a ? offset_a : offset_b, lds + slot + j * K::kWaves * 1024);
   }
   __device__ __forceinline__ void next() {
-    --left;
-    a += 128;
-    b += 128;
-    bytes_a -= 128;
-    bytes_b -= 128;
+    a.next();
+    b.next();
+    a.bytes = __builtin_amdgcn_readfirstlane(a.bytes);  // (descriptors lie in scalar registers)
+    b.bytes = __builtin_amdgcn_readfirstlane(b.bytes);
   }
 };
 
