@@ -237,7 +237,7 @@ __device__ __forceinline__ void finish_rows(const PairTask& p, uint32_t plane, b
       if (END == kLast) {
         if (r >= p.rows || c >= p.cols) continue;
 #pragma unroll
-        for (int n = 0; n < 4; ++n) v[n] = sum[a][b][n] * p.scale;
+        for (int n = 0; n < 4; ++n) v[n] = sum[a][b][n] * (1.f / (kOfPoly * kOfX)) * p.scale;
         store_n_within<T, 4>(static_cast<T*>(p.y.p) + plane * p.y.pitch + c * p.y.ld + r, p.rows - r, v);
         continue;
       }
@@ -815,8 +815,9 @@ struct Small {
     __syncthreads();
   }
 
-  // P X times unit, in the place of X.
-  __device__ __forceinline__ void apply(const Fragments& high, const Fragments& low, float unit, Strip& x) const {
+  // P X times unit, a power of two, and then times scale, in the place of X.  (One product for both would be a subnormal number of few bits for scales that
+  // results with it are not.)
+  __device__ __forceinline__ void apply(const Fragments& high, const Fragments& low, float unit, float scale, Strip& x) const {
 #pragma unroll
     for (int a = 0; a < NT; ++a) {
       v4f all[CT] = {};
@@ -835,7 +836,7 @@ struct Small {
 #pragma unroll
       for (int b = 0; b < CT; ++b)
 #pragma unroll
-        for (int k = 0; k < 4; ++k) x[a][b][k] = all[b][k] * unit;
+        for (int k = 0; k < 4; ++k) x[a][b][k] = all[b][k] * unit * scale;
     }
   }
 };
@@ -897,7 +898,8 @@ __global__ void __launch_bounds__(kSmallWaves* kWave) small_kernel(SmallTask p) 
     }
     __syncthreads();
     all.polynomial(p.abc[3 * step], p.abc[3 * step + 1], p.abc[3 * step + 2]);
-    all.apply(high, low, step + 1 == p.steps ? p.scale * (1.f / (kOfPoly * kOfX)) : kOfX / (kOfPoly * kOfX), x);
+    const bool last = step + 1 == p.steps;
+    all.apply(high, low, last ? 1.f / (kOfPoly * kOfX) : kOfX / (kOfPoly * kOfX), last ? p.scale : 1.f, x);
   }
   with_type(p.of_y, [&](auto of) {
     using T = decltype(of);
@@ -955,7 +957,7 @@ __global__ void __launch_bounds__(kSmallWaves* kWave) strip_kernel(StripTask p) 
     __syncthreads();
     all.polynomial(p.plus, p.times, p.square);
     const bool last = p.step == p.steps;
-    all.apply(high, low, last ? p.scale * (1.f / (kOfPoly * kOfX)) : kOfX / (kOfPoly * kOfX), x);
+    all.apply(high, low, last ? 1.f / (kOfPoly * kOfX) : kOfX / (kOfPoly * kOfX), last ? p.scale : 1.f, x);
     if (last) {
       with_type(p.of_y, [&](auto of) {
         using T = decltype(of);
@@ -1201,7 +1203,7 @@ hipError_t launch_orthogonalize(tng_type of_x, tng_type of_y, const Extent& e, c
     apply.by_r = l.x_by_n;
     apply.by_c = then;
     apply.y = y;
-    apply.scale = scale * (1.f / (kOfPoly * kOfX));
+    apply.scale = scale;
     if (!last) {
       product<float, kApply>(apply, s);
     } else {
