@@ -24,9 +24,9 @@ def orthogonalize(x, coefficients=(QUINTIC,) * 5, eps=1e-7, scale=1.0, out=None)
     device = x.device
     if device.type != "cuda":
         raise TypeError("x: expected a CUDA tensor")
-    flat = [float(v) for step in coefficients for v in step]
-    if len(flat) != 3 * len(coefficients):
+    if any(len(step) != 3 for step in coefficients):
         raise ValueError("coefficients: expected (a, b, c) for each step")
+    flat = [float(v) for step in coefficients for v in step]
     if out is None:
         got = lowbit._make("tng_orthogonalize", device, "mjow", x, (*flat, float(eps), float(scale)))
         if got is not None:
