@@ -361,7 +361,7 @@ tng_status tng_linear_i8(void* hip_stream, const tng_drop* drop, const tng_matri
 /* Root-mean-square norm of rows, with the addition of a residual in front:
  *   h = x + residual (NULL: x), rounded to x's type;  s = 1 / sqrt(mean h^2 + eps);  y = h s weight
  * in binary32, from h as it is stored: the same, bit for bit, as an addition by itself and the norm of its result.  A row of h that holds an infinity or
- * a NaN gives NaN; squares beyond binary32 are none of those (they are taken of h 2^-70 then).  Sums of a row: binary32, in a fixed order. */
+ * a NaN gives NaN; squares beyond binary32 are none of those (they are taken of h 2^-80 then).  Sums of a row: binary32, in a fixed order. */
 typedef struct {
   const float* weight; /* device float[cols], one for all workers; NULL: 1     */
   float eps;           /* FLT_MIN .. 2^64: rows of zeros give zeros            */

@@ -126,11 +126,12 @@ struct Joint {
 
 // 1 / sqrt(mean + eps) from the sum of squares.  squares(f): the sum of (h f)^2, taken again where the squares of large numbers are beyond
 // binary32 (eps is nothing beside them).  A row that holds what is not finite is NaN as a whole.
+// f = 2^-80: of 2^22 numbers below 2^128 the sum stays below 2^118, and of a sum beyond 2^128 it is above 2^-32, beside which squares that vanish count nothing.
 template <typename F>
 __device__ __forceinline__ float inverse_root(float sum, float eps, uint64_t cols, F squares) {
   if (!(sum <= FLT_MAX)) {
-    const float less = squares(0x1p-70f);
-    return less <= FLT_MAX ? 0x1p-70f / sqrtf(less / (float)cols) : __uint_as_float(0x7FC00000u);
+    const float less = squares(0x1p-80f);
+    return less <= FLT_MAX ? 0x1p-80f / sqrtf(less / (float)cols) : __uint_as_float(0x7FC00000u);
   }
   return 1.0f / sqrtf(sum / (float)cols + eps);
 }
