@@ -368,11 +368,11 @@ typedef struct {
 } tng_rms;
 
 /* Matrices of one type (F32, BF16, F16) and size, limits as for tng_quantize_rows; residual and h may be NULL (h: not wanted).  h and y may be x or
- * residual, but not both the same. */
+ * residual (a result that begins where an input does has to be that matrix, of its type and strides), but not both the same. */
 tng_status tng_rms_norm(void* hip_stream, const tng_matrix* x, const tng_matrix* residual, const tng_rms* norm, const tng_matrix* h,
                         const tng_matrix* y);
 /* The rows of y, before a rounding to x's type, as tng_quantize_rows codes them: q, scale[workers][rows], and with qt (NULL: not wanted) the same
- * codes turned. */
+ * codes turned; codes do not lie where another matrix does. */
 tng_status tng_rms_norm_codes(void* hip_stream, const tng_matrix* x, const tng_matrix* residual, const tng_rms* norm, const tng_matrix* h,
                               const tng_matrix* q, float* scale, const tng_matrix* qt);
 /* With g = weight dy:  dx = s (g - h s^2 mean(g h)) + dresidual,  dw[m] = sum over worker m's rows of dy h s.
@@ -385,7 +385,7 @@ tng_status tng_rms_norm_grad(void* hip_stream, const tng_matrix* dy, const tng_m
 
 /* Rows of a table by tokens: y[m][t] = scale table[id[m][t]], a product in binary32 rounded to y's type.
  * ids: I32 or I64, rows = tokens of each worker (as x's rows above), cols = 1, any ld; table: F32, BF16 or F16 [vocabulary][cols], one for all workers
- * (workers = 1) or one for each, vocabulary and cols <= 2^22; y: F32, BF16 or F16, not in the table's place; scale: host, NULL: 1.
+ * (workers = 1) or one for each, vocabulary and cols <= 2^22; y: F32, BF16 or F16, not in the table's or the tokens' place; scale: host, NULL: 1.
  * A token below 0 or from `vocabulary` on stands for nothing: its row of y is zeros, and no gradient comes of it. */
 tng_status tng_embed(void* hip_stream, const tng_matrix* ids, const tng_matrix* table, const float* scale, const tng_matrix* y);
 /* dtable[m][v] = scale times the sum of dy[m][t] over the tokens of v, in binary32 and in a fixed order; rows of no token are zeros.  dtable: F32
@@ -409,7 +409,7 @@ typedef struct {
   float scale;               /* finite                       */
 } tng_orthogonal;
 
-/* Each worker's matrix by itself.  x, y: F32, BF16 or F16, of one size, workers * rows <= 2^23, rows and cols <= 65536; y may be x.  No context, stream
+/* Each worker's matrix by itself.  x, y: F32, BF16 or F16, of one size, workers * rows <= 2^23, rows and cols <= 65536; y may be x, of its type and strides.  No context, stream
  * and workspace as for the layer calls. */
 size_t tng_orthogonalize_bytes(const tng_matrix* x);
 tng_status tng_orthogonalize(void* hip_stream, const tng_matrix* x, const tng_orthogonal* plan, const tng_matrix* y, void* workspace,

@@ -115,15 +115,22 @@ bool norm_ok(const tng_rms* n) {
 
 tng::NormArgs norm_args(const tng_rms& n) { return tng::NormArgs{n.weight, n.eps}; }
 
+// Whether two matrices begin at one place.
+bool same_place(const tng_matrix* a, const tng_matrix* b) { return a != nullptr && b != nullptr && !empty(*a) && !empty(*b) && a->data == b->data; }
+
+// Whether a result that may be an input is that, or begins elsewhere: of another type or other strides at its place, what one row's work writes is what
+// another's still reads.
+bool is_or_apart(const tng_matrix* in, const tng_matrix* out) {
+  if (!same_place(in, out)) return true;
+  return in->type == out->type && (in->rows <= 1 || in->ld == out->ld) && (in->workers == 1 || in->pitch == out->pitch);
+}
+
 // x and what goes with it in front of a norm; the matrices that may be absent are of x's type and size where they are there.
 bool normed_ok(const tng_matrix* x, const tng_matrix* residual, const tng_rms* norm, const tng_matrix* h) {
   if (!norm_ok(norm) || !sound(x, false) || !is_float(x->type) || !sides_ok(x)) return false;
   if (residual != nullptr && (!sound(residual, false) || residual->type != x->type || !same_size(x, residual))) return false;
-  return h == nullptr || (sound(h, true) && h->type == x->type && same_size(x, h));
+  return h == nullptr || (sound(h, true) && h->type == x->type && same_size(x, h) && is_or_apart(x, h) && is_or_apart(residual, h));
 }
-
-// Whether two results begin at one place.
-bool same_place(const tng_matrix* a, const tng_matrix* b) { return a != nullptr && b != nullptr && !empty(*a) && !empty(*b) && a->data == b->data; }
 
 // Tokens and the matrix with a row for each of them.
 bool tokens_ok(const tng_matrix* ids, const tng_matrix* rows, bool output) {
@@ -264,6 +271,7 @@ tng_status tng_rms_norm(void* hip_stream, const tng_matrix* x, const tng_matrix*
                         const tng_matrix* y) {
   if (!normed_ok(x, residual, norm, h) || !sound(y, true) || y->type != x->type || !same_size(x, y) || same_place(h, y))
     return TNG_ERR_INVALID_ARG;
+  if (!is_or_apart(x, y) || !is_or_apart(residual, y)) return TNG_ERR_INVALID_ARG;
   if (empty(*x)) return TNG_OK;
   return hip_status(tng::launch_rms_norm((tng_type)x->type, extent(x), view(x), view(residual), norm_args(*norm), view(h), view(y), nullptr,
                                          static_cast<hipStream_t>(hip_stream)));
@@ -274,6 +282,9 @@ tng_status tng_rms_norm_codes(void* hip_stream, const tng_matrix* x, const tng_m
   if (!normed_ok(x, residual, norm, h) || !sound(q, true) || q->type != TNG_TYPE_I8 || !same_size(x, q)) return TNG_ERR_INVALID_ARG;
   if (qt != nullptr && (!sound(qt, true) || qt->type != TNG_TYPE_I8 || qt->workers != x->workers || qt->rows != x->cols || qt->cols != x->rows))
     return TNG_ERR_INVALID_ARG;
+  for (const tng_matrix* codes : {q, qt})
+    if (same_place(x, codes) || same_place(residual, codes) || same_place(h, codes)) return TNG_ERR_INVALID_ARG;
+  if (same_place(q, qt)) return TNG_ERR_INVALID_ARG;
   if (x->rows == 0) return TNG_OK;
   if (scale == nullptr || !aligned(scale, 4)) return TNG_ERR_INVALID_ARG;
   const hipStream_t s = static_cast<hipStream_t>(hip_stream);
@@ -293,6 +304,7 @@ tng_status tng_rms_norm_grad(void* hip_stream, const tng_matrix* dy, const tng_m
                              const tng_matrix* dx, float* dw, void* workspace, size_t workspace_bytes) {
   if (!normed_ok(dy, h, norm, dx) || h == nullptr || dx == nullptr || !aligned(dw, 4)) return TNG_ERR_INVALID_ARG;
   if (dresidual != nullptr && (!sound(dresidual, false) || dresidual->type != dy->type || !same_size(dy, dresidual))) return TNG_ERR_INVALID_ARG;
+  if (!is_or_apart(dresidual, dx)) return TNG_ERR_INVALID_ARG;
   if (dy->cols == 0 || (dy->rows == 0 && dw == nullptr)) return TNG_OK;
   if (workspace == nullptr || !aligned(workspace, 256) || workspace_bytes < tng_rms_norm_grad_bytes(dy)) return TNG_ERR_WORKSPACE;
   return hip_status(tng::launch_rms_norm_grad((tng_type)dy->type, extent(dy), view(dy), view(h), view(dresidual), norm_args(*norm), view(dx), dw,
@@ -302,6 +314,7 @@ tng_status tng_rms_norm_grad(void* hip_stream, const tng_matrix* dy, const tng_m
 tng_status tng_embed(void* hip_stream, const tng_matrix* ids, const tng_matrix* table, const float* scale, const tng_matrix* y) {
   if (!tokens_ok(ids, y, true) || !scale_ok(scale) || !sound(table, false) || !is_float(table->type)) return TNG_ERR_INVALID_ARG;
   if (table->rows > kMaxSide || table->cols != y->cols || (table->workers != 1 && table->workers != y->workers)) return TNG_ERR_INVALID_ARG;
+  if (same_place(table, y) || same_place(ids, y)) return TNG_ERR_INVALID_ARG;
   if (empty(*y)) return TNG_OK;
   tng::View rows = view(table);
   if (table->workers == 1) rows.pitch = 0;
@@ -328,7 +341,7 @@ size_t tng_orthogonalize_bytes(const tng_matrix* x) { return update_ok(x) ? 256 
 
 tng_status tng_orthogonalize(void* hip_stream, const tng_matrix* x, const tng_orthogonal* plan, const tng_matrix* y, void* workspace,
                              size_t workspace_bytes) {
-  if (!sound(x, false) || !sound(y, true) || !update_ok(x) || !is_float(y->type) || !same_size(x, y)) return TNG_ERR_INVALID_ARG;
+  if (!sound(x, false) || !sound(y, true) || !update_ok(x) || !is_float(y->type) || !same_size(x, y) || !is_or_apart(x, y)) return TNG_ERR_INVALID_ARG;
   if (plan == nullptr || plan->coefficients == nullptr || plan->steps < 1 || plan->steps > 64) return TNG_ERR_INVALID_ARG;
   if (!(plan->eps >= FLT_MIN && plan->eps <= FLT_MAX) || !std::isfinite(plan->scale)) return TNG_ERR_INVALID_ARG;
   for (uint32_t k = 0; k < 3 * plan->steps; ++k)
