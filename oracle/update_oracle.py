@@ -29,3 +29,38 @@ def orthogonalize(x, coefficients, eps, scale, roundings=None):
         x = new
     x = (x.T if tall else x) * scale
     return (x, error * abs(scale)) if roundings else x
+
+
+def kept(v, bits):
+    """v with so many significant bits."""
+    m, e = np.frexp(v)
+    return np.ldexp(np.rint(np.ldexp(m, bits)), e - bits)
+
+
+def in_bits(x, coefficients, eps, bits, result=24):
+    """One matrix with no more rows than columns, as products of operands of so many significant bits make it: bits has those of the operands of X X^T, of G G and
+    of P X (P's, X's).  Sums in binary64, everything that they give rounded to `result` bits."""
+    x = kept(x.astype(np.float64) / (np.linalg.norm(x.astype(np.float64)) + eps), result)
+    for a, b, c in coefficients:
+        y = kept(x, bits["gram"])
+        g = kept(y @ y.T, result)
+        h = kept(g, bits["square"])
+        p = kept(a * np.eye(len(g)) + b * g + c * (h @ h), result)
+        x = kept(kept(p, bits["poly"]) @ kept(x, bits["apply"]), result)
+    return x
+
+
+def step_in(x, coefficients, eps, dtype=np.float32):
+    """The same in numpy's products of a type."""
+    x = (x.astype(np.float64) / (np.linalg.norm(x.astype(np.float64)) + eps)).astype(dtype)
+    for a, b, c in np.asarray(coefficients, dtype):
+        g = x @ x.T
+        x = a * x + (b * g + c * (g @ g)) @ x
+    return x
+
+
+def as_binary32(got, want, plain):
+    """Whether a result is as near to binary64's (want) as binary32's own (plain) is, within a factor of four; where little is summed binary32 rounds a X once, and
+    pairs of 22 bits show three of their roundings, 3 2^-22."""
+    size = np.linalg.norm
+    return bool(size(got - want) <= 4 * size(plain - want) + 3 * 2.0 ** -22 * size(want))
