@@ -397,9 +397,11 @@ tng_status tng_embed_grad(void* hip_stream, const tng_matrix* ids, const tng_mat
 /* ---- The update of a matrix -----------------------------------------------------------------------------------------
  * A decoded average (or what a momentum makes of it) whose singular values are brought near 1 before the step:
  *   X = x / (||x|| + eps);  for each of the steps, with its a, b, c:  G = X X^T,  X = (a + b G + c G G) X;  y = scale X
- * ||x||: the root of the sum of squares, in binary64.  Products are of pairs of binary16 that hold 22 bits of a number and more, but nothing
- * below 2^-39, summed in binary32, in an order that sizes and the number of matrices decide (a call repeats bit for bit; a matrix alone and the same
- * among others may differ in their last bits).  A matrix that holds an infinity or a NaN gives NaN; one of zeros gives zeros.
+ * ||x||: the root of the sum of squares, in binary64.  X is binary32 from step to step.  Products are of pairs of binary16 that hold 22 bits of a number and more, but
+ * of a row (and of a column) of X nothing below 2^-39 of what the steps so far can have made of its norm; norms within 2^10 of the longest may be taken as that,
+ * and norms below 2^-60 are taken as 2^-60.  They are summed in binary32, in an order that sizes and the number of matrices decide (a call repeats bit for bit; a
+ * matrix alone and the same among others may differ in their last bits).  Every row and column comes out as near to the exact one as by binary32's products,
+ * within a factor of four and 3 2^-22.  A matrix that holds an infinity or a NaN gives NaN; one of zeros gives zeros.
  * The coefficients have to keep the singular values, which begin at 1 or below, under 2, and a + b s^2 + c s^4 of them within 8 (TNG_ERR_UNSUPPORTED
  * otherwise); the optimiser Muon's (3.4445, -4.775, 2.0315), and (1.5, -0.5, 0) and (1.875, -1.25, 0.375), whose values approach 1, do. */
 typedef struct {
@@ -409,8 +411,8 @@ typedef struct {
   float scale;               /* finite                       */
 } tng_orthogonal;
 
-/* Each worker's matrix by itself.  x, y: F32, BF16 or F16, of one size, workers * rows <= 2^23, rows and cols <= 65536; y may be x, of its type and strides.  No context, stream
- * and workspace as for the layer calls. */
+/* Each worker's matrix by itself.  x, y: F32, BF16 or F16, of one size, workers * rows <= 2^23, rows and cols <= 65536; y may be x, of its type and strides.
+ * No context, stream and workspace as for the layer calls. */
 size_t tng_orthogonalize_bytes(const tng_matrix* x);
 tng_status tng_orthogonalize(void* hip_stream, const tng_matrix* x, const tng_orthogonal* plan, const tng_matrix* y, void* workspace,
                              size_t workspace_bytes);

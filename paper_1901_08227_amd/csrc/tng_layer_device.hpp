@@ -138,6 +138,12 @@ __device__ __forceinline__ uint32_t pack4(uint32_t a, uint32_t b, uint32_t c, ui
   return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0C0C0400u), __builtin_amdgcn_perm(b, a, 0x0C0C0400u), 0x05040100u);
 }
 
+// x and the lane's that a data-parallel control names, in the rows of 16 lanes that ROWS has.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float plus_other(float x) {
+  return x + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, ROWS, 0xF, false));
+}
+
 // ---- Tiles of the products: loads that go to LDS directly.
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 

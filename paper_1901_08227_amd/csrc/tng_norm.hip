@@ -70,10 +70,6 @@ __device__ __forceinline__ void load_weight(const float* weight, const Eight& e,
   }
 }
 
-template <int CTRL, int ROWS>
-__device__ __forceinline__ float plus_other(float x) {
-  return x + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, ROWS, 0xF, false));
-}
 __device__ __forceinline__ float wave_sum(float x) {
   x = plus_other<0xB1, 0xF>(x);  // the neighbour, the pair, the half and the row of 16
   x = plus_other<0x4E, 0xF>(x);
